@@ -330,6 +330,106 @@ kmq_status kmq_quantize_blockscaled(const uint16_t* Wdense, int64_t N, int64_t K
                                     uint32_t* packed, uint16_t* codebook, uint16_t* scales,
                                     void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- Between the QKV product and the output product ----------------------------------
+ * A decoder layer's attention at inference: heads normalised and rotated, keys and values held in
+ * 4 bits, attention over them.  Rows of heads are what the products of this library leave: M rows
+ * of bf16, heads one after the other, `stride` elements from row to row.
+ *
+ * Strides are multiples of 8 elements, at least as long as the row's heads (KMQ_ERR_SHAPE); rows
+ * start 16-byte aligned.  A call with 0 rows does nothing and succeeds.  Outputs overlap no input,
+ * but where a call says so. */
+
+/* What turns a head: RMSNorm, then the rotation of its first rotary_dim elements by position.
+ *     n_i = x_i * gain_i / sqrt( (1/D) sum_j x_j^2 + eps )                 (rmsnorm = 1; else n = x)
+ *     a_i = position * inv_freq[i],  i = 0 .. rotary_dim/2 - 1
+ *     left  = n_l cos a_i - n_r sin a_i,   right = n_r cos a_i + n_l sin a_i
+ *     (l, r) = (i, i + rotary_dim/2), or (2i, 2i + 1) where `interleaved` is 1
+ * Computed in 64 bits, rounded to 32 and then to bf16 (nearest even).  rotary_dim is a multiple of 16, at
+ * most the head's size; 0: no rotation, and positions and inv_freq are not looked at.  A host structure, read
+ * during the call; what it points to is device memory. */
+typedef struct kmq_head_turn {
+    const int32_t* positions;   /* one a row; NULL (kmq_kv_append only): the row's position in the cache */
+    const float* inv_freq;      /* rotary_dim / 2 */
+    const uint16_t* q_gain;     /* head_dim bf16, 16-byte aligned, or NULL: unit gains */
+    const uint16_t* k_gain;
+    float eps;                  /* >= 0 (looked at where rmsnorm is 1) */
+    int32_t rmsnorm, rotary_dim, interleaved;
+} kmq_head_turn;
+
+/* Queries and keys turned, in one launch.  qk: `rows` rows of q_heads + k_heads heads (either may be 0) of
+ * head_dim elements, 8 to 512, a multiple of 8.  q_out, k_out: their own rows; they may be the input's own
+ * places (q_out = qk, k_out = qk + q_heads * head_dim, same strides).  turn->positions is required with a rotation. */
+kmq_status kmq_qk_norm_rope(const uint16_t* qk, int64_t qk_stride, int64_t rows, int q_heads, int k_heads, int head_dim,
+                            const kmq_head_turn* turn, uint16_t* q_out, int64_t q_stride, uint16_t* k_out, int64_t k_stride,
+                            void* hip_stream);
+
+/* The key / value cache: the block-scaled format above at 4 bits.  K and V have a codebook of 16 bf16 centroids
+ * each, ascending; every KMQ_BLOCK = 64 elements of a token's head have a bf16 scale, the largest
+ * magnitude among them.  (kmq_quantize_blockscaled on a sample of K or V rows gives such a codebook.)
+ *     index = number of boundaries b_j, j = 0..14, with x > b_j * scale    (scale 0: x > b_j), compared exactly
+ *     b_j   = (c_j + c_(j+1)) / 2, the sum rounded to fp32;   value = c[index] * scale
+ * A block with a NaN or an infinity has the largest of its bit patterns without sign as scale; its indices are some.
+ * A cache is num_pages pages of kmq_kv_page_bytes bytes; a page holds page_size tokens of every head.
+ *     page: [kv_heads][page_size / 16] tiles of 16 tokens, 17 * D bytes each (D = head_dim):
+ *     K     byte ((d/16 % 4) * 16 + t) * D/8 + (d/64) * 8 + (d % 16) / 2            low nibble: even d
+ *     V     byte 8 D + ((t/4) * 16 + d % 16) * D/8 + (d/32) * 4 + t % 4            low nibble: d % 32 < 16
+ *     scale bf16 at byte 16 D + ((t/4 * 2 + (0: K, 1: V)) * D/64 + d/64) * 8 + (t % 4) * 2
+ * for element d of token t (0..15) of the tile.  Pages need not be initialised.  Host structures, read during the call. */
+typedef struct kmq_kv_cache {
+    void* pages;                /* device, 16-byte aligned */
+    const uint16_t* codebooks;  /* device, 2 x 16 bf16: K's, then V's; 4-byte aligned */
+    int64_t num_pages;
+    int32_t page_size;          /* tokens: a multiple of 32 (a cache without pages: one page a sequence) */
+    int32_t kv_heads;
+    int32_t head_dim;           /* 64, 128 or 256 */
+} kmq_kv_cache;
+
+/* Which rows belong to which sequence, and where its tokens are.  Row row_starts[b] + i of sequence b, i < n = row_starts[b+1] -
+ * row_starts[b], stands at position lengths[b] - n + i: the rows are the sequence's last ones, and lengths counts them.
+ * Position p is token p % page_size of page page_table[b][p / page_size].  row_starts ascends from 0; rows from
+ * row_starts[sequences] on belong to no sequence, and every call leaves theirs as it was.  NULL: one row a sequence.
+ * A position outside 0 .. table_width * page_size - 1 or on a page outside 0 .. num_pages - 1 is not in the cache: writing it
+ * does nothing, reading it gives zeros, attention passes over it.  A page that is written belongs to one sequence. */
+typedef struct kmq_kv_batch {
+    const int32_t* page_table;  /* device, sequences x table_width */
+    const int32_t* lengths;     /* device, sequences */
+    const int32_t* row_starts;  /* device, sequences + 1, or NULL (then rows = sequences) */
+    int64_t rows;               /* rows of the tensors of the call */
+    int32_t sequences, table_width;   /* table_width * page_size < 2^31 */
+} kmq_kv_batch;
+
+/* Bytes of a page, 17/16 * page_size * kv_heads * head_dim; -1 on bad arguments. */
+int64_t kmq_kv_page_bytes(int page_size, int kv_heads, int head_dim);
+
+/* K and V rows (kv_heads heads each) quantised into their places in the cache. */
+kmq_status kmq_kv_write(const kmq_kv_cache* cache, const kmq_kv_batch* batch, const uint16_t* k, int64_t k_stride,
+                        const uint16_t* v, int64_t v_stride, void* hip_stream);
+
+/* The rows' places in the cache as bf16(c[index] * scale). */
+kmq_status kmq_kv_read(const kmq_kv_cache* cache, const kmq_kv_batch* batch, uint16_t* k, int64_t k_stride,
+                       uint16_t* v, int64_t v_stride, void* hip_stream);
+
+/* From the fused QKV product to the attention in one launch: rows of q_heads + 2 * kv_heads heads; queries turned into q_out
+ * (which may be their own place), keys turned and quantised, values quantised.  Bit for bit what kmq_qk_norm_rope and
+ * kmq_kv_write on its keys give. */
+kmq_status kmq_kv_append(const kmq_kv_cache* cache, const kmq_kv_batch* batch, const uint16_t* qkv, int64_t qkv_stride,
+                         int q_heads, const kmq_head_turn* turn, uint16_t* q_out, int64_t q_stride, void* hip_stream);
+
+/* Attention of the batch's rows over the cache.  Query head h reads key head h / (q_heads / kv_heads).
+ *     S_j = scale * q . K_j,    out = sum_j exp(S_j) V_j / sum_j exp(S_j)
+ * over the positions j of the row's sequence that are in the cache, below lengths, with j <= p (causal = 1) and j > p - window
+ * (window > 0), p the row's position.  A row that sees none is zero.  Sums in fp32, one rounding to bf16.
+ *   lse        rows x q_heads fp32, log sum_j exp(S_j) (minus infinity where none is seen), or NULL
+ *   workspace  kmq_kv_attention_workspace_bytes() bytes, 16-byte aligned, not initialised: where the rows are too few to fill the
+ *              compute units, the tokens are split over workgroups, and a second kernel joins the parts in their order
+ * The size depends on the structures' numbers alone, not on lengths, so a captured call may be replayed with others. */
+size_t kmq_kv_attention_workspace_bytes(const kmq_kv_cache* cache, const kmq_kv_batch* batch, int q_heads);
+kmq_status kmq_kv_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch, const uint16_t* q, int64_t q_stride, int q_heads,
+                            float scale, int causal, int window, uint16_t* out, int64_t out_stride, float* lse,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
+/* As kmq_kernel_name, for the attention. */
+const char* kmq_kernel_name_kv_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch, int q_heads);
+
 /* Name of the kernel variant the launch heuristic picks for this problem
  * (static string, never NULL; "invalid" on bad arguments).  For reports. */
 const char* kmq_kernel_name(int64_t N, int64_t K, int bits, int M, int layout);

@@ -204,6 +204,62 @@ static kmq_status check_and_run(const GemmArgs& a_in, void* stream, bool library
     return hip_status(e);
 }
 
+// ---- cache, batch and heads: what every call on them checks ----
+static bool row_of_heads(const void* p, int64_t stride, int64_t heads, int head_dim) {   // (the pointer is checked apart)
+    return p && stride % 8 == 0 && stride >= heads * head_dim && stride <= (int64_t(1) << 31);
+}
+constexpr int64_t kMaxHeads = 4096;
+constexpr int kMaxSequences = 1 << 20;
+
+static kmq_status check_cache(const kmq_kv_cache* c) {
+    if (!c || !c->pages || !c->codebooks) return KMQ_ERR_NULL;
+    if (kmq_kv_page_bytes(c->page_size, c->kv_heads, c->head_dim) < 0 || c->num_pages < 1 || c->num_pages > 0x7FFFFFFF) return KMQ_ERR_SHAPE;
+    if (!aligned(c->pages, 16) || !aligned(c->codebooks, 4)) return KMQ_ERR_ALIGN;
+    return KMQ_OK;
+}
+
+static kmq_status check_batch(const kmq_kv_cache* c, const kmq_kv_batch* b) {
+    if (!b || !b->page_table || !b->lengths) return KMQ_ERR_NULL;
+    if (b->sequences < 1 || b->sequences > kMaxSequences || b->table_width < 1 || b->rows < 0 || b->rows > kMaxDim) return KMQ_ERR_SHAPE;
+    if (!b->row_starts && b->rows != b->sequences) return KMQ_ERR_SHAPE;
+    if (static_cast<int64_t>(b->table_width) * c->page_size > 0x7FFFFFFF) return KMQ_ERR_SHAPE;   // positions are 32-bit numbers
+    if (!aligned(b->page_table, 4) || !aligned(b->lengths, 4) || !aligned(b->row_starts, 4)) return KMQ_ERR_ALIGN;
+    return KMQ_OK;
+}
+
+static kmq_status check_cached(const kmq_kv_cache* c, const kmq_kv_batch* b) {
+    const kmq_status s = check_cache(c);
+    return s != KMQ_OK ? s : check_batch(c, b);
+}
+
+static KvCacheArgs cache_args(const kmq_kv_cache* c) {
+    return {static_cast<uint8_t*>(c->pages), c->codebooks, c->num_pages, c->page_size, c->kv_heads, c->head_dim};
+}
+static KvBatchArgs batch_args(const kmq_kv_batch* b) {
+    return {b->page_table, b->lengths, b->row_starts, b->rows, b->sequences, b->table_width};
+}
+
+// Norm and rotation of heads of `head_dim` elements; `positions` may be missing where the cache gives them.
+static kmq_status check_turn(const kmq_head_turn* t, int head_dim, bool positions_given) {
+    if (!t) return KMQ_ERR_NULL;
+    if ((t->rmsnorm != 0 && t->rmsnorm != 1) || (t->interleaved != 0 && t->interleaved != 1) || (t->rmsnorm && !(t->eps >= 0.f))) return KMQ_ERR_SHAPE;
+    if (t->rotary_dim < 0 || t->rotary_dim > head_dim || t->rotary_dim % 16) return KMQ_ERR_SHAPE;
+    if (t->rotary_dim && (!t->inv_freq || !positions_given)) return KMQ_ERR_NULL;
+    if (t->rmsnorm && (!aligned(t->q_gain, 16) || !aligned(t->k_gain, 16))) return KMQ_ERR_ALIGN;
+    if (t->rotary_dim && (!aligned(t->inv_freq, 4) || !aligned(t->positions, 4))) return KMQ_ERR_ALIGN;
+    return KMQ_OK;
+}
+static void set_turn(HeadsArgs& a, const kmq_head_turn* t) {
+    a.norm = t->rmsnorm != 0;
+    a.q_gain = t->q_gain;
+    a.k_gain = t->k_gain;
+    a.eps = t->eps;
+    a.rotary_dim = t->rotary_dim;
+    a.interleaved = t->interleaved != 0;
+    a.positions = t->positions;
+    a.inv_freq = t->inv_freq;
+}
+
 }  // namespace kmq
 
 extern "C" {
@@ -398,6 +454,131 @@ kmq_status kmq_dequant_blockscaled(const uint32_t* W, const uint16_t* codebook, 
         (reinterpret_cast<uintptr_t>(scales) & 1) || (reinterpret_cast<uintptr_t>(Wdense) & 15)) return KMQ_ERR_ALIGN;
     return kmq::hip_status(kmq::launch_dequant_blockscaled(W, codebook, scales, Wdense, N, K, bits,
                                                            static_cast<hipStream_t>(hip_stream)));
+}
+
+int64_t kmq_kv_page_bytes(int page_size, int kv_heads, int head_dim) {
+    if (head_dim != 64 && head_dim != 128 && head_dim != 256) return -1;
+    if (page_size < 32 || page_size % 32 || page_size > (1 << 30) || kv_heads < 1 || kv_heads > kmq::kMaxHeads) return -1;
+    return static_cast<int64_t>(kv_heads) * (page_size / 16) * (17 * head_dim);
+}
+
+kmq_status kmq_qk_norm_rope(const uint16_t* qk, int64_t qk_stride, int64_t rows, int q_heads, int k_heads, int head_dim,
+                            const kmq_head_turn* turn, uint16_t* q_out, int64_t q_stride, uint16_t* k_out, int64_t k_stride,
+                            void* hip_stream) {
+    if (!qk || !turn || (q_heads > 0 && !q_out) || (k_heads > 0 && !k_out)) return KMQ_ERR_NULL;
+    if (rows < 0 || rows > kmq::kMaxDim || q_heads < 0 || k_heads < 0 || q_heads > kmq::kMaxHeads || k_heads > kmq::kMaxHeads ||
+        q_heads + k_heads < 1 || head_dim < 8 || head_dim > 512 || head_dim % 8) return KMQ_ERR_SHAPE;
+    const kmq_status t = kmq::check_turn(turn, head_dim, turn->positions != nullptr);
+    if (t != KMQ_OK) return t;
+    if (!kmq::row_of_heads(qk, qk_stride, int64_t(q_heads) + k_heads, head_dim) || (q_heads && !kmq::row_of_heads(q_out, q_stride, q_heads, head_dim)) ||
+        (k_heads && !kmq::row_of_heads(k_out, k_stride, k_heads, head_dim))) return KMQ_ERR_SHAPE;
+    if (!kmq::aligned(qk, 16) || !kmq::aligned(q_out, 16) || !kmq::aligned(k_out, 16)) return KMQ_ERR_ALIGN;
+    kmq::HeadsArgs a;
+    a.q = qk;
+    a.k = qk + static_cast<int64_t>(q_heads) * head_dim;
+    a.q_stride = a.k_stride = qk_stride;
+    a.rows = rows;
+    a.q_heads = q_heads;
+    a.k_heads = k_heads;
+    a.head_dim = head_dim;
+    kmq::set_turn(a, turn);
+    a.q_out = q_out;
+    a.k_out = k_out;
+    a.q_out_stride = q_stride;
+    a.k_out_stride = k_stride;
+    return kmq::hip_status(kmq::launch_heads(a, nullptr, nullptr, static_cast<hipStream_t>(hip_stream)));
+}
+
+kmq_status kmq_kv_write(const kmq_kv_cache* cache, const kmq_kv_batch* batch, const uint16_t* k, int64_t k_stride,
+                        const uint16_t* v, int64_t v_stride, void* hip_stream) {
+    if (!k || !v) return KMQ_ERR_NULL;
+    const kmq_status c = kmq::check_cached(cache, batch);
+    if (c != KMQ_OK) return c;
+    if (!kmq::row_of_heads(k, k_stride, cache->kv_heads, cache->head_dim) || !kmq::row_of_heads(v, v_stride, cache->kv_heads, cache->head_dim)) return KMQ_ERR_SHAPE;
+    if (!kmq::aligned(k, 16) || !kmq::aligned(v, 16)) return KMQ_ERR_ALIGN;
+    kmq::HeadsArgs a;
+    a.k = k;
+    a.v = v;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.rows = batch->rows;
+    a.k_heads = a.v_heads = cache->kv_heads;
+    a.head_dim = cache->head_dim;
+    const kmq::KvCacheArgs ca = kmq::cache_args(cache);
+    const kmq::KvBatchArgs ba = kmq::batch_args(batch);
+    return kmq::hip_status(kmq::launch_heads(a, &ca, &ba, static_cast<hipStream_t>(hip_stream)));
+}
+
+kmq_status kmq_kv_read(const kmq_kv_cache* cache, const kmq_kv_batch* batch, uint16_t* k, int64_t k_stride,
+                       uint16_t* v, int64_t v_stride, void* hip_stream) {
+    if (!k || !v) return KMQ_ERR_NULL;
+    const kmq_status c = kmq::check_cached(cache, batch);
+    if (c != KMQ_OK) return c;
+    if (!kmq::row_of_heads(k, k_stride, cache->kv_heads, cache->head_dim) || !kmq::row_of_heads(v, v_stride, cache->kv_heads, cache->head_dim)) return KMQ_ERR_SHAPE;
+    if (!kmq::aligned(k, 16) || !kmq::aligned(v, 16)) return KMQ_ERR_ALIGN;
+    return kmq::hip_status(kmq::launch_kv_read(kmq::cache_args(cache), kmq::batch_args(batch), k, k_stride, v, v_stride, static_cast<hipStream_t>(hip_stream)));
+}
+
+kmq_status kmq_kv_append(const kmq_kv_cache* cache, const kmq_kv_batch* batch, const uint16_t* qkv, int64_t qkv_stride,
+                         int q_heads, const kmq_head_turn* turn, uint16_t* q_out, int64_t q_stride, void* hip_stream) {
+    if (!qkv || !q_out || !turn) return KMQ_ERR_NULL;
+    const kmq_status c = kmq::check_cached(cache, batch);
+    if (c != KMQ_OK) return c;
+    if (q_heads < 1 || q_heads > kmq::kMaxHeads) return KMQ_ERR_SHAPE;
+    const int D = cache->head_dim, kv = cache->kv_heads;
+    const kmq_status t = kmq::check_turn(turn, D, true);
+    if (t != KMQ_OK) return t;
+    if (!kmq::row_of_heads(qkv, qkv_stride, int64_t(q_heads) + 2 * kv, D) || !kmq::row_of_heads(q_out, q_stride, q_heads, D)) return KMQ_ERR_SHAPE;
+    if (!kmq::aligned(qkv, 16) || !kmq::aligned(q_out, 16)) return KMQ_ERR_ALIGN;
+    kmq::HeadsArgs a;
+    a.q = qkv;
+    a.k = qkv + static_cast<int64_t>(q_heads) * D;
+    a.v = a.k + static_cast<int64_t>(kv) * D;
+    a.q_stride = a.k_stride = a.v_stride = qkv_stride;
+    a.rows = batch->rows;
+    a.q_heads = q_heads;
+    a.k_heads = a.v_heads = kv;
+    a.head_dim = D;
+    kmq::set_turn(a, turn);
+    a.q_out = q_out;
+    a.q_out_stride = q_stride;
+    const kmq::KvCacheArgs ca = kmq::cache_args(cache);
+    const kmq::KvBatchArgs ba = kmq::batch_args(batch);
+    return kmq::hip_status(kmq::launch_heads(a, &ca, &ba, static_cast<hipStream_t>(hip_stream)));
+}
+
+// The shapes an attention can have: (rows, query heads) pairs and their partial results are counted in 64 bits, workgroups in 31.
+static kmq_status check_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch, int q_heads) {
+    if (q_heads < 1 || q_heads > kmq::kMaxHeads || q_heads % cache->kv_heads || batch->rows * q_heads > (int64_t(1) << 30)) return KMQ_ERR_SHAPE;
+    return KMQ_OK;
+}
+
+size_t kmq_kv_attention_workspace_bytes(const kmq_kv_cache* cache, const kmq_kv_batch* batch, int q_heads) {
+    if (kmq::check_cached(cache, batch) != KMQ_OK || check_attention(cache, batch, q_heads) != KMQ_OK) return 0;
+    return kmq::attention_plan(kmq::cache_args(cache), kmq::batch_args(batch), q_heads).workspace_bytes;
+}
+
+const char* kmq_kernel_name_kv_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch, int q_heads) {
+    if (kmq::check_cached(cache, batch) != KMQ_OK || check_attention(cache, batch, q_heads) != KMQ_OK) return "invalid";
+    return kmq::attention_plan(kmq::cache_args(cache), kmq::batch_args(batch), q_heads).name;
+}
+
+kmq_status kmq_kv_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch, const uint16_t* q, int64_t q_stride, int q_heads,
+                            float scale, int causal, int window, uint16_t* out, int64_t out_stride, float* lse,
+                            void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!q || !out) return KMQ_ERR_NULL;
+    const kmq_status c = kmq::check_cached(cache, batch);
+    if (c != KMQ_OK) return c;
+    const kmq_status h = check_attention(cache, batch, q_heads);
+    if (h != KMQ_OK) return h;
+    if (!(scale - scale == 0.f) || (causal != 0 && causal != 1) || window < 0) return KMQ_ERR_SHAPE;   // (an infinity or a NaN less itself is a NaN)
+    if (!kmq::row_of_heads(q, q_stride, q_heads, cache->head_dim) || !kmq::row_of_heads(out, out_stride, q_heads, cache->head_dim)) return KMQ_ERR_SHAPE;
+    if (!kmq::aligned(q, 16) || !kmq::aligned(out, 16) || !kmq::aligned(lse, 4)) return KMQ_ERR_ALIGN;
+    const kmq::AttentionArgs a{kmq::cache_args(cache), kmq::batch_args(batch), q, out, q_stride, out_stride, q_heads, scale, causal != 0, window, lse, workspace};
+    const size_t need = kmq::attention_plan(a.cache, a.batch, q_heads).workspace_bytes;
+    if (need > 0 && (!workspace || workspace_bytes < need)) return KMQ_ERR_WORKSPACE;
+    if (need > 0 && !kmq::aligned(workspace, 16)) return KMQ_ERR_ALIGN;
+    return kmq::hip_status(kmq::launch_attention(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 const char* kmq_last_hip_error(void) { return kmq::g_last_hip_error; }

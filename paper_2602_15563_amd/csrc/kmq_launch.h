@@ -108,6 +108,63 @@ bool lut_loop_has_kernel(int64_t N, int64_t K, int bits, int layout);
 const char* lut_loop_name(int bits);
 hipError_t launch_lut_loop(const GemmArgs& a, hipStream_t s);
 
+// ---- Between the QKV and the output product: heads, the 4-bit key / value cache, attention (kmq_kv.h) ----
+struct KvCacheArgs {
+    uint8_t* pages;
+    const uint16_t* codebooks;           // 16 centroids of K, then 16 of V
+    int64_t num_pages;
+    int page_size, kv_heads, head_dim;
+};
+
+struct KvBatchArgs {
+    const int32_t* page_table;           // sequences x table_width
+    const int32_t* lengths;
+    const int32_t* row_starts;           // sequences + 1; nullptr: a row a sequence
+    int64_t rows;
+    int sequences, table_width;
+};
+
+// Rows of heads on their way into the attention: queries and keys normalised and rotated, keys and values quantised.
+struct HeadsArgs {
+    const uint16_t *q = nullptr, *k = nullptr, *v = nullptr;      // first head of row 0
+    int64_t q_stride = 0, k_stride = 0, v_stride = 0;             // elements from row to row
+    int64_t rows = 0;
+    int q_heads = 0, k_heads = 0, v_heads = 0, head_dim = 0;
+    bool norm = false;
+    const uint16_t *q_gain = nullptr, *k_gain = nullptr;
+    float eps = 0.f;
+    int rotary_dim = 0;
+    bool interleaved = false;
+    const int32_t* positions = nullptr;  // nullptr: the position in the cache
+    const float* inv_freq = nullptr;
+    uint16_t *q_out = nullptr, *k_out = nullptr;                  // k_out nullptr: keys go into the cache
+    int64_t q_out_stride = 0, k_out_stride = 0;
+};
+hipError_t launch_heads(const HeadsArgs& a, const KvCacheArgs* cache, const KvBatchArgs* batch, hipStream_t s);
+hipError_t launch_kv_read(const KvCacheArgs& c, const KvBatchArgs& b, uint16_t* k, int64_t k_stride, uint16_t* v, int64_t v_stride, hipStream_t s);
+
+struct AttentionArgs {
+    KvCacheArgs cache;
+    KvBatchArgs batch;
+    const uint16_t* q;
+    uint16_t* out;
+    int64_t q_stride, out_stride;
+    int q_heads;
+    float scale;
+    bool causal;
+    int window;                          // 0: none
+    float* lse;                          // rows x q_heads, or nullptr
+    void* workspace;
+};
+struct AttentionPlan {
+    const char* name;
+    int columns;                         // (row, query head) pairs a workgroup takes
+    int splits;                          // parts of the tokens, joined by a second kernel
+    size_t workspace_bytes;
+};
+AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads);
+hipError_t launch_attention(const AttentionArgs& a, hipStream_t s);
+
 }  // namespace kmq
 
 #endif

@@ -88,6 +88,22 @@ _lib.kmq_quantize_blockscaled_workspace_bytes.restype = _sz
 _lib.kmq_quantize_blockscaled_workspace_bytes.argtypes = []
 _lib.kmq_quantize_blockscaled.restype = ctypes.c_int32
 _lib.kmq_quantize_blockscaled.argtypes = [_vp, _i64, _i64, _int, _int, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.kmq_kv_page_bytes.restype = _i64
+_lib.kmq_kv_page_bytes.argtypes = [_int, _int, _int]
+_lib.kmq_qk_norm_rope.restype = ctypes.c_int32
+_lib.kmq_qk_norm_rope.argtypes = [_vp, _i64, _i64, _int, _int, _int, _vp, _vp, _i64, _vp, _i64, _vp]
+_lib.kmq_kv_write.restype = ctypes.c_int32
+_lib.kmq_kv_write.argtypes = [_vp, _vp, _vp, _i64, _vp, _i64, _vp]
+_lib.kmq_kv_read.restype = ctypes.c_int32
+_lib.kmq_kv_read.argtypes = [_vp, _vp, _vp, _i64, _vp, _i64, _vp]
+_lib.kmq_kv_append.restype = ctypes.c_int32
+_lib.kmq_kv_append.argtypes = [_vp, _vp, _vp, _i64, _int, _vp, _vp, _i64, _vp]
+_lib.kmq_kv_attention_workspace_bytes.restype = _sz
+_lib.kmq_kv_attention_workspace_bytes.argtypes = [_vp, _vp, _int]
+_lib.kmq_kv_attention.restype = ctypes.c_int32
+_lib.kmq_kv_attention.argtypes = [_vp, _vp, _vp, _i64, _int, ctypes.c_float, _int, _int, _vp, _i64, _vp, _vp, _sz, _vp]
+_lib.kmq_kernel_name_kv_attention.restype = ctypes.c_char_p
+_lib.kmq_kernel_name_kv_attention.argtypes = [_vp, _vp, _int]
 _lib.kmq_last_hip_error.restype = ctypes.c_char_p
 _lib.kmq_last_hip_error.argtypes = []
 _lib.kmq_status_string.restype = ctypes.c_char_p
@@ -307,3 +323,110 @@ def dequant(W, codebook, Wdense, N: int, K: int, bits: int, layout: int = 0):
 def dequant_blockscaled(W, codebook, scales, Wdense, N: int, K: int, bits: int):
     """Wdense[N][K] (bf16 storage) = bf16(codebook[idx] * scale) of the block-scaled format, on torch's current stream."""
     _check(_lib.kmq_dequant_blockscaled(_ptr(W), _ptr(codebook), _ptr(scales), _ptr(Wdense), N, K, bits, _stream()))
+
+
+# ---- between the QKV product and the output product -------------------------------------------------------------------
+
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("pages", _vp), ("codebooks", _vp), ("num_pages", _i64), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class _BatchStruct(ctypes.Structure):
+    _fields_ = [("page_table", _vp), ("lengths", _vp), ("row_starts", _vp), ("rows", _i64), ("sequences", ctypes.c_int32),
+                ("table_width", ctypes.c_int32)]
+
+
+class _TurnStruct(ctypes.Structure):
+    _fields_ = [("positions", _vp), ("inv_freq", _vp), ("q_gain", _vp), ("k_gain", _vp), ("eps", ctypes.c_float), ("rmsnorm", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+def kv_page_bytes(page_size: int, kv_heads: int, head_dim: int) -> int:
+    return int(_lib.kmq_kv_page_bytes(page_size, kv_heads, head_dim))
+
+
+class KvCache:
+    """A paged 4-bit key / value cache: `pages` (device bytes, num_pages * kv_page_bytes) and `codebooks` (device, 2 x 16 bf16:
+    K's centroids, then V's).  Keeps both alive; made once, handed to every call on the cache."""
+
+    def __init__(self, pages, codebooks, num_pages: int, page_size: int, kv_heads: int, head_dim: int):
+        size = kv_page_bytes(page_size, kv_heads, head_dim)
+        if size < 0 or num_pages < 1 or codebooks.numel() * codebooks.element_size() != 64 or pages.numel() * pages.element_size() < num_pages * size:
+            raise KmqError(3)
+        if not (pages.is_contiguous() and codebooks.is_contiguous()):
+            raise KmqError(3)
+        self.pages, self.codebooks = pages, codebooks
+        self.num_pages, self.page_size, self.kv_heads, self.head_dim = num_pages, page_size, kv_heads, head_dim
+        self._struct = _CacheStruct(_ptr(pages), _ptr(codebooks), num_pages, page_size, kv_heads, head_dim)
+        self._at = ctypes.addressof(self._struct)
+
+
+class KvBatch:
+    """Which rows belong to which sequence (include/kmq.h): int32 device tensors page_table (sequences x width), lengths (sequences)
+    and row_starts (sequences + 1; None: one row a sequence).  Their contents may change from call to call."""
+
+    def __init__(self, page_table, lengths, row_starts=None, rows: int = None):
+        sequences, width = page_table.shape
+        for t in (page_table, lengths, row_starts):
+            if t is not None and (t.element_size() != 4 or t.is_floating_point() or not t.is_contiguous()):
+                raise KmqError(3)
+        if lengths.numel() != sequences or (row_starts is not None and row_starts.numel() != sequences + 1):
+            raise KmqError(3)
+        if rows is None:
+            if row_starts is not None:
+                raise KmqError(3)
+            rows = sequences
+        self.page_table, self.lengths, self.row_starts, self.rows = page_table, lengths, row_starts, rows
+        self._struct = _BatchStruct(_ptr(page_table), _ptr(lengths), _ptr(row_starts), rows, sequences, width)
+        self._at = ctypes.addressof(self._struct)
+
+
+def _turn(positions, inv_freq, rotary_dim, interleaved, rmsnorm, q_gain, k_gain, eps):
+    if rmsnorm is None:
+        rmsnorm = q_gain is not None or k_gain is not None
+    return _TurnStruct(_ptr(positions), _ptr(inv_freq), _ptr(q_gain), _ptr(k_gain), eps, 1 if rmsnorm else 0, rotary_dim, 1 if interleaved else 0)
+
+
+def qk_norm_rope(qk, qk_stride: int, q_out, q_stride: int, k_out, k_stride: int, rows: int, q_heads: int, k_heads: int, head_dim: int,
+                 positions=None, inv_freq=None, rotary_dim: int = 0, interleaved: bool = False, rmsnorm=None, q_gain=None, k_gain=None,
+                 eps: float = 0.0):
+    """Query and key heads normalised (RMSNorm over each head) and rotated by position, in one launch on torch's current stream.
+    rmsnorm defaults to "gains were given"; True without gains normalises with unit gains."""
+    turn = _turn(positions, inv_freq, rotary_dim, interleaved, rmsnorm, q_gain, k_gain, eps)
+    _check(_lib.kmq_qk_norm_rope(_ptr(qk), qk_stride, rows, q_heads, k_heads, head_dim, ctypes.addressof(turn), _ptr(q_out), q_stride,
+                                 _ptr(k_out), k_stride, _stream()))
+
+
+def kv_write(cache: KvCache, batch: KvBatch, k, k_stride: int, v, v_stride: int):
+    """K and V rows quantised into their places in the cache, on torch's current stream."""
+    _check(_lib.kmq_kv_write(cache._at, batch._at, _ptr(k), k_stride, _ptr(v), v_stride, _stream()))
+
+
+def kv_read(cache: KvCache, batch: KvBatch, k, k_stride: int, v, v_stride: int):
+    """The rows' places in the cache as bf16, on torch's current stream."""
+    _check(_lib.kmq_kv_read(cache._at, batch._at, _ptr(k), k_stride, _ptr(v), v_stride, _stream()))
+
+
+def kv_append(cache: KvCache, batch: KvBatch, qkv, qkv_stride: int, q_out, q_stride: int, q_heads: int, positions=None, inv_freq=None,
+              rotary_dim: int = 0, interleaved: bool = False, rmsnorm=None, q_gain=None, k_gain=None, eps: float = 0.0):
+    """Rows of the fused QKV product on their way into the attention, in one launch: queries turned into q_out, keys turned and quantised
+    into the cache, values quantised.  positions=None: the rows' positions in the cache."""
+    turn = _turn(positions, inv_freq, rotary_dim, interleaved, rmsnorm, q_gain, k_gain, eps)
+    _check(_lib.kmq_kv_append(cache._at, batch._at, _ptr(qkv), qkv_stride, q_heads, ctypes.addressof(turn), _ptr(q_out), q_stride, _stream()))
+
+
+def kv_attention_workspace_bytes(cache: KvCache, batch: KvBatch, q_heads: int) -> int:
+    return int(_lib.kmq_kv_attention_workspace_bytes(cache._at, batch._at, q_heads))
+
+
+def kernel_name_kv_attention(cache: KvCache, batch: KvBatch, q_heads: int) -> str:
+    return _lib.kmq_kernel_name_kv_attention(cache._at, batch._at, q_heads).decode()
+
+
+def kv_attention(cache: KvCache, batch: KvBatch, q, q_stride: int, out, out_stride: int, q_heads: int, scale: float, causal: bool = True,
+                 window: int = 0, lse=None, workspace=None):
+    """Attention of the batch's rows over the cache, on torch's current stream.  workspace: kv_attention_workspace_bytes() device bytes."""
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_lib.kmq_kv_attention(cache._at, batch._at, _ptr(q), q_stride, q_heads, scale, 1 if causal else 0, window, _ptr(out), out_stride,
+                                 _ptr(lse), _ptr(workspace), ws_bytes, _stream()))

@@ -44,3 +44,21 @@ def swiglu_contract_bound(U, Ag, Au, silu_G, want):
 def rmsnorm_commute_bound(A_product):
     """A_product: sum_k |w xn| of the product alone (without a residual)."""
     return 2.0 ** -7 * A_product
+
+
+def attention_lse_bound(size, tokens, head_dim):
+    """Log-sum-exp of attention over `tokens` tokens in fp32.  size: the largest |scale| sum_d |q_d k_d| among them.  A score is a sum
+    of head_dim products that are exact in fp32, then multiplied by a block's scale and by scale * log2(e) and brought to base 2 less
+    the maximum: (head_dim + 24) roundings of at most 2^-23 * size.  The exponential is good to 2^-21 of itself, and a sum of
+    `tokens` positive terms to tokens * 2^-23; the last logarithm, and adding the maximum, are a few roundings more (2^-20 of 1 + size)."""
+    return (head_dim + 24) * 2.0 ** -23 * size + 2.0 ** -21 + tokens * 2.0 ** -23 + 2.0 ** -20 * (1 + size)
+
+
+def attention_bound(out, spread, size, tokens, head_dim):
+    """Attention output in bf16.  out: the fp64 result; spread: sum p |v| / sum p.  Every p is off by d, the score's error and the
+    exponential's (attention_lse_bound bounds both), in the numerator and in the sum that divides it; p times V's scale, or V times its
+    scale, or both are rounded to bf16 once (2^-8 each) before the second product, whose fp32 sum of `tokens` terms adds
+    tokens * 2^-23; the result is rounded once more."""
+    d = attention_lse_bound(size, tokens, head_dim)[..., None]
+    inner = (2 * d * (1 + d) + 2 * 2.0 ** -8 + (tokens + 8) * 2.0 ** -23) * spread
+    return inner + 2.0 ** -8 * (np.abs(out) + inner)

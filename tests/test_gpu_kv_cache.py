@@ -1,0 +1,180 @@
+"""The 4-bit cache on the GPU: writing it (kmq_kv_write, kmq_kv_append) leaves the oracle's bytes, reading it (kmq_kv_read) gives the
+oracle's values, both bit for bit; what no row belongs to stays as it was."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv as okv
+from paper_2602_15563_amd import kmq
+from tests.kv_util import NAN16, Case, dev, host, patterns
+
+pytestmark = pytest.mark.gpu
+
+CASES = [  # news, lengths, page_size, kv_heads, D, more
+    ([1], [1], 32, 1, 64, {}),
+    ([1, 1, 1], [32, 33, 700], 32, 3, 128, dict(starts=False)),
+    ([1, 0, 5, 40], [17, 9, 5, 71], 32, 2, 64, dict(behind=3)),
+    ([33, 64], [33, 100], 96, 2, 128, {}),
+    ([7, 20], [40, 21], 64, 1, 256, dict(behind=1)),
+    ([5, 9], [3, 0], 32, 1, 64, {}),                             # more rows than tokens: the first stand before the sequence
+    ([40], [75], 32, 2, 64, dict(width=2)),                      # a table too short for its length
+    ([1, 2, 0] * 50, [64, 65, 3] * 50, 64, 1, 64, {}),           # more sequences than a wave has lanes
+]
+
+
+def fill(c, seed):
+    g = np.random.default_rng(seed)
+    k = g.standard_normal((c.rows, c.kv_heads, c.D)) * 2.0 ** g.integers(-8, 9, (c.rows, c.kv_heads, 1))
+    return patterns(k), patterns(g.standard_normal(k.shape))
+
+
+def write_and_read(c, k, v, pad=0):
+    row = c.kv_heads * c.D
+    kd, vd = (torch.full((c.rows, row + pad), NAN16, dtype=torch.int16, device="cuda") for _ in range(2))
+    kd[:, :row], vd[:, :row] = dev(k.reshape(c.rows, row)), dev(v.reshape(c.rows, row))
+    kmq.kv_write(c.cache, c.batch, kd, row + pad, vd, row + pad)
+    out = [torch.full((c.rows, row + pad), NAN16, dtype=torch.int16, device="cuda") for _ in range(2)]
+    kmq.kv_read(c.cache, c.batch, out[0], row + pad, out[1], row + pad)
+    torch.cuda.synchronize()
+    got = [host(o) for o in out]
+    for o in got:
+        assert (o[:, row:] == NAN16).all()
+    return [o[:, :row].reshape(c.rows, c.kv_heads, c.D) for o in got]
+
+
+def check(c, k, v, pad=0):
+    got = write_and_read(c.to_device(), k, v, pad)
+    want = [np.zeros_like(k), np.zeros_like(v)]
+    for row, page, token in c.places():
+        c.pages.write(page, token, k[row], v[row], c.books)
+    for row, page, token in c.places():
+        for w, x in zip(want, c.pages.read(page, token, c.books)):
+            w[row] = okv.round_bf16(x)
+    c.check_pages()
+    for g, w in zip(got, want):
+        w[c.starts[-1]:] = NAN16
+        assert np.array_equal(okv.bf16_value(g), okv.bf16_value(w), equal_nan=True)
+
+
+@pytest.mark.parametrize("i", range(len(CASES)))
+@pytest.mark.parametrize("pad", (0, 8))
+def test_write_and_read(i, pad):
+    news, lengths, page, heads, D, more = CASES[i]
+    print(f"write and read case {i} {CASES[i] if len(news) < 10 else (page, heads, D)} pad {pad}", flush=True)
+    c = Case(i, news, lengths, page, heads, D, **more)
+    check(c, *fill(c, 50 + i), pad)
+
+
+def test_pages_that_are_none():
+    c = Case(20, [70], [70], 32, 2, 64)
+    c.table[0, 0], c.table[0, 2] = c.num_pages, -7
+    check(c, *fill(c, 70))
+
+
+def test_values_next_to_boundaries():
+    """Every bf16 value next to every boundary of every block: the comparison is exact."""
+    c = Case(21, [64], [64], 32, 2, 128)
+    g = np.random.default_rng(71)
+    c.books[0] = patterns(np.sort(np.concatenate([-(2.0 ** -np.arange(8)), 2.0 ** -np.arange(8) * 0.75])))
+    c.books[1] = patterns(np.sort(g.uniform(-1, 1, 16)))
+    k, v = fill(c, 72)
+    for x, book in ((k, c.books[0]), (v, c.books[1])):
+        blocks = x.reshape(-1, 64)
+        scale = patterns(2.0 ** g.integers(-100, 100, len(blocks)) * g.uniform(1, 2, len(blocks)))
+        scale[:4] = [0x0001, 0x0080, 0x7F7F, 0x0007]                                        # denormal, smallest normal, largest
+        edge = patterns(np.outer(okv.bf16_value(scale), okv.boundaries(book)))
+        for j, step in enumerate((-1, 0, 1)):
+            blocks[:, 1 + 15 * j:16 + 15 * j] = edge + step * (edge & 0x7FFF != 0)
+        blocks[:, 0] = scale
+        over = (blocks & 0x7FFF) > scale[:, None]
+        blocks[over] = 0
+    check(c, k, v)
+
+
+def test_codebooks_with_equal_centroids_and_far_ones():
+    c = Case(22, [40], [40], 32, 1, 64)
+    c.books[0] = patterns([-1.0] * 5 + [0.0] * 6 + [1e-30, 1e-20, 0.5, 1.0, 1.0])
+    c.books[1] = patterns([0.25] * 16)
+    check(c, *fill(c, 73))
+
+
+def test_zeros_and_non_finite_values():
+    c = Case(23, [6], [6], 32, 1, 128)
+    k, v = fill(c, 74)
+    k[0], v[0] = 0, 0x8000
+    k[1, 0, 3], k[1, 0, 70] = 0x7F80, 0xFFC1
+    v[2, 0, 127] = 0xFF80
+    keep = [(r, kv, b) for r in range(6) for kv in range(2) for b in range(2) if (r, kv, b) not in ((1, 0, 0), (1, 0, 1), (2, 1, 1))]
+    got = write_and_read(c.to_device(), k, v)
+    for r, page, token in c.places():
+        c.pages.write(page, token, k[r], v[r], c.books)
+    for r, page, token in c.places():
+        want = [okv.round_bf16(x) for x in c.pages.read(page, token, c.books)]
+        for kv in range(2):
+            for b in range(2):
+                g, w = okv.bf16_value(got[kv][r, 0, 64 * b:64 * b + 64]), okv.bf16_value(want[kv][0, 64 * b:64 * b + 64])
+                if (r, kv, b) in keep:
+                    assert np.array_equal(g, w)
+                else:
+                    assert not np.isfinite(g).any()                                          # the block's values are lost, and only its
+
+
+@pytest.mark.parametrize("i", (1, 2, 3, 4, 7))
+@pytest.mark.parametrize("rot,interleaved,norm", [(0, False, False), (64, False, True), (32, True, True)])
+@pytest.mark.parametrize("given", (False, True))
+def test_append(i, rot, interleaved, norm, given):
+    """One launch: the queries of kmq_qk_norm_rope, and the cache that kmq_kv_write leaves of its keys."""
+    news, lengths, page, heads, D, more = CASES[i]
+    print(f"append case {i} rot {rot} interleaved {interleaved} norm {norm} positions {given}", flush=True)
+    c = Case(100 + i, news, lengths, page, heads, D, **more)
+    g = np.random.default_rng(200 + i)
+    nq = 3 * heads
+    x = patterns(g.standard_normal((c.rows, nq + 2 * heads, D)))
+    gq, gk = patterns(1 + 0.3 * g.standard_normal(D)), patterns(1 + 0.3 * g.standard_normal(D))
+    freq = (10000.0 ** (-np.arange(0, rot, 2) / max(rot, 1))).astype(np.float32)
+    at = np.array([c.position(r)[1] for r in range(c.rows)])
+    pos = g.integers(0, 100000, c.rows).astype(np.int32) if given else at.astype(np.int32)
+    stride = (nq + 2 * heads) * D + 16
+    xd = torch.full((c.rows, stride), NAN16, dtype=torch.int16, device="cuda")
+    xd[:, :stride - 16] = dev(x.reshape(c.rows, -1))
+    q = torch.full((c.rows, nq * D + 8), NAN16, dtype=torch.int16, device="cuda")
+    c.to_device()
+    kmq.kv_append(c.cache, c.batch, xd, stride, q, nq * D + 8, nq, positions=dev(pos) if given else None, inv_freq=dev(freq) if rot else None,
+                  rotary_dim=rot, interleaved=interleaved, rmsnorm=norm, q_gain=dev(gq), k_gain=dev(gk), eps=1e-6)
+    torch.cuda.synchronize()
+    turned = [okv.round_bf16(okv.turn(x[:, a:b], pos, freq, rot, interleaved, norm, gain, 1e-6)) for a, b, gain in ((0, nq, gq), (nq, nq + heads, gk))]
+    for r, page_, token in c.places():
+        c.pages.write(page_, token, turned[1][r], x[r, nq + heads:], c.books)
+    c.check_pages()
+    got = host(q)
+    assert (got[:, nq * D:] == NAN16).all() and (got[c.starts[-1]:] == NAN16).all()
+    end = c.starts[-1]
+    assert np.array_equal(got[:end, :nq * D].reshape(end, nq, D), turned[0][:end])
+    # the same through the two calls
+    d = Case(100 + i, news, lengths, page, heads, D, **more).to_device()
+    q2, k2 = torch.empty((c.rows, nq * D), dtype=torch.int16, device="cuda"), torch.empty((c.rows, heads * D), dtype=torch.int16, device="cuda")
+    kmq.qk_norm_rope(xd, stride, q2, nq * D, k2, heads * D, c.rows, nq, heads, D, positions=dev(pos), inv_freq=dev(freq), rotary_dim=rot,
+                     interleaved=interleaved, rmsnorm=norm, q_gain=dev(gq), k_gain=dev(gk), eps=1e-6)
+    kmq.kv_write(d.cache, d.batch, k2, heads * D, xd[:, (nq + heads) * D:], stride)
+    torch.cuda.synchronize()
+    assert np.array_equal(host(q2)[:end], got[:end, :nq * D]) and torch.equal(d.pages_d, c.pages_d)
+
+
+def test_codebooks_from_the_quantiser():
+    """kmq_quantize_blockscaled on a sample gives a codebook, and kmq_kv_write the sample's indices and scales under it."""
+    g = np.random.default_rng(30)
+    c = Case(30, [64], [64], 64, 1, 128)
+    k, v = patterns(g.standard_normal((64, 1, 128))), patterns(g.standard_normal((64, 1, 128)) ** 3)
+    ws = torch.empty(kmq.quantize_blockscaled_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    kept = []
+    for kv, x in enumerate((k, v)):
+        packed = torch.empty((64, 16), dtype=torch.int32, device="cuda")
+        book, scales = torch.empty(16, dtype=torch.int16, device="cuda"), torch.empty((64, 2), dtype=torch.int16, device="cuda")
+        kmq.quantize_blockscaled(dev(x.reshape(64, 128)), 64, 128, 4, 20, packed, book, scales, ws)
+        torch.cuda.synchronize()
+        c.books[kv] = host(book)
+        kept.append((kmq.unpack(packed.cpu().numpy().view(np.uint32), 128, 4), host(scales)))
+    for (idx, scale), x, book in zip(kept, (k, v), c.books):
+        i2, s2 = okv.quantize(x[:, 0], book)
+        assert np.array_equal(i2, idx) and np.array_equal(s2, scale)
+    check(c, k, v)
