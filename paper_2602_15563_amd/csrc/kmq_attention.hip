@@ -17,6 +17,7 @@ constexpr int kAttnWaves = 4, kAttnThreads = kAttnWaves * kWave;
 constexpr int kAttnColumns = 16;              // columns of a workgroup: one matrix-core tile
 constexpr int kAttnMinSteps = 2 * kAttnWaves; // steps of a part at least: fewer are not worth the joining
 constexpr float kLowest = -3.402823466e38f;   // start of a running maximum: finite, so that differences from it are no NaN
+constexpr float kSlack = 8.f;                 // scores (base 2) may pass the running maximum by this before everything is rescaled
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // 16 centroids as two byte planes (low bytes, high bytes), four entries a register.
@@ -48,6 +49,45 @@ __device__ __forceinline__ u32x4_t decode8(const Centroids& c, uint32_t w) {
     decode4(c, w >> 4 & 0x07070707u, (w >> 5 & 0x04040404u) | 0x03020100u, r[2], r[3]);
     return u32x4_t{r[0], r[1], r[2], r[3]};
 }
+
+// The same from a table of all pairs in shared memory: a byte's two indices are a register's two bf16, in their order.
+__device__ __forceinline__ u32x4_t decode8_table(const uint32_t* table, uint32_t w) {
+    return u32x4_t{table[w & 0xFFu], table[w >> 8 & 0xFFu], table[w >> 16 & 0xFFu], table[w >> 24]};
+}
+// Eight bf16 in the order in which decode8 leaves a dword's indices: even ones, then odd ones.
+__device__ __forceinline__ u32x4_t even_odd(u32x4_t v) {
+    return u32x4_t{__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u),
+                   __builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u)};
+}
+__device__ __forceinline__ float half_of(uint32_t v, int upper) { return __uint_as_float(upper ? v & 0xFFFF0000u : v << 16); }
+
+// N dwords (N * 4 a power of two, or a multiple of 16 bytes) from an address aligned to their size, at most 16 bytes a load.
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t* to, const uint8_t* from) {
+    if constexpr (N >= 4) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *reinterpret_cast<u32x4_t*>(to + i) = *reinterpret_cast<const u32x4_t*>(from + 4 * i);
+    } else {
+        static_assert(N == 2, "two or a multiple of four");
+        *reinterpret_cast<u32x2_t*>(to) = *reinterpret_cast<const u32x2_t*>(from);
+    }
+}
+// A step's indices of K and all its scales: of a lane's token in every tile, and of the four tokens of its quarter.
+template <int D>
+struct KWords {
+    uint32_t k[2][D / 32], sc[2][D / 16];
+    __device__ __forceinline__ void load(const uint8_t* base, int lane, int quarter) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            load_words<D / 32>(k[t], base + t * 17 * D + lane * (D / 8));
+            load_words<D / 16>(sc[t], base + t * 17 * D + 16 * D + quarter * (D / 4));
+        }
+    }
+};
+struct Place {
+    const uint8_t* base;   // of a step's two tiles
+    bool there;
+};
 
 __device__ __forceinline__ f32x4_t mfma(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
@@ -114,6 +154,11 @@ struct AttnArgs {
     float* part_ml;        // splits x rows x heads x 2
 };
 
+#ifdef KMQ_ATTN_PERM
+constexpr bool LUT_K = false;
+#else
+constexpr bool LUT_K = true;
+#endif
 template <int D>
 __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
     constexpr int NB = D / KMQ_BLOCK, DT = D / 16;
@@ -122,9 +167,10 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
     const KvBatchArgs& b = a.batch;
     constexpr int DC = D < 128 ? D : 128;            // elements joined at a time
     __shared__ float part[kAttnWaves][kAttnColumns][DC + 4];
+    __shared__ uint32_t table[256];
     __shared__ float stat[2][kAttnWaves][kAttnColumns];
 
-    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), wave = static_cast<int>(threadIdx.x) / kWave;
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
     const int col = lane & 15, quarter = lane >> 4;
     const int head = static_cast<int>(blockIdx.x) % a.cache.kv_heads;
     const int group = a.q_heads / a.cache.kv_heads;
@@ -155,8 +201,8 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
     const int steps = step1 > step0 ? step1 - step0 : 0;
     int per = (steps + A.splits - 1) / A.splits;
     per = per > kAttnMinSteps ? per : kAttnMinSteps;
-    const int64_t from = step0 + static_cast<int64_t>(blockIdx.y) * per;
-    const int64_t to = from + per < step1 ? from + per : step1;
+    const int64_t from64 = step0 + static_cast<int64_t>(blockIdx.y) * per;
+    const int from = static_cast<int>(from64 < step1 ? from64 : step1), to = step1 - from < per ? step1 : from + per;
 
     if (A.splits > 1 && from >= to) {                              // a part without tokens
         if (wave == 0 && quarter == 0 && live) {
@@ -168,18 +214,23 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
     }
 
     // queries as the first product's second operand: lane (column, quarter) holds elements 64 b + 16 quarter + 8 j + e, in the
-    // order in which decode8 leaves a dword's indices (even ones, then odd ones)
+    // order in which a dword's indices are decoded
     u32x4_t q[2 * NB];
 #pragma unroll
     for (int s = 0; s < 2 * NB; ++s) {
         u32x4_t v = {0, 0, 0, 0};
         if (live) v = *reinterpret_cast<const u32x4_t*>(a.q + row * a.q_stride + static_cast<int64_t>(qh) * D + s / 2 * 64 + quarter * 16 + s % 2 * 8);
-        q[s][0] = __builtin_amdgcn_perm(v[1], v[0], 0x05040100u);
-        q[s][1] = __builtin_amdgcn_perm(v[3], v[2], 0x05040100u);
-        q[s][2] = __builtin_amdgcn_perm(v[1], v[0], 0x07060302u);
-        q[s][3] = __builtin_amdgcn_perm(v[3], v[2], 0x07060302u);
+        q[s] = LUT_K ? v : even_odd(v);
     }
-    const Centroids ck = load_centroids(a.cache.codebooks), cv = load_centroids(a.cache.codebooks + kKvCentroids);
+    Centroids ck;
+    if (LUT_K) {
+        const uint32_t at = threadIdx.x;
+        table[at] = a.cache.codebooks[at & 15] | static_cast<uint32_t>(a.cache.codebooks[at >> 4]) << 16;
+        __syncthreads();
+    } else {
+        ck = load_centroids(a.cache.codebooks);
+    }
+    const Centroids cv = load_centroids(a.cache.codebooks + kKvCentroids);
     const float scale = a.scale * kLog2e;
 
     f32x4_t o[DT];
@@ -187,47 +238,78 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
     for (int d = 0; d < DT; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = kLowest, l = 0.f;
 
+    // steps that every live column sees whole need no mask
+    const int64_t last_begin = a.window && p_hi - a.window + 1 > 0 ? p_hi - a.window + 1 : 0;
+    const int64_t first_end = a.causal && p_lo + 1 < inside ? (p_lo + 1 > 0 ? p_lo + 1 : 0) : inside;
+    const int whole_from = static_cast<int>((last_begin + kKvStep - 1) / kKvStep), whole_to = static_cast<int>(first_end / kKvStep);
+    const int see_from = static_cast<int>(see_begin), see_to = static_cast<int>(see_end);
+
+    const int32_t* const table_row = b.page_table + static_cast<int64_t>(tile.seq) * b.table_width;
+    const int64_t page_stride = static_cast<int64_t>(a.cache.kv_heads) * (a.cache.page_size / kKvTile) * kTile;
+    const uint8_t* const head_base = a.cache.pages + static_cast<int64_t>(head) * (a.cache.page_size / kKvTile) * kTile;
     const int steps_per_page = a.cache.page_size / kKvStep;
-    for (int64_t step = from + wave; step < to; step += kAttnWaves) {
-        const int64_t slot = step / steps_per_page;
-        const int64_t page = b.page_table[static_cast<int64_t>(tile.seq) * b.table_width + slot];
+    int step = from + wave;
+    int slot = step / steps_per_page, within = step - slot * steps_per_page;      // of the step whose page is looked up next
+    const auto look_up = [&](int s) {                     // page of step s, whose place is (slot, within); then on to the wave's next step
+        const int page = s < to ? table_row[slot] : 0;
         const bool there = page >= 0 && page < a.cache.num_pages;
-        const uint8_t* base = a.cache.pages + ((there ? page : 0) * a.cache.kv_heads + head) * (a.cache.page_size / kKvTile) * kTile +
-                              (step - slot * steps_per_page) * 2 * kTile;
+        const uint8_t* base = head_base + (there ? page : 0) * page_stride + within * (2 * kTile);
+        within += kAttnWaves;
+        while (within >= steps_per_page) {
+            within -= steps_per_page;
+            ++slot;
+        }
+        return Place{base, there};
+    };
+    Place at = look_up(step), next = look_up(step + kAttnWaves);
+    KWords<D> kw;
+    if (step < to) kw.load(at.base, lane, quarter);
+    for (; step < to; step += kAttnWaves) {
+        uint32_t vw[2][D / 32];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) load_words<D / 32>(vw[t], at.base + t * kTile + 8 * D + lane * (D / 8));
+        const KWords<D> now = kw;
+        if (step + kAttnWaves < to) kw.load(next.base, lane, quarter);
+        const Place after = look_up(step + 2 * kAttnWaves);
+
         float s[8];
-        uint32_t p[NB][4];
-        float sv[2][NB][4];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const uint32_t* kw = reinterpret_cast<const uint32_t*>(base + t * kTile + lane * (D / 8));
-            const u32x2_t* sc = reinterpret_cast<const u32x2_t*>(base + t * kTile + 16 * D + quarter * (D / 4));
             f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-                acc = mfma(decode8(ck, kw[2 * n]), q[2 * n], acc);
-                acc = mfma(decode8(ck, kw[2 * n + 1]), q[2 * n + 1], acc);
-                const u32x2_t sk = sc[n], svp = sc[NB + n];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sum[e] = fmaf(acc[e], bf16_to_f32(sk[e / 2] >> (e % 2 * 16) & 0xFFFFu), sum[e]);
-                    sv[t][n][e] = bf16_to_f32(svp[e / 2] >> (e % 2 * 16) & 0xFFFFu);
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t w = now.k[t][2 * n + j];
+                    acc = mfma(LUT_K ? decode8_table(table, w) : decode8(ck, w), q[2 * n + j], acc);
                 }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] = fmaf(acc[e], half_of(now.sc[t][n * 2 + e / 2], e % 2), sum[e]);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t j = step * kKvStep + t * kKvTile + quarter * 4 + e;
-                const bool seen = there && j >= see_begin && j < see_end;
-                s[4 * t + e] = seen ? sum[e] * scale : -INFINITY;
+            for (int e = 0; e < 4; ++e) s[4 * t + e] = sum[e] * scale;
+        }
+        float sv[NB][8];
 #pragma unroll
-                for (int n = 0; n < NB; ++n) sv[t][n][e] = seen ? sv[t][n][e] : 0.f;   // (what lies behind a sequence may be anything)
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sv[n][e] = half_of(now.sc[e / 4][(NB + n) * 2 + e % 4 / 2], e % 2);
+        if (step < whole_from || step >= whole_to || !at.there) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
+                const bool seen = at.there && j >= see_from && j < see_to;
+                s[e] = seen ? s[e] : -INFINITY;
+#pragma unroll
+                for (int n = 0; n < NB; ++n) sv[n][e] = seen ? sv[n][e] : 0.f;       // (what lies behind a sequence may be anything)
             }
         }
         float top = s[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
-        top = max_over_quarters(top);
-        if (top > m) {
+        if (__ballot(top > m + kSlack)) {
+            top = fmaxf(m, max_over_quarters(top));
             const float shrink = __builtin_amdgcn_exp2f(m - top);
             m = top;
             l *= shrink;
@@ -242,18 +324,19 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
             l += s[e];
         }
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int n = 0; n < NB; ++n) {
+            u32x4_t p;
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) p[n][e / 2] = pack_bf16(s[e] * sv[e / 4][n][e % 4], s[e + 1] * sv[e / 4][n][e % 4 + 1]);
-        const uint32_t* v0 = reinterpret_cast<const uint32_t*>(base + 8 * D + lane * (D / 8));
-        const uint32_t* v1 = reinterpret_cast<const uint32_t*>(base + kTile + 8 * D + lane * (D / 8));
+            for (int e = 0; e < 8; e += 2) p[e / 2] = pack_bf16(s[e] * sv[n][e], s[e + 1] * sv[n][e + 1]);
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
-            const u32x4_t x = decode8(cv, v0[j]), y = decode8(cv, v1[j]);
-            const u32x4_t pj = {p[j / 2][0], p[j / 2][1], p[j / 2][2], p[j / 2][3]};
-            o[2 * j] = mfma(u32x4_t{x[0], x[1], y[0], y[1]}, pj, o[2 * j]);
-            o[2 * j + 1] = mfma(u32x4_t{x[2], x[3], y[2], y[3]}, pj, o[2 * j + 1]);
+            for (int j = 2 * n; j < 2 * n + 2; ++j) {
+                const u32x4_t x = decode8(cv, vw[0][j]), y = decode8(cv, vw[1][j]);
+                o[2 * j] = mfma(u32x4_t{x[0], x[1], y[0], y[1]}, p, o[2 * j]);
+                o[2 * j + 1] = mfma(u32x4_t{x[2], x[3], y[2], y[3]}, p, o[2 * j + 1]);
+            }
         }
+        at = next;
+        next = after;
     }
 
     // the waves' results joined: every wave's on the scale of the largest maximum
