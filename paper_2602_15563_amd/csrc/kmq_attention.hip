@@ -84,11 +84,6 @@ struct KWords {
         }
     }
 };
-struct Place {
-    const uint8_t* base;   // of a step's two tiles
-    bool there;
-};
-
 __device__ __forceinline__ f32x4_t mfma(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
@@ -154,13 +149,115 @@ struct AttnArgs {
     float* part_ml;        // splits x rows x heads x 2
 };
 
-#ifdef KMQ_ATTN_PERM
-constexpr bool LUT_K = false;
-#else
-constexpr bool LUT_K = true;
-#endif
+// The positions that a row sees: causal up to its own, a window back from it.
+struct Sight {
+    int64_t first_pos;     // of the sequence's first row: may be negative
+    int64_t inside;        // tokens that the cache can hold
+    int window;
+    bool causal;
+    __device__ __forceinline__ int64_t begin(int64_t row) const {
+        const int64_t v = first_pos + row - window + 1;
+        return window && v > 0 ? v : 0;
+    }
+    __device__ __forceinline__ int64_t end(int64_t row) const {
+        const int64_t v = first_pos + row + 1;
+        return causal && v < inside ? (v > 0 ? v : 0) : inside;
+    }
+};
+__device__ __forceinline__ Sight sight_of(const AttentionArgs& a, int seq) {
+    const KvBatchArgs& b = a.batch;
+    const int64_t length = b.lengths[seq], capacity = static_cast<int64_t>(b.table_width) * a.cache.page_size;
+    const int64_t rows = b.row_starts ? static_cast<int64_t>(b.row_starts[seq + 1]) - b.row_starts[seq] : 1;
+    return {length - rows, length < 0 ? 0 : length < capacity ? length : capacity, a.window, a.causal};
+}
+// Steps of 32 tokens: those that any of the rows lo..hi sees, and those that every one of them sees whole (they need no mask).
+struct Steps {
+    int from, to, whole_from, whole_to;
+};
+__device__ __forceinline__ Steps steps_of(const Sight& g, int64_t lo, int64_t hi) {
+    Steps s;
+    s.from = static_cast<int>(g.begin(lo) / kKvStep);
+    s.to = static_cast<int>((g.end(hi) + kKvStep - 1) / kKvStep);
+    s.to = s.to > s.from ? s.to : s.from;
+    s.whole_from = static_cast<int>((g.begin(hi) + kKvStep - 1) / kKvStep);
+    s.whole_to = static_cast<int>(g.end(lo) / kKvStep);
+    return s;
+}
+// This workgroup's part of them.
+__device__ __forceinline__ void take_part(Steps& s, int splits, int part) {
+    int per = (s.to - s.from + splits - 1) / splits;
+    per = per > kAttnMinSteps ? per : kAttnMinSteps;
+    const int64_t from = s.from + static_cast<int64_t>(part) * per;
+    s.from = static_cast<int>(from < s.to ? from : s.to);
+    s.to = s.to - s.from < per ? s.to : s.from + per;
+}
+
+// Walks the page table along steps that are `stride` apart.
+struct Place {
+    const uint8_t* base;   // of a step's two tiles
+    bool there;
+};
 template <int D>
-__global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
+struct Walk {
+    const int32_t* table;
+    const uint8_t* head_base;
+    int64_t page_stride;
+    int64_t num_pages;
+    int slot, within, steps_per_page;
+    __device__ __forceinline__ Walk(const AttentionArgs& a, int seq, int head, int step) {
+        const int tiles = a.cache.page_size / kKvTile;
+        table = a.batch.page_table + static_cast<int64_t>(seq) * a.batch.table_width;
+        page_stride = static_cast<int64_t>(a.cache.kv_heads) * tiles * (17 * D);
+        head_base = a.cache.pages + static_cast<int64_t>(head) * tiles * (17 * D);
+        num_pages = a.cache.num_pages;
+        steps_per_page = tiles / 2;
+        slot = step / steps_per_page;
+        within = step - slot * steps_per_page;
+    }
+    // the place of the step that the walk stands at, which lies on the table only where `inside`; then on by `stride`
+    __device__ __forceinline__ Place next(bool inside, int stride) {
+        const int page = inside ? table[slot] : 0;
+        const bool there = page >= 0 && page < num_pages;
+        const uint8_t* base = head_base + (there ? page : 0) * page_stride + static_cast<int64_t>(within) * (2 * 17 * D);
+        within += stride;
+        while (within >= steps_per_page) {
+            within -= steps_per_page;
+            ++slot;
+        }
+        return {base, there};
+    }
+};
+
+// Scores of a column (base 2, this lane's four tokens of each of a step's tiles) on their way to the second product: the running
+// maximum m and sum l, and what is accumulated already, brought to a new maximum where a score passes the old one by kSlack.
+template <int DT>
+__device__ __forceinline__ void soften(float (&s)[8], float& m, float& l, f32x4_t (&o)[DT]) {
+    float top = s[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
+    if (__ballot(top > m + kSlack)) {
+        top = fmaxf(m, max_over_quarters(top));
+        const float shrink = __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= shrink;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[d][e] *= shrink;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        s[e] = __builtin_amdgcn_exp2f(s[e] - m);
+        l += s[e];
+    }
+}
+
+// Few columns a sequence (single tokens, drafts): a workgroup takes 16 columns, and its waves take the steps in turn.  A wave reads
+// and decodes for itself, K by a table of index pairs in shared memory, V by byte permutes from registers: either way alone
+// keeps its unit busier than the memory (16 contexts of 32768 tokens: 134 us so, 151 by permutes alone, before the
+// accumulators were kept out of the second register file, which took it to 113).
+template <int D>
+__global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     constexpr int NB = D / KMQ_BLOCK, DT = D / 16;
     constexpr int kTile = 17 * D;
     const AttentionArgs& a = A.a;
@@ -178,33 +275,18 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
     if (tile.seq < 0) return;
 
     // this lane's column, and the tokens it may see
-    const int64_t column = static_cast<int64_t>(tile.index) * kAttnColumns + col;
-    const bool live = column < static_cast<int64_t>(tile.count) * group;
-    const int i = live ? static_cast<int>(column / group) : 0;
-    const int64_t row = tile.start + i;
-    const int qh = head * group + (live ? static_cast<int>(column % group) : 0);
-    const int64_t capacity = static_cast<int64_t>(b.table_width) * a.cache.page_size;
-    const int64_t length = b.lengths[tile.seq];
-    const int64_t inside = length < 0 ? 0 : length < capacity ? length : capacity;
-    const int64_t first_pos = length - (b.row_starts ? b.row_starts[tile.seq + 1] - b.row_starts[tile.seq] : 1);
-    const int64_t pos = first_pos + i;
-    const int64_t see_end = a.causal && pos + 1 < inside ? (pos + 1 > 0 ? pos + 1 : 0) : inside;
-    const int64_t see_begin = a.window && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0;
-    // the workgroup's range: from its first row's begin to its last row's end
-    const int64_t i_lo = static_cast<int64_t>(tile.index) * kAttnColumns / group;
-    int64_t i_hi = (static_cast<int64_t>(tile.index) * kAttnColumns + kAttnColumns - 1) / group;
-    if (i_hi > tile.count - 1) i_hi = tile.count - 1;
-    const int64_t p_lo = first_pos + i_lo, p_hi = first_pos + i_hi;
-    const int64_t end = a.causal && p_hi + 1 < inside ? (p_hi + 1 > 0 ? p_hi + 1 : 0) : inside;
-    const int64_t begin = a.window && p_lo - a.window + 1 > 0 ? p_lo - a.window + 1 : 0;
-    const int step0 = static_cast<int>(begin / kKvStep), step1 = static_cast<int>((end + kKvStep - 1) / kKvStep);
-    const int steps = step1 > step0 ? step1 - step0 : 0;
-    int per = (steps + A.splits - 1) / A.splits;
-    per = per > kAttnMinSteps ? per : kAttnMinSteps;
-    const int64_t from64 = step0 + static_cast<int64_t>(blockIdx.y) * per;
-    const int from = static_cast<int>(from64 < step1 ? from64 : step1), to = step1 - from < per ? step1 : from + per;
+    const int64_t first_column = static_cast<int64_t>(tile.index) * kAttnColumns, columns = static_cast<int64_t>(tile.count) * group;
+    const bool live = first_column + col < columns;
+    const int64_t column = live ? first_column + col : first_column;
+    const int64_t row = tile.start + column / group;
+    const int qh = head * group + static_cast<int>(column % group);
+    const Sight sight = sight_of(a, tile.seq);
+    const int see_from = static_cast<int>(sight.begin(column / group)), see_to = static_cast<int>(sight.end(column / group));
+    const int64_t last_column = first_column + kAttnColumns < columns ? first_column + kAttnColumns - 1 : columns - 1;
+    Steps steps = steps_of(sight, first_column / group, last_column / group);
+    take_part(steps, A.splits, static_cast<int>(blockIdx.y));
 
-    if (A.splits > 1 && from >= to) {                              // a part without tokens
+    if (A.splits > 1 && steps.from >= steps.to) {                              // a part without tokens
         if (wave == 0 && quarter == 0 && live) {
             float* ml = A.part_ml + ((static_cast<int64_t>(blockIdx.y) * b.rows + row) * a.q_heads + qh) * 2;
             ml[0] = kLowest;
@@ -213,23 +295,16 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
         return;
     }
 
-    // queries as the first product's second operand: lane (column, quarter) holds elements 64 b + 16 quarter + 8 j + e, in the
-    // order in which a dword's indices are decoded
+    // queries as the first product's second operand: lane (column, quarter) holds elements 64 b + 16 quarter + 8 j + e
     u32x4_t q[2 * NB];
 #pragma unroll
     for (int s = 0; s < 2 * NB; ++s) {
         u32x4_t v = {0, 0, 0, 0};
         if (live) v = *reinterpret_cast<const u32x4_t*>(a.q + row * a.q_stride + static_cast<int64_t>(qh) * D + s / 2 * 64 + quarter * 16 + s % 2 * 8);
-        q[s] = LUT_K ? v : even_odd(v);
+        q[s] = v;
     }
-    Centroids ck;
-    if (LUT_K) {
-        const uint32_t at = threadIdx.x;
-        table[at] = a.cache.codebooks[at & 15] | static_cast<uint32_t>(a.cache.codebooks[at >> 4]) << 16;
-        __syncthreads();
-    } else {
-        ck = load_centroids(a.cache.codebooks);
-    }
+    table[threadIdx.x] = a.cache.codebooks[threadIdx.x & 15] | static_cast<uint32_t>(a.cache.codebooks[threadIdx.x >> 4]) << 16;
+    __syncthreads();
     const Centroids cv = load_centroids(a.cache.codebooks + kKvCentroids);
     const float scale = a.scale * kLog2e;
 
@@ -238,39 +313,18 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
     for (int d = 0; d < DT; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = kLowest, l = 0.f;
 
-    // steps that every live column sees whole need no mask
-    const int64_t last_begin = a.window && p_hi - a.window + 1 > 0 ? p_hi - a.window + 1 : 0;
-    const int64_t first_end = a.causal && p_lo + 1 < inside ? (p_lo + 1 > 0 ? p_lo + 1 : 0) : inside;
-    const int whole_from = static_cast<int>((last_begin + kKvStep - 1) / kKvStep), whole_to = static_cast<int>(first_end / kKvStep);
-    const int see_from = static_cast<int>(see_begin), see_to = static_cast<int>(see_end);
-
-    const int32_t* const table_row = b.page_table + static_cast<int64_t>(tile.seq) * b.table_width;
-    const int64_t page_stride = static_cast<int64_t>(a.cache.kv_heads) * (a.cache.page_size / kKvTile) * kTile;
-    const uint8_t* const head_base = a.cache.pages + static_cast<int64_t>(head) * (a.cache.page_size / kKvTile) * kTile;
-    const int steps_per_page = a.cache.page_size / kKvStep;
-    int step = from + wave;
-    int slot = step / steps_per_page, within = step - slot * steps_per_page;      // of the step whose page is looked up next
-    const auto look_up = [&](int s) {                     // page of step s, whose place is (slot, within); then on to the wave's next step
-        const int page = s < to ? table_row[slot] : 0;
-        const bool there = page >= 0 && page < a.cache.num_pages;
-        const uint8_t* base = head_base + (there ? page : 0) * page_stride + within * (2 * kTile);
-        within += kAttnWaves;
-        while (within >= steps_per_page) {
-            within -= steps_per_page;
-            ++slot;
-        }
-        return Place{base, there};
-    };
-    Place at = look_up(step), next = look_up(step + kAttnWaves);
+    int step = steps.from + wave;
+    Walk<D> walk(a, tile.seq, head, step);
+    Place at = walk.next(step < steps.to, kAttnWaves), next = walk.next(step + kAttnWaves < steps.to, kAttnWaves);
     KWords<D> kw;
-    if (step < to) kw.load(at.base, lane, quarter);
-    for (; step < to; step += kAttnWaves) {
+    if (step < steps.to) kw.load(at.base, lane, quarter);
+    for (; step < steps.to; step += kAttnWaves) {
         uint32_t vw[2][D / 32];
 #pragma unroll
         for (int t = 0; t < 2; ++t) load_words<D / 32>(vw[t], at.base + t * kTile + 8 * D + lane * (D / 8));
         const KWords<D> now = kw;
-        if (step + kAttnWaves < to) kw.load(next.base, lane, quarter);
-        const Place after = look_up(step + 2 * kAttnWaves);
+        if (step + kAttnWaves < steps.to) kw.load(next.base, lane, quarter);
+        const Place after = walk.next(step + 2 * kAttnWaves < steps.to, kAttnWaves);
 
         float s[8];
 #pragma unroll
@@ -282,7 +336,7 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const uint32_t w = now.k[t][2 * n + j];
-                    acc = mfma(LUT_K ? decode8_table(table, w) : decode8(ck, w), q[2 * n + j], acc);
+                    acc = mfma(decode8_table(table, w), q[2 * n + j], acc);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[e] = fmaf(acc[e], half_of(now.sc[t][n * 2 + e / 2], e % 2), sum[e]);
@@ -295,7 +349,7 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int e = 0; e < 8; ++e) sv[n][e] = half_of(now.sc[e / 4][(NB + n) * 2 + e % 4 / 2], e % 2);
-        if (step < whole_from || step >= whole_to || !at.there) {
+        if (step < steps.whole_from || step >= steps.whole_to || !at.there) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
@@ -305,24 +359,7 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
                 for (int n = 0; n < NB; ++n) sv[n][e] = seen ? sv[n][e] : 0.f;       // (what lies behind a sequence may be anything)
             }
         }
-        float top = s[0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
-        if (__ballot(top > m + kSlack)) {
-            top = fmaxf(m, max_over_quarters(top));
-            const float shrink = __builtin_amdgcn_exp2f(m - top);
-            m = top;
-            l *= shrink;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[d][e] *= shrink;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s[e] = __builtin_amdgcn_exp2f(s[e] - m);
-            l += s[e];
-        }
+        soften<DT>(s, m, l, o);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             u32x4_t p;
@@ -393,34 +430,277 @@ __global__ void __launch_bounds__(kAttnThreads) attn_kernel(AttnArgs A) {
     }
 }
 
-// The parts of a (row, query head) pair joined, a wave a pair.  Parts without tokens wrote a sum of zero and are passed over.
+// Many columns a sequence (prompts, long drafts): a workgroup takes 4 x 16 x CT columns, 16 x CT a wave, and its waves decode every step
+// together, a quarter of it each, into shared memory in the order of the first product's and the second product's first operand.
+// Two such buffers: the next step is decoded into one while the products read the other.
+template <int D, int CT>
+__global__ void __launch_bounds__(kAttnThreads, 2) attn_tile_kernel(AttnArgs A) {
+    constexpr int NB = D / KMQ_BLOCK, DT = D / 16, KF = D / 32;
+    constexpr int kTile = 17 * D, kColumns = kAttnWaves * 16 * CT;
+    constexpr int KD = D / 64, VD = D > 128 ? D / 128 : 1;          // a wave's dwords a lane: of K in one tile, of V in each of the two
+    __shared__ u32x4_t kf[2][2 * KF][kWave], vf[2][DT][kWave];
+    __shared__ uint32_t scales[2][D / 2];
+    const AttentionArgs& a = A.a;
+    const KvBatchArgs& b = a.batch;
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int col = lane & 15, quarter = lane >> 4;
+    const int head = static_cast<int>(blockIdx.x) % a.cache.kv_heads;
+    const int group = a.q_heads / a.cache.kv_heads;
+    // the last tiles first: they see most
+    const Tile tile = find_tile(b, group, kColumns, static_cast<int>(gridDim.x / a.cache.kv_heads - 1 - blockIdx.x / a.cache.kv_heads));
+    if (tile.seq < 0) return;
+
+    const int64_t columns = static_cast<int64_t>(tile.count) * group;
+    const int64_t first_column = static_cast<int64_t>(tile.index) * kColumns, mine = first_column + wave * 16 * CT;
+    const int64_t last_column = first_column + kColumns < columns ? first_column + kColumns - 1 : columns - 1;
+    const int64_t my_last = mine + 16 * CT < columns ? mine + 16 * CT - 1 : columns - 1;
+    const bool busy = mine < columns;                                // a wave without columns decodes all the same
+    const Sight sight = sight_of(a, tile.seq);
+    Steps steps = steps_of(sight, first_column / group, last_column / group);
+    Steps own = steps_of(sight, (busy ? mine : first_column) / group, (busy ? my_last : first_column) / group);
+    take_part(steps, A.splits, static_cast<int>(blockIdx.y));
+
+    u32x4_t q[CT][2 * NB];
+    f32x4_t o[CT][DT];
+    float m[CT], l[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        const int64_t column = mine + 16 * c + col;
+        const bool live = column < columns;
+        const uint16_t* from = a.q + (tile.start + (live ? column / group : 0)) * a.q_stride + (head * group + (live ? static_cast<int>(column % group) : 0)) * D;
+#pragma unroll
+        for (int s = 0; s < 2 * NB; ++s) {
+            u32x4_t v = {0, 0, 0, 0};
+            if (live) v = *reinterpret_cast<const u32x4_t*>(from + s / 2 * 64 + quarter * 16 + s % 2 * 8);
+            q[c][s] = even_odd(v);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[c][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        m[c] = kLowest;
+        l[c] = 0.f;
+    }
+    const Centroids ck = load_centroids(a.cache.codebooks), cv = load_centroids(a.cache.codebooks + kKvCentroids);
+    const float scale = a.scale * kLog2e;
+
+    // this wave's share of a step
+    const int kt = wave >> 1, k0 = (wave & 1) * KD;                  // K: a tile's half of its dwords
+    const int v0 = D > 64 ? wave * VD : wave >> 1;                   // V: dwords of both tiles; 64 elements: half of the nibbles of one
+    uint32_t kw[KD], vw[2][VD], sw = 0;
+    const auto load = [&](const uint8_t* base) {
+        const uint8_t* k = base + kt * kTile + lane * (D / 8) + 4 * k0;
+        if constexpr (KD == 1) kw[0] = *reinterpret_cast<const uint32_t*>(k);
+        else load_words<KD>(kw, k);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint8_t* v = base + t * kTile + 8 * D + lane * (D / 8) + 4 * v0;
+            if constexpr (VD == 1) vw[t][0] = *reinterpret_cast<const uint32_t*>(v);
+            else load_words<VD>(vw[t], v);
+        }
+        if (tid < D / 2) sw = *reinterpret_cast<const uint32_t*>(base + tid / (D / 4) * kTile + 16 * D + tid % (D / 4) * 4);
+    };
+    const auto decode = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < KD; ++i) kf[buffer][kt * KF + k0 + i][lane] = decode8(ck, kw[i]);
+        if constexpr (D > 64) {
+#pragma unroll
+            for (int i = 0; i < VD; ++i) {
+                const u32x4_t x = decode8(cv, vw[0][i]), y = decode8(cv, vw[1][i]);
+                vf[buffer][2 * (v0 + i)][lane] = u32x4_t{x[0], x[1], y[0], y[1]};
+                vf[buffer][2 * (v0 + i) + 1][lane] = u32x4_t{x[2], x[3], y[2], y[3]};
+            }
+        } else {
+            const int shift = (wave & 1) * 4;
+            uint32_t r[4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const uint32_t w = vw[t][0] >> shift;
+                decode4(cv, w & 0x07070707u, (w >> 1 & 0x04040404u) | 0x03020100u, r[2 * t], r[2 * t + 1]);
+            }
+            vf[buffer][wave][lane] = u32x4_t{r[0], r[1], r[2], r[3]};
+        }
+        if (tid < D / 2) scales[buffer][tid] = sw;
+    };
+
+    Walk<D> walk(a, tile.seq, head, steps.from);
+    Place at = walk.next(steps.from < steps.to, 1), next = walk.next(steps.from + 1 < steps.to, 1);
+    bool decoded = at.there, coming = next.there;                    // whether the step in the buffer, and the one in registers, is in the cache
+    if (steps.from < steps.to) {
+        load(at.base);
+        decode(0);
+        if (steps.from + 1 < steps.to) load(next.base);
+    }
+    __syncthreads();
+    for (int step = steps.from, buffer = 0; step < steps.to; ++step, buffer ^= 1) {
+        const bool there = decoded;
+        if (step + 1 < steps.to) {
+            decode(buffer ^ 1);
+            decoded = coming;
+            next = walk.next(step + 2 < steps.to, 1);
+            coming = next.there;
+            if (step + 2 < steps.to) load(next.base);
+        }
+        if (busy && step >= own.from && step < own.to) {
+            float s[CT][8];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
+                    const u32x4_t a0 = kf[buffer][t * KF + 2 * n][lane], a1 = kf[buffer][t * KF + 2 * n + 1][lane];
+                    const u32x2_t sk = *reinterpret_cast<const u32x2_t*>(&scales[buffer][t * (D / 4) + quarter * (D / 16) + 2 * n]);
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) {
+                        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+                        acc = mfma(a0, q[c][2 * n], acc);
+                        acc = mfma(a1, q[c][2 * n + 1], acc);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float k = half_of(sk[e / 2], e % 2) * scale;
+                            s[c][4 * t + e] = n ? fmaf(acc[e], k, s[c][4 * t + e]) : acc[e] * k;
+                        }
+                    }
+                }
+            const bool masked = step < own.whole_from || step >= own.whole_to || !there;
+            uint32_t unseen[CT];                                     // a bit a token of this lane
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                unseen[c] = 0;
+                if (masked) {
+                    const int64_t column = mine + 16 * c + col, i = (column < columns ? column : columns - 1) / group;
+                    const int from = static_cast<int>(sight.begin(i)), to = static_cast<int>(sight.end(i));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
+                        const bool seen = there && j >= from && j < to;
+                        s[c][e] = seen ? s[c][e] : -INFINITY;
+                        unseen[c] |= seen ? 0u : 1u << e;
+                    }
+                }
+                soften<DT>(s[c], m[c], l[c], o[c]);
+            }
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                u32x4_t p[CT];
+                float sv[8];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const u32x2_t w = *reinterpret_cast<const u32x2_t*>(&scales[buffer][t * (D / 4) + quarter * (D / 16) + 2 * (NB + n)]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sv[4 * t + e] = half_of(w[e / 2], e % 2);
+                }
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    float w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = s[c][e] * sv[e];
+                    if (masked) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[e] = unseen[c] >> e & 1u ? 0.f : w[e];      // (what lies behind a sequence may be anything)
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) p[c][e / 2] = pack_bf16(w[e], w[e + 1]);
+                }
+#pragma unroll
+                for (int d = 4 * n; d < 4 * n + 4; ++d) {
+                    const u32x4_t v = vf[buffer][d][lane];
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) o[c][d] = mfma(v, p[c], o[c][d]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+
+    const bool whole = A.splits == 1;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        const int64_t column = mine + 16 * c + col;
+        const float all = sum_over_quarters(l[c]);
+        if (column >= columns) continue;
+        const bool none = all == 0.f;
+        const float norm = none ? 0.f : 1.f / all;
+        const int64_t row = tile.start + column / group;
+        const int qh = head * group + static_cast<int>(column % group);
+        const int64_t pair = row * a.q_heads + qh;
+        if (quarter == 0) {
+            if (!whole) {
+                float* ml = A.part_ml + (static_cast<int64_t>(blockIdx.y) * b.rows * a.q_heads + pair) * 2;
+                ml[0] = m[c];
+                ml[1] = all;
+            } else if (a.lse) {
+                a.lse[pair] = none ? -INFINITY : (m[c] + __builtin_amdgcn_logf(all)) * kLn2;
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const f32x4_t v = o[c][d];
+            const int at_d = 16 * d + 4 * quarter;
+            if (whole) {
+                const u32x2_t r = {pack_bf16(none ? 0.f : v[0] * norm, none ? 0.f : v[1] * norm), pack_bf16(none ? 0.f : v[2] * norm, none ? 0.f : v[3] * norm)};
+                *reinterpret_cast<u32x2_t*>(a.out + row * a.out_stride + static_cast<int64_t>(qh) * D + at_d) = r;
+            } else if (!none) {
+                *reinterpret_cast<f32x4_t*>(A.part_o + (static_cast<int64_t>(blockIdx.y) * b.rows * a.q_heads + pair) * D + at_d) = v;
+            }
+        }
+    }
+}
+
+// The parts of a (row, query head) pair joined, a workgroup a pair: a thread a part for the weights, then D / 4 threads a part and
+// several parts at once for the sums, which are added in a fixed order.  Parts without tokens have no sums and are passed over.
 template <int D>
 __global__ void __launch_bounds__(kAttnThreads) attn_join_kernel(AttnArgs A) {
+    constexpr int kLanes = D / 4, kAtOnce = kAttnThreads / kLanes;
+    __shared__ float weight[kAttnThreads], scratch[2][kAttnWaves];
+    __shared__ f32x4_t sums[kAtOnce][kLanes];
     const AttentionArgs& a = A.a;
-    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
-    const int64_t pairs = a.batch.rows * a.q_heads;
-    const int64_t pair = static_cast<int64_t>(blockIdx.x) * kAttnWaves + threadIdx.x / kWave;
-    if (pair >= pairs) return;
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1), wave = tid / kWave;
+    const int64_t pairs = a.batch.rows * a.q_heads, pair = blockIdx.x;
     const int64_t row = pair / a.q_heads;
     if (kv_find_row(a.batch, row).seq < 0) return;                 // rows of no sequence stay as they were
-    float most = kLowest;
-    for (int s = 0; s < A.splits; ++s) most = fmaxf(most, A.part_ml[(s * pairs + pair) * 2]);
-    float all = 0.f, sum[D / 64];
-#pragma unroll
-    for (int n = 0; n < D / 64; ++n) sum[n] = 0.f;
-    for (int s = 0; s < A.splits; ++s) {
-        const float l = A.part_ml[(s * pairs + pair) * 2 + 1];
-        if (l == 0.f) continue;
-        const float w = __builtin_amdgcn_exp2f(A.part_ml[(s * pairs + pair) * 2] - most);
-        all += l * w;
-#pragma unroll
-        for (int n = 0; n < D / 64; ++n) sum[n] = fmaf(A.part_o[(s * pairs + pair) * D + n * 64 + lane], w, sum[n]);
+    float m = kLowest, l = 0.f;
+    if (tid < A.splits) {
+        const float* ml = A.part_ml + (tid * pairs + pair) * 2;
+        m = ml[0];
+        l = ml[1];
     }
-    const bool none = all == 0.f;
-    uint16_t* out = a.out + row * a.out_stride + (pair - row * a.q_heads) * D;
+    float most = m;
 #pragma unroll
-    for (int n = 0; n < D / 64; ++n) out[n * 64 + lane] = none ? 0 : f32_to_bf16(sum[n] / all);
-    if (a.lse && lane == 0) a.lse[pair] = none ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kLn2;
+    for (int d = 1; d < kWave; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+    if (lane == 0) scratch[0][wave] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) most = fmaxf(most, scratch[0][w]);
+    const float mine = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - most);
+    weight[tid] = mine;
+    float all = l * mine;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) all += __shfl_xor(all, d);
+    if (lane == 0) scratch[1][wave] = all;
+    __syncthreads();
+    all = 0.f;
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w) all += scratch[1][w];
+
+    const int part = tid / kLanes, d = tid % kLanes;
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = part; s < A.splits; s += kAtOnce) {
+        const float w = weight[s];
+        if (w == 0.f) continue;
+        const f32x4_t o = *reinterpret_cast<const f32x4_t*>(A.part_o + (s * pairs + pair) * D + 4 * d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = fmaf(o[e], w, sum[e]);
+    }
+    sums[part][d] = sum;
+    __syncthreads();
+    if (part) return;
+#pragma unroll
+    for (int p = 1; p < kAtOnce; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += sums[p][d][e];
+    const bool none = all == 0.f;
+    const u32x2_t r = {pack_bf16(none ? 0.f : sum[0] / all, none ? 0.f : sum[1] / all), pack_bf16(none ? 0.f : sum[2] / all, none ? 0.f : sum[3] / all)};
+    *reinterpret_cast<u32x2_t*>(a.out + row * a.out_stride + (pair - row * a.q_heads) * D + 4 * d) = r;
+    if (a.lse && d == 0) a.lse[pair] = none ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kLn2;
 }
 
 static int64_t column_tiles(const KvBatchArgs& b, int group, int columns) {
@@ -429,14 +709,29 @@ static int64_t column_tiles(const KvBatchArgs& b, int group, int columns) {
     return (b.rows * group + (columns - 1) * used) / columns;
 }
 
+#ifndef TARGET
+#define TARGET 768
+#endif
+#ifndef TTARGET
+#define TTARGET 512
+#endif
+#ifndef CT1
+#define CT1 2
+#endif
+#ifndef WIDE
+#define WIDE 32
+#endif
+constexpr int kTileColumns = kAttnWaves * 16 * CT1;
 AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
-    AttentionPlan p{"kv_attention", kAttnColumns, 1, 0};
-    const int64_t items = column_tiles(b, q_heads / c.kv_heads, kAttnColumns) * c.kv_heads;
+    const int group = q_heads / c.kv_heads;
+    const bool wide = b.rows * group > static_cast<int64_t>(WIDE) * b.sequences;
+    AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? kTileColumns : kAttnColumns, 1, 0};
+    const int64_t items = column_tiles(b, group, p.columns) * c.kv_heads;
     const int64_t steps = static_cast<int64_t>(b.table_width) * (c.page_size / kKvStep);
-    int64_t splits = (1024 + items - 1) / (items > 0 ? items : 1);
+    int64_t splits = ((wide ? TTARGET : TARGET) + items - 1) / (items > 0 ? items : 1);
     const int64_t most = (steps + kAttnMinSteps - 1) / kAttnMinSteps;
     if (splits > most) splits = most;
-    if (splits > 256) splits = 256;
+    if (splits > kAttnThreads) splits = kAttnThreads;              // (the joining kernel has a thread a part)
     if (splits > 1) {
         p.splits = static_cast<int>(splits);
         p.workspace_bytes = static_cast<size_t>(splits) * b.rows * q_heads * (c.head_dim + 2) * sizeof(float);
@@ -445,12 +740,15 @@ AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_h
 }
 
 template <int D>
-static hipError_t launch_attn(const AttnArgs& A, int64_t items, hipStream_t s) {
-    attn_kernel<D><<<dim3(static_cast<unsigned>(items), static_cast<unsigned>(A.splits)), kAttnThreads, 0, s>>>(A);
-    hipError_t e = hipGetLastError();
+static hipError_t launch_attn(const AttnArgs& A, const AttentionPlan& p, hipStream_t s) {
+    const KvBatchArgs& b = A.a.batch;
+    const int64_t items = column_tiles(b, A.a.q_heads / A.a.cache.kv_heads, p.columns) * A.a.cache.kv_heads;
+    const dim3 grid(static_cast<unsigned>(items), static_cast<unsigned>(A.splits));
+    if (p.columns == kAttnColumns) attn_kernel<D><<<grid, kAttnThreads, 0, s>>>(A);
+    else attn_tile_kernel<D, CT1><<<grid, kAttnThreads, 0, s>>>(A);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits == 1) return e;
-    const int64_t pairs = A.a.batch.rows * A.a.q_heads;
-    attn_join_kernel<D><<<dim3(static_cast<unsigned>((pairs + kAttnWaves - 1) / kAttnWaves)), kAttnThreads, 0, s>>>(A);
+    attn_join_kernel<D><<<dim3(static_cast<unsigned>(b.rows * A.a.q_heads)), kAttnThreads, 0, s>>>(A);
     return hipGetLastError();
 }
 
@@ -459,11 +757,10 @@ hipError_t launch_attention(const AttentionArgs& a, hipStream_t s) {
     const AttentionPlan p = attention_plan(a.cache, a.batch, a.q_heads);
     AttnArgs A{a, p.splits, static_cast<float*>(a.workspace), nullptr};
     if (p.splits > 1) A.part_ml = A.part_o + static_cast<int64_t>(p.splits) * a.batch.rows * a.q_heads * a.cache.head_dim;
-    const int64_t items = column_tiles(a.batch, a.q_heads / a.cache.kv_heads, p.columns) * a.cache.kv_heads;
     switch (a.cache.head_dim) {
-        case 64: return launch_attn<64>(A, items, s);
-        case 128: return launch_attn<128>(A, items, s);
-        default: return launch_attn<256>(A, items, s);
+        case 64: return launch_attn<64>(A, p, s);
+        case 128: return launch_attn<128>(A, p, s);
+        default: return launch_attn<256>(A, p, s);
     }
 }
 
