@@ -9,6 +9,8 @@
 // as they are, because V is stored in that order of tokens (kmq_kv.h): no probability crosses a lane.
 // Maxima, sums and products are kept in 32 bits; queries and centroids are bf16 as they come, and p * sV is rounded to
 // bf16 for the second product (off by 2^-8 of itself at most, to either side; the sum of p that divides it is not rounded).
+#include <type_traits>
+
 #include "kmq_kv.h"
 
 namespace kmq {
@@ -228,28 +230,39 @@ struct Walk {
     }
 };
 
-// Scores of a column (base 2, this lane's four tokens of each of a step's tiles) on their way to the second product: the running
-// maximum m and sum l, and what is accumulated already, brought to a new maximum where a score passes the old one by kSlack.
-template <int DT>
-__device__ __forceinline__ void soften(float (&s)[8], float& m, float& l, f32x4_t (&o)[DT]) {
-    float top = s[0];
+// Scores of CT columns (base 2, this lane's four tokens of each of a step's tiles) on their way to the second product.  The running
+// maxima m and sums l, and what is accumulated already, are brought to new maxima where a score passes an old one by kSlack;
+// then scores become exp2(score - maximum) and are added up.
+template <int CT, int DT>
+__device__ __forceinline__ void soften(float (&s)[CT][8], float (&m)[CT], float (&l)[CT], f32x4_t (&o)[CT][DT]) {
+    float top[CT];
+    bool past = false;
 #pragma unroll
-    for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
-    if (__ballot(top > m + kSlack)) {
-        top = fmaxf(m, max_over_quarters(top));
-        const float shrink = __builtin_amdgcn_exp2f(m - top);
-        m = top;
-        l *= shrink;
+    for (int c = 0; c < CT; ++c) {
+        top[c] = s[c][0];
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int e = 1; e < 8; ++e) top[c] = fmaxf(top[c], s[c][e]);
+        past |= top[c] > m[c] + kSlack;
+    }
+    if (__ballot(past)) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[d][e] *= shrink;
+        for (int c = 0; c < CT; ++c) {
+            const float to = fmaxf(m[c], max_over_quarters(top[c])), shrink = __builtin_amdgcn_exp2f(m[c] - to);
+            m[c] = to;
+            l[c] *= shrink;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[c][d][e] *= shrink;
+        }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        s[e] = __builtin_amdgcn_exp2f(s[e] - m);
-        l += s[e];
-    }
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[c][e] = __builtin_amdgcn_exp2f(s[c][e] - m[c]);
+            l[c] += s[c][e];
+        }
 }
 
 // Few columns a sequence (single tokens, drafts): a workgroup takes 16 columns, and its waves take the steps in turn.  A wave reads
@@ -275,14 +288,14 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     if (tile.seq < 0) return;
 
     // this lane's column, and the tokens it may see
-    const int64_t first_column = static_cast<int64_t>(tile.index) * kAttnColumns, columns = static_cast<int64_t>(tile.count) * group;
+    const int first_column = tile.index * kAttnColumns, columns = tile.count * group;      // (fewer than 2^30: kmq_kv_attention sees to it)
     const bool live = first_column + col < columns;
-    const int64_t column = live ? first_column + col : first_column;
-    const int64_t row = tile.start + column / group;
-    const int qh = head * group + static_cast<int>(column % group);
+    const int column = live ? first_column + col : first_column, i = column / group;
+    const int64_t row = tile.start + i;
+    const int qh = head * group + column - i * group;
     const Sight sight = sight_of(a, tile.seq);
-    const int see_from = static_cast<int>(sight.begin(column / group)), see_to = static_cast<int>(sight.end(column / group));
-    const int64_t last_column = first_column + kAttnColumns < columns ? first_column + kAttnColumns - 1 : columns - 1;
+    const int see_from = static_cast<int>(sight.begin(i)), see_to = static_cast<int>(sight.end(i));
+    const int last_column = first_column + kAttnColumns < columns ? first_column + kAttnColumns - 1 : columns - 1;
     Steps steps = steps_of(sight, first_column / group, last_column / group);
     take_part(steps, A.splits, static_cast<int>(blockIdx.y));
 
@@ -308,10 +321,10 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     const Centroids cv = load_centroids(a.cache.codebooks + kKvCentroids);
     const float scale = a.scale * kLog2e;
 
-    f32x4_t o[DT];
+    f32x4_t o[1][DT];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float m = kLowest, l = 0.f;
+    for (int d = 0; d < DT; ++d) o[0][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m[1] = {kLowest}, l[1] = {0.f};
 
     int step = steps.from + wave;
     Walk<D> walk(a, tile.seq, head, step);
@@ -326,7 +339,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
         if (step + kAttnWaves < steps.to) kw.load(next.base, lane, quarter);
         const Place after = walk.next(step + 2 * kAttnWaves < steps.to, kAttnWaves);
 
-        float s[8];
+        float s[1][8];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
@@ -342,7 +355,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
                 for (int e = 0; e < 4; ++e) sum[e] = fmaf(acc[e], half_of(now.sc[t][n * 2 + e / 2], e % 2), sum[e]);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[4 * t + e] = sum[e] * scale;
+            for (int e = 0; e < 4; ++e) s[0][4 * t + e] = sum[e] * scale;
         }
         float sv[NB][8];
 #pragma unroll
@@ -354,22 +367,22 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
             for (int e = 0; e < 8; ++e) {
                 const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
                 const bool seen = at.there && j >= see_from && j < see_to;
-                s[e] = seen ? s[e] : -INFINITY;
+                s[0][e] = seen ? s[0][e] : -INFINITY;
 #pragma unroll
                 for (int n = 0; n < NB; ++n) sv[n][e] = seen ? sv[n][e] : 0.f;       // (what lies behind a sequence may be anything)
             }
         }
-        soften<DT>(s, m, l, o);
+        soften<1, DT>(s, m, l, o);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             u32x4_t p;
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) p[e / 2] = pack_bf16(s[e] * sv[n][e], s[e + 1] * sv[n][e + 1]);
+            for (int e = 0; e < 8; e += 2) p[e / 2] = pack_bf16(s[0][e] * sv[n][e], s[0][e + 1] * sv[n][e + 1]);
 #pragma unroll
             for (int j = 2 * n; j < 2 * n + 2; ++j) {
                 const u32x4_t x = decode8(cv, vw[0][j]), y = decode8(cv, vw[1][j]);
-                o[2 * j] = mfma(u32x4_t{x[0], x[1], y[0], y[1]}, p, o[2 * j]);
-                o[2 * j + 1] = mfma(u32x4_t{x[2], x[3], y[2], y[3]}, p, o[2 * j + 1]);
+                o[0][2 * j] = mfma(u32x4_t{x[0], x[1], y[0], y[1]}, p, o[0][2 * j]);
+                o[0][2 * j + 1] = mfma(u32x4_t{x[2], x[3], y[2], y[3]}, p, o[0][2 * j + 1]);
             }
         }
         at = next;
@@ -377,10 +390,10 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     }
 
     // the waves' results joined: every wave's on the scale of the largest maximum
-    l = sum_over_quarters(l);
+    const float sum_l = sum_over_quarters(l[0]);
     if (quarter == 0) {
-        stat[0][wave][col] = m;
-        stat[1][wave][col] = l;
+        stat[0][wave][col] = m[0];
+        stat[1][wave][col] = sum_l;
     }
     __syncthreads();
     float most = stat[0][0][col], all = 0.f;
@@ -400,14 +413,14 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
             a.lse[pair] = none ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kLn2;
         }
     }
-    const float weight = __builtin_amdgcn_exp2f(m - most), norm = none ? 0.f : 1.f / all;
+    const float weight = __builtin_amdgcn_exp2f(m[0] - most), norm = none ? 0.f : 1.f / all;
 #pragma unroll
     for (int c0 = 0; c0 < D; c0 += DC) {
         if (c0) __syncthreads();
 #pragma unroll
         for (int d = 0; d < DC / 16; ++d)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[wave][col][16 * d + 4 * quarter + e] = o[c0 / 16 + d][e] * weight;
+            for (int e = 0; e < 4; ++e) part[wave][col][16 * d + 4 * quarter + e] = o[0][c0 / 16 + d][e] * weight;
         __syncthreads();
         // a wave's lane writes its column's elements 4 x (wave * 4 + quarter) + 64 x n
 #pragma unroll
@@ -430,16 +443,20 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     }
 }
 
-// Many columns a sequence (prompts, long drafts): a workgroup takes 4 x 16 x CT columns, 16 x CT a wave, and its waves decode every step
-// together, a quarter of it each, into shared memory in the order of the first product's and the second product's first operand.
+// Many columns a sequence (prompts, long drafts): a workgroup takes 16 x CT columns a wave, and its waves decode every step
+// together, an equal share of it each, into shared memory in the order of the first product's and the second product's first operand.
 // Two such buffers: the next step is decoded into one while the products read the other.
-template <int D, int CT>
-__global__ void __launch_bounds__(kAttnThreads, 2) attn_tile_kernel(AttnArgs A) {
+template <int D, int CT, int WAVES>
+__global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_kernel(AttnArgs A) {
     constexpr int NB = D / KMQ_BLOCK, DT = D / 16, KF = D / 32;
-    constexpr int kTile = 17 * D, kColumns = kAttnWaves * 16 * CT;
-    constexpr int KD = D / 64, VD = D > 128 ? D / 128 : 1;          // a wave's dwords a lane: of K in one tile, of V in each of the two
+    constexpr int kTile = 17 * D, kColumns = WAVES * 16 * CT;
+    // a wave's dwords a lane: of K in one tile (a share of it), of V in both tiles (of fewer than there are waves: half of the nibbles)
+    constexpr int kShares = WAVES / 2, KD = KF / kShares;
+    constexpr bool kHalves = KF < WAVES;
+    constexpr int VD = kHalves ? 1 : KF / WAVES;
+    static_assert(KD >= 1 && (!kHalves || WAVES == 2 * KF), "a share is a dword at least");
     __shared__ u32x4_t kf[2][2 * KF][kWave], vf[2][DT][kWave];
-    __shared__ uint32_t scales[2][D / 2];
+    __shared__ float scales[2][2 * D / 2];                              // in the tiles' order, K's times the scale of the scores
     const AttentionArgs& a = A.a;
     const KvBatchArgs& b = a.batch;
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -450,10 +467,10 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_tile_kernel(AttnArgs A) 
     const Tile tile = find_tile(b, group, kColumns, static_cast<int>(gridDim.x / a.cache.kv_heads - 1 - blockIdx.x / a.cache.kv_heads));
     if (tile.seq < 0) return;
 
-    const int64_t columns = static_cast<int64_t>(tile.count) * group;
-    const int64_t first_column = static_cast<int64_t>(tile.index) * kColumns, mine = first_column + wave * 16 * CT;
-    const int64_t last_column = first_column + kColumns < columns ? first_column + kColumns - 1 : columns - 1;
-    const int64_t my_last = mine + 16 * CT < columns ? mine + 16 * CT - 1 : columns - 1;
+    const int columns = tile.count * group;
+    const int first_column = tile.index * kColumns, mine = first_column + wave * 16 * CT;
+    const int last_column = first_column + kColumns < columns ? first_column + kColumns - 1 : columns - 1;
+    const int my_last = mine + 16 * CT < columns ? mine + 16 * CT - 1 : columns - 1;
     const bool busy = mine < columns;                                // a wave without columns decodes all the same
     const Sight sight = sight_of(a, tile.seq);
     Steps steps = steps_of(sight, first_column / group, last_column / group);
@@ -463,11 +480,15 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_tile_kernel(AttnArgs A) 
     u32x4_t q[CT][2 * NB];
     f32x4_t o[CT][DT];
     float m[CT], l[CT];
+    int see_from[CT], see_to[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        const int64_t column = mine + 16 * c + col;
+        const int column = mine + 16 * c + col;
         const bool live = column < columns;
-        const uint16_t* from = a.q + (tile.start + (live ? column / group : 0)) * a.q_stride + (head * group + (live ? static_cast<int>(column % group) : 0)) * D;
+        const int at_column = live ? column : columns - 1, i = at_column / group;
+        see_from[c] = static_cast<int>(sight.begin(i));
+        see_to[c] = static_cast<int>(sight.end(i));
+        const uint16_t* from = a.q + static_cast<int64_t>(tile.start + i) * a.q_stride + (head * group + at_column - i * group) * D;
 #pragma unroll
         for (int s = 0; s < 2 * NB; ++s) {
             u32x4_t v = {0, 0, 0, 0};
@@ -480,11 +501,10 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_tile_kernel(AttnArgs A) 
         l[c] = 0.f;
     }
     const Centroids ck = load_centroids(a.cache.codebooks), cv = load_centroids(a.cache.codebooks + kKvCentroids);
-    const float scale = a.scale * kLog2e;
 
     // this wave's share of a step
-    const int kt = wave >> 1, k0 = (wave & 1) * KD;                  // K: a tile's half of its dwords
-    const int v0 = D > 64 ? wave * VD : wave >> 1;                   // V: dwords of both tiles; 64 elements: half of the nibbles of one
+    const int kt = wave / kShares, k0 = wave % kShares * KD;
+    const int v0 = kHalves ? wave >> 1 : wave * VD;
     uint32_t kw[KD], vw[2][VD], sw = 0;
     const auto load = [&](const uint8_t* base) {
         const uint8_t* k = base + kt * kTile + lane * (D / 8) + 4 * k0;
@@ -498,10 +518,11 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_tile_kernel(AttnArgs A) 
         }
         if (tid < D / 2) sw = *reinterpret_cast<const uint32_t*>(base + tid / (D / 4) * kTile + 16 * D + tid % (D / 4) * 4);
     };
+    const float sf = tid / (2 * NB) & 1 ? 1.f : a.scale * kLog2e;     // (dword tid of the scales: its quarter's K, then V)
     const auto decode = [&](int buffer) {
 #pragma unroll
         for (int i = 0; i < KD; ++i) kf[buffer][kt * KF + k0 + i][lane] = decode8(ck, kw[i]);
-        if constexpr (D > 64) {
+        if constexpr (!kHalves) {
 #pragma unroll
             for (int i = 0; i < VD; ++i) {
                 const u32x4_t x = decode8(cv, vw[0][i]), y = decode8(cv, vw[1][i]);
@@ -518,7 +539,68 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_tile_kernel(AttnArgs A) 
             }
             vf[buffer][wave][lane] = u32x4_t{r[0], r[1], r[2], r[3]};
         }
-        if (tid < D / 2) scales[buffer][tid] = sw;
+        if (tid < D / 2) {
+            scales[buffer][2 * tid] = half_of(sw, 0) * sf;
+            scales[buffer][2 * tid + 1] = half_of(sw, 1) * sf;
+        }
+    };
+    const auto multiply = [&](int step, int buffer, bool there, auto masked) {
+        float s[CT][8];
+        __builtin_amdgcn_s_setprio(1);                           // the waves of a unit out of step: one multiplies while another computes exponentials
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const u32x4_t a0 = kf[buffer][t * KF + 2 * n][lane], a1 = kf[buffer][t * KF + 2 * n + 1][lane];
+                const f32x4_t sk = *reinterpret_cast<const f32x4_t*>(&scales[buffer][t * (D / 2) + quarter * (D / 8) + 4 * n]);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+                    acc = mfma(a0, q[c][2 * n], acc);
+                    acc = mfma(a1, q[c][2 * n + 1], acc);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[c][4 * t + e] = n ? fmaf(acc[e], sk[e], s[c][4 * t + e]) : acc[e] * sk[e];
+                }
+            }
+        __builtin_amdgcn_s_setprio(0);
+        uint32_t unseen[CT] = {};                                // a bit a token of this lane
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            if constexpr (masked) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
+                    const bool seen = there && j >= see_from[c] && j < see_to[c];
+                    s[c][e] = seen ? s[c][e] : -INFINITY;
+                    unseen[c] |= seen ? 0u : 1u << e;
+                }
+            }
+        }
+        soften<CT, DT>(s, m, l, o);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            u32x4_t p[CT];
+            f32x4_t sv[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) sv[t] = *reinterpret_cast<const f32x4_t*>(&scales[buffer][t * (D / 2) + quarter * (D / 8) + 4 * (NB + n)]);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                float w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    w[e] = s[c][e] * sv[e / 4][e % 4];
+                    if constexpr (masked) w[e] = unseen[c] >> e & 1u ? 0.f : w[e];           // (what lies behind a sequence may be anything)
+                }
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) p[c][e / 2] = pack_bf16(w[e], w[e + 1]);
+            }
+#pragma unroll
+            for (int d = 4 * n; d < 4 * n + 4; ++d) {
+                const u32x4_t v = vf[buffer][d][lane];
+#pragma unroll
+                for (int c = 0; c < CT; ++c) o[c][d] = mfma(v, p[c], o[c][d]);
+            }
+        }
     };
 
     Walk<D> walk(a, tile.seq, head, steps.from);
@@ -540,72 +622,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_tile_kernel(AttnArgs A) 
             if (step + 2 < steps.to) load(next.base);
         }
         if (busy && step >= own.from && step < own.to) {
-            float s[CT][8];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int n = 0; n < NB; ++n) {
-                    const u32x4_t a0 = kf[buffer][t * KF + 2 * n][lane], a1 = kf[buffer][t * KF + 2 * n + 1][lane];
-                    const u32x2_t sk = *reinterpret_cast<const u32x2_t*>(&scales[buffer][t * (D / 4) + quarter * (D / 16) + 2 * n]);
-#pragma unroll
-                    for (int c = 0; c < CT; ++c) {
-                        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-                        acc = mfma(a0, q[c][2 * n], acc);
-                        acc = mfma(a1, q[c][2 * n + 1], acc);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float k = half_of(sk[e / 2], e % 2) * scale;
-                            s[c][4 * t + e] = n ? fmaf(acc[e], k, s[c][4 * t + e]) : acc[e] * k;
-                        }
-                    }
-                }
-            const bool masked = step < own.whole_from || step >= own.whole_to || !there;
-            uint32_t unseen[CT];                                     // a bit a token of this lane
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                unseen[c] = 0;
-                if (masked) {
-                    const int64_t column = mine + 16 * c + col, i = (column < columns ? column : columns - 1) / group;
-                    const int from = static_cast<int>(sight.begin(i)), to = static_cast<int>(sight.end(i));
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
-                        const bool seen = there && j >= from && j < to;
-                        s[c][e] = seen ? s[c][e] : -INFINITY;
-                        unseen[c] |= seen ? 0u : 1u << e;
-                    }
-                }
-                soften<DT>(s[c], m[c], l[c], o[c]);
-            }
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                u32x4_t p[CT];
-                float sv[8];
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const u32x2_t w = *reinterpret_cast<const u32x2_t*>(&scales[buffer][t * (D / 4) + quarter * (D / 16) + 2 * (NB + n)]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sv[4 * t + e] = half_of(w[e / 2], e % 2);
-                }
-#pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    float w[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = s[c][e] * sv[e];
-                    if (masked) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = unseen[c] >> e & 1u ? 0.f : w[e];      // (what lies behind a sequence may be anything)
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) p[c][e / 2] = pack_bf16(w[e], w[e + 1]);
-                }
-#pragma unroll
-                for (int d = 4 * n; d < 4 * n + 4; ++d) {
-                    const u32x4_t v = vf[buffer][d][lane];
-#pragma unroll
-                    for (int c = 0; c < CT; ++c) o[c][d] = mfma(v, p[c], o[c][d]);
-                }
-            }
+            if (step < own.whole_from || step >= own.whole_to || !there) multiply(step, buffer, there, std::true_type{});
+            else multiply(step, buffer, there, std::false_type{});
         }
         __syncthreads();
     }
@@ -613,13 +631,13 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_tile_kernel(AttnArgs A) 
     const bool whole = A.splits == 1;
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        const int64_t column = mine + 16 * c + col;
+        const int column = mine + 16 * c + col;
         const float all = sum_over_quarters(l[c]);
         if (column >= columns) continue;
         const bool none = all == 0.f;
         const float norm = none ? 0.f : 1.f / all;
-        const int64_t row = tile.start + column / group;
-        const int qh = head * group + static_cast<int>(column % group);
+        const int i = column / group, qh = head * group + column - i * group;
+        const int64_t row = tile.start + i;
         const int64_t pair = row * a.q_heads + qh;
         if (quarter == 0) {
             if (!whole) {
@@ -642,6 +660,15 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_tile_kernel(AttnArgs A) 
             }
         }
     }
+}
+
+template <int D>
+__device__ __forceinline__ void join_store(const AttentionArgs& a, int64_t pair, int64_t row, int d, f32x4_t sum, float all, float most) {
+    const bool none = all == 0.f;
+    const float norm = none ? 0.f : 1.f / all;
+    const u32x2_t r = {pack_bf16(sum[0] * norm, sum[1] * norm), pack_bf16(sum[2] * norm, sum[3] * norm)};     // (nothing seen: every sum is zero)
+    *reinterpret_cast<u32x2_t*>(a.out + row * a.out_stride + (pair - row * a.q_heads) * D + 4 * d) = r;
+    if (a.lse && d == 0) a.lse[pair] = none ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kLn2;
 }
 
 // The parts of a (row, query head) pair joined, a workgroup a pair: a thread a part for the weights, then D / 4 threads a part and
@@ -697,10 +724,50 @@ __global__ void __launch_bounds__(kAttnThreads) attn_join_kernel(AttnArgs A) {
     for (int p = 1; p < kAtOnce; ++p)
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += sums[p][d][e];
-    const bool none = all == 0.f;
-    const u32x2_t r = {pack_bf16(none ? 0.f : sum[0] / all, none ? 0.f : sum[1] / all), pack_bf16(none ? 0.f : sum[2] / all, none ? 0.f : sum[3] / all)};
-    *reinterpret_cast<u32x2_t*>(a.out + row * a.out_stride + (pair - row * a.q_heads) * D + 4 * d) = r;
-    if (a.lse && d == 0) a.lse[pair] = none ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kLn2;
+    join_store<D>(a, pair, row, d, sum, all, most);
+}
+
+// The same for few parts: D / 4 threads a pair, and each passes over all of them.
+constexpr int kFewParts = 8;
+template <int D>
+__global__ void __launch_bounds__(kAttnThreads) attn_join_few_kernel(AttnArgs A) {
+    constexpr int kLanes = D / 4;
+    const AttentionArgs& a = A.a;
+    const int64_t pairs = a.batch.rows * a.q_heads;
+    const int64_t pair = static_cast<int64_t>(blockIdx.x) * (kAttnThreads / kLanes) + threadIdx.x / kLanes;
+    const int d = static_cast<int>(threadIdx.x) % kLanes;
+    const int row = static_cast<int>((pair < pairs ? pair : pairs - 1) / a.q_heads);
+    bool mine = false;                                             // (a wave looks for a row together, so for its pairs' rows one after the other)
+#pragma unroll
+    for (int i = 0; i < kWave / kLanes; ++i) {
+        const bool found = kv_find_row(a.batch, __builtin_amdgcn_readlane(row, i * kLanes)).seq >= 0;
+        mine |= found && static_cast<int>(threadIdx.x) % kWave / kLanes == i;
+    }
+    if (!mine || pair >= pairs) return;
+    float m[kFewParts], l[kFewParts], most = kLowest;
+#pragma unroll
+    for (int s = 0; s < kFewParts; ++s) {
+        m[s] = kLowest;
+        l[s] = 0.f;
+        if (s < A.splits) {
+            const float* ml = A.part_ml + (s * pairs + pair) * 2;
+            m[s] = ml[0];
+            l[s] = ml[1];
+        }
+        most = fmaxf(most, m[s]);
+    }
+    float all = 0.f;
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < kFewParts; ++s) {
+        const float w = l[s] == 0.f ? 0.f : __builtin_amdgcn_exp2f(m[s] - most);
+        if (s >= A.splits || w == 0.f) continue;
+        all += l[s] * w;
+        const f32x4_t o = *reinterpret_cast<const f32x4_t*>(A.part_o + (s * pairs + pair) * D + 4 * d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = fmaf(o[e], w, sum[e]);
+    }
+    join_store<D>(a, pair, row, d, sum, all, most);
 }
 
 static int64_t column_tiles(const KvBatchArgs& b, int group, int columns) {
@@ -721,11 +788,16 @@ static int64_t column_tiles(const KvBatchArgs& b, int group, int columns) {
 #ifndef WIDE
 #define WIDE 32
 #endif
-constexpr int kTileColumns = kAttnWaves * 16 * CT1;
+#ifndef TW
+#define TW 8
+#endif
+template <int D> constexpr int kTW = D == 64 ? 4 : TW;
+template <int D> constexpr int kCT = D == 256 ? 1 : CT1;
+inline int tile_columns(int D) { return D == 64 ? kTW<64> * 16 * kCT<64> : D == 128 ? kTW<128> * 16 * kCT<128> : kTW<256> * 16 * kCT<256>; }
 AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
     const int group = q_heads / c.kv_heads;
     const bool wide = b.rows * group > static_cast<int64_t>(WIDE) * b.sequences;
-    AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? kTileColumns : kAttnColumns, 1, 0};
+    AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? tile_columns(c.head_dim) : kAttnColumns, 1, 0};
     const int64_t items = column_tiles(b, group, p.columns) * c.kv_heads;
     const int64_t steps = static_cast<int64_t>(b.table_width) * (c.page_size / kKvStep);
     int64_t splits = ((wide ? TTARGET : TARGET) + items - 1) / (items > 0 ? items : 1);
@@ -745,10 +817,12 @@ static hipError_t launch_attn(const AttnArgs& A, const AttentionPlan& p, hipStre
     const int64_t items = column_tiles(b, A.a.q_heads / A.a.cache.kv_heads, p.columns) * A.a.cache.kv_heads;
     const dim3 grid(static_cast<unsigned>(items), static_cast<unsigned>(A.splits));
     if (p.columns == kAttnColumns) attn_kernel<D><<<grid, kAttnThreads, 0, s>>>(A);
-    else attn_tile_kernel<D, CT1><<<grid, kAttnThreads, 0, s>>>(A);
+    else attn_tile_kernel<D, kCT<D>, kTW<D>><<<grid, kTW<D> * kWave, 0, s>>>(A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits == 1) return e;
-    attn_join_kernel<D><<<dim3(static_cast<unsigned>(b.rows * A.a.q_heads)), kAttnThreads, 0, s>>>(A);
+    const int64_t pairs = b.rows * A.a.q_heads, at_once = kAttnThreads / (D / 4);
+    if (A.splits <= kFewParts) attn_join_few_kernel<D><<<dim3(static_cast<unsigned>((pairs + at_once - 1) / at_once)), kAttnThreads, 0, s>>>(A);
+    else attn_join_kernel<D><<<dim3(static_cast<unsigned>(pairs)), kAttnThreads, 0, s>>>(A);
     return hipGetLastError();
 }
 
