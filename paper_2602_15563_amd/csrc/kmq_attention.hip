@@ -61,8 +61,6 @@ __device__ __forceinline__ u32x4_t even_odd(u32x4_t v) {
     return u32x4_t{__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u),
                    __builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u)};
 }
-__device__ __forceinline__ float half_of(uint32_t v, int upper) { return __uint_as_float(upper ? v & 0xFFFF0000u : v << 16); }
-
 // N dwords (N * 4 a power of two, or a multiple of 16 bytes) from an address aligned to their size, at most 16 bytes a load.
 template <int N>
 __device__ __forceinline__ void load_words(uint32_t* to, const uint8_t* from) {
@@ -88,10 +86,6 @@ struct KWords {
 };
 __device__ __forceinline__ f32x4_t mfma(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    const bf16x2_t v = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
-    return __builtin_bit_cast(uint32_t, v);
 }
 // (the maximum of two, a NaN carried by neither: it reaches the output through exp)
 __device__ __forceinline__ float max_over_quarters(float v) {
@@ -352,7 +346,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
                     acc = mfma(decode8_table(table, w), q[2 * n + j], acc);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[e] = fmaf(acc[e], half_of(now.sc[t][n * 2 + e / 2], e % 2), sum[e]);
+                for (int e = 0; e < 4; ++e) sum[e] = fmaf(acc[e], kv_half(now.sc[t][n * 2 + e / 2], e % 2), sum[e]);
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[0][4 * t + e] = sum[e] * scale;
@@ -361,7 +355,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sv[n][e] = half_of(now.sc[e / 4][(NB + n) * 2 + e % 4 / 2], e % 2);
+            for (int e = 0; e < 8; ++e) sv[n][e] = kv_half(now.sc[e / 4][(NB + n) * 2 + e % 4 / 2], e % 2);
         if (step < steps.whole_from || step >= steps.whole_to || !at.there) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -377,7 +371,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
         for (int n = 0; n < NB; ++n) {
             u32x4_t p;
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) p[e / 2] = pack_bf16(s[0][e] * sv[n][e], s[0][e + 1] * sv[n][e + 1]);
+            for (int e = 0; e < 8; e += 2) p[e / 2] = kv_pack2(s[0][e] * sv[n][e], s[0][e + 1] * sv[n][e + 1]);
 #pragma unroll
             for (int j = 2 * n; j < 2 * n + 2; ++j) {
                 const u32x4_t x = decode8(cv, vw[0][j]), y = decode8(cv, vw[1][j]);
@@ -433,8 +427,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
                 for (int e = 0; e < 4; ++e) sum[e] += part[w][col][d + e];
             if (!live) continue;
             if (whole) {
-                const u32x2_t r = {pack_bf16(none ? 0.f : sum[0] * norm, none ? 0.f : sum[1] * norm),
-                                   pack_bf16(none ? 0.f : sum[2] * norm, none ? 0.f : sum[3] * norm)};
+                const u32x2_t r = {kv_pack2(none ? 0.f : sum[0] * norm, none ? 0.f : sum[1] * norm),
+                                   kv_pack2(none ? 0.f : sum[2] * norm, none ? 0.f : sum[3] * norm)};
                 *reinterpret_cast<u32x2_t*>(a.out + row * a.out_stride + static_cast<int64_t>(qh) * D + c0 + d) = r;
             } else {
                 *reinterpret_cast<f32x4_t*>(A.part_o + (static_cast<int64_t>(blockIdx.y) * b.rows * a.q_heads + pair) * D + c0 + d) = sum;
@@ -540,8 +534,8 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
             vf[buffer][wave][lane] = u32x4_t{r[0], r[1], r[2], r[3]};
         }
         if (tid < D / 2) {
-            scales[buffer][2 * tid] = half_of(sw, 0) * sf;
-            scales[buffer][2 * tid + 1] = half_of(sw, 1) * sf;
+            scales[buffer][2 * tid] = kv_half(sw, 0) * sf;
+            scales[buffer][2 * tid + 1] = kv_half(sw, 1) * sf;
         }
     };
     const auto multiply = [&](int step, int buffer, bool there, auto masked) {
@@ -592,7 +586,7 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
                     if constexpr (masked) w[e] = unseen[c] >> e & 1u ? 0.f : w[e];           // (what lies behind a sequence may be anything)
                 }
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) p[c][e / 2] = pack_bf16(w[e], w[e + 1]);
+                for (int e = 0; e < 8; e += 2) p[c][e / 2] = kv_pack2(w[e], w[e + 1]);
             }
 #pragma unroll
             for (int d = 4 * n; d < 4 * n + 4; ++d) {
@@ -653,7 +647,7 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
             const f32x4_t v = o[c][d];
             const int at_d = 16 * d + 4 * quarter;
             if (whole) {
-                const u32x2_t r = {pack_bf16(none ? 0.f : v[0] * norm, none ? 0.f : v[1] * norm), pack_bf16(none ? 0.f : v[2] * norm, none ? 0.f : v[3] * norm)};
+                const u32x2_t r = {kv_pack2(none ? 0.f : v[0] * norm, none ? 0.f : v[1] * norm), kv_pack2(none ? 0.f : v[2] * norm, none ? 0.f : v[3] * norm)};
                 *reinterpret_cast<u32x2_t*>(a.out + row * a.out_stride + static_cast<int64_t>(qh) * D + at_d) = r;
             } else if (!none) {
                 *reinterpret_cast<f32x4_t*>(A.part_o + (static_cast<int64_t>(blockIdx.y) * b.rows * a.q_heads + pair) * D + at_d) = v;
@@ -666,7 +660,7 @@ template <int D>
 __device__ __forceinline__ void join_store(const AttentionArgs& a, int64_t pair, int64_t row, int d, f32x4_t sum, float all, float most) {
     const bool none = all == 0.f;
     const float norm = none ? 0.f : 1.f / all;
-    const u32x2_t r = {pack_bf16(sum[0] * norm, sum[1] * norm), pack_bf16(sum[2] * norm, sum[3] * norm)};     // (nothing seen: every sum is zero)
+    const u32x2_t r = {kv_pack2(sum[0] * norm, sum[1] * norm), kv_pack2(sum[2] * norm, sum[3] * norm)};     // (nothing seen: every sum is zero)
     *reinterpret_cast<u32x2_t*>(a.out + row * a.out_stride + (pair - row * a.q_heads) * D + 4 * d) = r;
     if (a.lse && d == 0) a.lse[pair] = none ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kLn2;
 }

@@ -6,202 +6,412 @@
 //     y_left = n_left cos a_i - n_right sin a_i,   y_right = n_right cos a_i + n_left sin a_i
 //     cache:  scale = max |y| over 64 elements,  index = number of boundaries b_j with y > b_j * scale
 //
-// All of it is computed in 64 bits, rounded to 32 and then to bf16: a far position times a frequency needs them, and the
-// index of a key is decided by a comparison, so that with them it is the definition's own and the oracle's.
-// (The vector units multiply and add 64-bit floats at the rate of 32-bit ones.)
+// The turning is computed in 64 bits, rounded to 32 and then to bf16: a far position times a frequency needs them, and the
+// index of a key is decided by a comparison, so that with them it is the definition's own and the oracle's.  (The vector units
+// multiply and add 64-bit floats at the rate of 32-bit ones.)  With r = 1 / sqrt(..) an element is
+//     y_e = r * (x_e A_e + x_partner B_e),   A_e = gain_e cos,  B_e = +-gain_partner sin,
+// and A and B are the same for all query heads of a row, and for all its key heads: three operations an element.
+#include <type_traits>
+
 #include "kmq_kv.h"
 
 namespace kmq {
 
-constexpr int kHeadThreads = 256;
-constexpr int kMaxRotaryPairs = 256;
+constexpr int kHeadThreads = 256, kHeadWaves = kHeadThreads / kWave;
+constexpr int kGroupRows = 4;      // tokens whose V indices share a dword of the cache
 
-// The boundary between two centroids, in 32 bits.
-__device__ __forceinline__ double kv_boundary(const uint16_t* codebook, int i) {
-    return static_cast<double>((bf16_to_f32(codebook[i]) + bf16_to_f32(codebook[i + 1])) * 0.5f);
+template <int CTRL>
+__device__ __forceinline__ double dpp_move64(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, 0xF, 0xF, true));
+    const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, 0xF, 0xF, true));
+    return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
 }
-
-// Index of x (bf16): boundaries that lie below it once they are scaled.  A boundary of at most 24 bits times a scale of 8
-// is exact in 64 bits.  Four comparisons: the boundaries ascend.
-__device__ __forceinline__ uint32_t kv_index(const double* boundary, double scale, double x) {
-    uint32_t i = 0;
-#pragma unroll
-    for (int half = 8; half > 0; half >>= 1) i += x > boundary[i + half - 1] * scale ? half : 0;
-    return i;
-}
-
-// LANES lanes hold a head, 8 elements each; a head never crosses a wave.
+// The sum over groups of LANES lanes, in all of them.
 template <int LANES>
-__global__ void __launch_bounds__(kHeadThreads) heads_kernel(HeadsArgs a, KvCacheArgs c, KvBatchArgs b, bool cached, int heads_per_group) {
-    __shared__ double turn[2][kMaxRotaryPairs];
-    __shared__ double boundary[2][kKvCentroids - 1];
-    const int64_t row = blockIdx.x;
-    const int tid = threadIdx.x;
-    const KvRow at = cached ? kv_find_row(b, row) : KvRow{0, 0};
-    if (at.seq < 0) return;                               // (the same for all waves of the workgroup)
-    if (a.rotary_dim) {
-        const double pos = a.positions ? static_cast<double>(a.positions[row]) : static_cast<double>(at.pos);
-        for (int i = tid; i < a.rotary_dim / 2; i += kHeadThreads) sincos(pos * static_cast<double>(a.inv_freq[i]), &turn[1][i], &turn[0][i]);
+__device__ __forceinline__ double sum_over(double v) {
+    v += dpp_move64<0xB1>(v);                             // quad_perm [1,0,3,2]
+    v += dpp_move64<0x4E>(v);                             // quad_perm [2,3,0,1]
+    v += dpp_move64<0x141>(v);                            // row_half_mirror
+    if (LANES >= 16) v += dpp_move64<0x140>(v);           // row_mirror
+    if (LANES >= 32) v += __shfl_xor(v, 16);
+    if (LANES >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+// 1 / sqrt(v): the unit's estimate and two Newton steps, each of which doubles its good bits.
+__device__ __forceinline__ double inverse_root(double v) {
+    double y = __builtin_amdgcn_rsq(v);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) y *= fma(-0.5 * v * y, y, 1.5);
+    return y;
+}
+// The largest of 8 neighbouring lanes' patterns, in all of them.
+__device__ __forceinline__ uint32_t max_over_8(uint32_t v) {
+    const auto other = [](uint32_t x, auto ctrl) { return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, 0xF, 0xF, true)); };
+    const uint32_t a = other(v, std::integral_constant<int, 0xB1>{});   // quad_perm [1,0,3,2]
+    v = a > v ? a : v;
+    const uint32_t b = other(v, std::integral_constant<int, 0x4E>{});   // quad_perm [2,3,0,1]
+    v = b > v ? b : v;
+    const uint32_t c = other(v, std::integral_constant<int, 0x141>{});  // row_half_mirror
+    return c > v ? c : v;
+}
+
+// What turns the elements of a lane, the same for every head of a kind: y = r * (x * own + partner * far).
+struct Factors {
+    double own[8], far[8];
+};
+__device__ __forceinline__ Factors make_factors(const HeadsArgs& a, const uint16_t* gain, const double* cosine, const double* sine, int d0, bool live) {
+    Factors f;
+    const int half = a.rotary_dim / 2;
+    const bool turned = live && d0 < a.rotary_dim;
+    const int other = a.interleaved ? d0 : d0 < half ? d0 + half : d0 - half, i0 = a.interleaved ? d0 / 2 : d0 < half ? d0 : d0 - half;
+    u32x4_t g = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, go = g;
+    if (gain && live) g = *reinterpret_cast<const u32x4_t*>(gain + d0);
+    if (gain && turned) go = *reinterpret_cast<const u32x4_t*>(gain + other);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int i = a.interleaved ? i0 + e / 2 : i0 + e;
+        const bool left = a.interleaved ? e % 2 == 0 : d0 < half;
+        const double c = turned ? cosine[i] : 1.0, s = turned ? sine[i] : 0.0;
+        const float partner = a.interleaved ? kv_half(go[(e ^ 1) / 2], (e ^ 1) % 2) : kv_half(go[e / 2], e % 2);
+        f.own[e] = static_cast<double>(kv_half(g[e / 2], e % 2)) * c;
+        f.far[e] = static_cast<double>(partner) * (left ? -s : s);
     }
-    if (cached && tid < 2 * (kKvCentroids - 1)) {
-        const int kv = tid / (kKvCentroids - 1), i = tid % (kKvCentroids - 1);
-        boundary[kv][i] = kv_boundary(c.codebooks + kv * kKvCentroids, i);
+    return f;
+}
+
+// One head's elements of a lane, turned.  `far` are its partners in the split form; `mean` is 1 / D.
+template <int LANES>
+__device__ __forceinline__ u32x4_t turn_head(const HeadsArgs& a, const Factors& f, u32x4_t own, u32x4_t far, bool turned, double mean) {
+    if (a.interleaved && turned) far = u32x4_t{own[0] >> 16 | own[0] << 16, own[1] >> 16 | own[1] << 16, own[2] >> 16 | own[2] << 16, own[3] >> 16 | own[3] << 16};
+    double r = 1.0;
+    if (a.norm) {
+        double ss = 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const double x = kv_half(own[e / 2], e % 2);
+            ss = fma(x, x, ss);
+        }
+        r = inverse_root(fma(sum_over<LANES>(ss), mean, static_cast<double>(a.eps)));
+    }
+    u32x4_t out;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        float y[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const double x = kv_half(own[e / 2], k), p = kv_half(far[e / 2], k);
+            y[k] = static_cast<float>(r * fma(x, f.own[e + k], p * f.far[e + k]));
+            asm("" : "+v"(y[k]));                         // (else the compiler makes one rounding of the two, which are specified)
+        }
+        out[e / 2] = kv_pack2(y[0], y[1]);
+    }
+    return out;
+}
+
+// A boundary's place among bf16 values once it is scaled: x > b * s exactly where x > threshold.  The product is rounded to
+// nearest; where it was rounded up to a value that x may have, one step down.
+__device__ __forceinline__ float kv_threshold(float b, float s) {
+    const double exact = static_cast<double>(b) * static_cast<double>(s);      // 24 and 8 bits
+    float p = static_cast<float>(exact);
+    if (static_cast<double>(p) > exact) {
+        const uint32_t u = __float_as_uint(p);
+        p = p == 0.f ? -__uint_as_float(1u) : __uint_as_float(p > 0.f ? u - 1u : u + 1u);
+    }
+    return p;
+}
+
+// Eight elements of a block of 64 (8 neighbouring lanes) -> their indices in the nibbles of a dword, and the block's scale.
+// `place`: this wave's thresholds in shared memory, 16 of each of its 8 blocks.  Four comparisons an element, the boundaries
+// ascending: the first two against registers, the others against shared memory.
+__device__ __forceinline__ uint32_t quantise8(u32x4_t x, const float* boundary, float* place, uint32_t& scale) {
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), sub = lane & 7;
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t l = x[e] & 0x7FFFu, h = x[e] >> 16 & 0x7FFFu, m = l > h ? l : h;
+        top = m > top ? m : top;
+    }
+    top = max_over_8(top);
+    scale = top;
+    const float s = top ? bf16_to_f32(top) : 1.f;
+    float* mine = place + lane / 8 * 16;
+    mine[2 * sub] = kv_threshold(boundary[2 * sub], s);
+    mine[2 * sub + 1] = kv_threshold(boundary[2 * sub + 1], s);               // (the sixteenth is never looked at)
+    __builtin_amdgcn_wave_barrier();
+    const float t3 = mine[3], t7 = mine[7], t11 = mine[11];
+    uint32_t word = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float v = kv_half(x[e / 2], e % 2);
+        const bool b3 = v > t7, b2 = v > (b3 ? t11 : t3);
+        uint32_t i = (b3 ? 8u : 0u) + (b2 ? 4u : 0u);
+        i += v > mine[i + 1] ? 2u : 0u;
+        i += v > mine[i] ? 1u : 0u;
+        word |= i << (4 * e);
+    }
+    __builtin_amdgcn_wave_barrier();
+    return word;
+}
+
+// Where a row's token goes: the first tile of its page's heads, and its place in the tile.
+struct Target {
+    uint8_t* page_tile;    // tile of head 0; nullptr: not in the cache
+    int token;
+};
+__device__ __forceinline__ Target target_of(const KvCacheArgs& c, const KvBatchArgs& b, int D, KvRow r) {
+    return {kv_tile(c, b, D, r, 0), static_cast<int>(r.pos & (kKvTile - 1))};
+}
+
+__device__ __forceinline__ void store_k(uint8_t* tile, int D, int t, int d0, uint32_t word, uint32_t scale) {
+    *reinterpret_cast<uint32_t*>(tile + kv_k_dword(D, t, d0)) = word;
+    if (d0 % KMQ_BLOCK == 0) *reinterpret_cast<uint16_t*>(tile + kv_scale(D, t, 0, d0)) = static_cast<uint16_t>(scale);
+}
+// The four bytes of V that a lane stores for a token: elements d and d + 16 for four d, from its own dword and that of the lane which
+// holds the other 16.  Returned with byte e for the e-th of the four d.
+__device__ __forceinline__ uint32_t v_bytes(uint32_t word, int d0) {
+    const uint32_t pair = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(word), 0x4E, 0xF, 0xF, true));   // two lanes on, or back
+    const bool upper = d0 & 16;                           // this lane stores the later four of the pair's eight
+    const uint32_t lo = upper ? pair >> 16 : word & 0xFFFFu, hi = upper ? word >> 16 : pair & 0xFFFFu;
+    // nibbles spread to bytes: 0x4321 -> 0x04030201
+    const auto spread = [](uint32_t n) {
+        n = (n | n << 8) & 0x00FF00FFu;
+        return (n | n << 4) & 0x0F0F0F0Fu;
+    };
+    return spread(lo) | spread(hi) << 4;
+}
+__device__ __forceinline__ int v_first(int d0) { return (d0 & ~16) + (d0 & 16 ? 4 : 0); }
+
+// LANES lanes hold a head, 8 elements each; a head never crosses a wave.  ROWS = 1: a workgroup takes a row, or with few rows a
+// part of its heads.  ROWS = 4 (cached): the rows of four tokens that share V's dwords, of one sequence.
+template <int LANES, int ROWS>
+__global__ void __launch_bounds__(kHeadThreads) heads_kernel(HeadsArgs a, KvCacheArgs c, KvBatchArgs b, bool cached, int units_per_group) {
+    constexpr int kHeads = kWave / LANES;                 // heads of a unit: what a wave takes at once
+    constexpr int kPairs = LANES * 4;     // of a head of LANES * 8 elements
+    __shared__ double cosine[ROWS][kPairs], sine[ROWS][kPairs];
+    __shared__ float boundary[2][kKvCentroids], threshold[kHeadWaves][8 * 16];
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int D = a.head_dim;
+
+    // the rows of this workgroup: first .. first + 3, those in `have`
+    int64_t first;
+    uint32_t have = 1;
+    KvRow at = {0, 0};                                    // of row `first` (which need not be a row: a group starts at a multiple of four tokens)
+    if constexpr (ROWS == 1) {
+        first = blockIdx.x;
+        if (cached) at = kv_find_row(b, first);
+        if (at.seq < 0) return;                           // (the same for the whole workgroup)
+    } else {
+        const KvGroup g = kv_find_group(b, static_cast<int>(blockIdx.x));
+        if (g.seq < 0) return;
+        first = g.row;
+        have = g.have;
+        at = {g.seq, g.pos};
+    }
+    const int pairs = a.rotary_dim / 2;
+    if (pairs) {
+        for (int i = tid; i < ROWS * pairs; i += kHeadThreads) {
+            const int r = ROWS == 1 ? 0 : i / pairs, p = i - r * pairs;
+            if (!(have >> r & 1u)) continue;
+            const double pos = a.positions ? static_cast<double>(a.positions[first + r]) : static_cast<double>(at.pos + r);
+            sincos(pos * static_cast<double>(a.inv_freq[p]), &sine[r][p], &cosine[r][p]);
+        }
+    }
+    if (cached && tid < 2 * kKvCentroids) {
+        const int kv = tid / kKvCentroids, i = tid % kKvCentroids;
+        const uint16_t* book = c.codebooks + kv * kKvCentroids;
+        boundary[kv][i] = i + 1 < kKvCentroids ? (bf16_to_f32(book[i]) + bf16_to_f32(book[i + 1])) * 0.5f : 0.f;
     }
     __syncthreads();
 
-    const int sub = tid % LANES, d0 = sub * 8;
-    const int D = a.head_dim, half = a.rotary_dim / 2;
-    const int total = a.q_heads + a.k_heads + a.v_heads;
-    const int first = blockIdx.y * heads_per_group;
-    const int last = first + heads_per_group < total ? first + heads_per_group : total;
-    for (int base = first; base < last; base += kHeadThreads / LANES) {
-        const int h = base + tid / LANES;
-        const bool live = h < last && d0 < D;
-        const int kind = h < a.q_heads ? 0 : h < a.q_heads + a.k_heads ? 1 : 2;
-        const int hh = h - (kind == 0 ? 0 : kind == 1 ? a.q_heads : a.q_heads + a.k_heads);
-        const uint16_t* src = kind == 0 ? a.q + row * a.q_stride : kind == 1 ? a.k + row * a.k_stride : a.v + row * a.v_stride;
-        src += static_cast<int64_t>(hh) * D;
-        const bool turned = live && kind < 2 && d0 < a.rotary_dim;
-        const int other = a.interleaved ? d0 : d0 < half ? d0 + half : d0 - half;
-        u32x4_t own = {0, 0, 0, 0}, far = {0, 0, 0, 0};
-        if (live) own = *reinterpret_cast<const u32x4_t*>(src + d0);
-        if (turned && !a.interleaved) far = *reinterpret_cast<const u32x4_t*>(src + other);
-
-        if (kind < 2 && (a.norm || a.rotary_dim)) {
-            double x[8], r = 1.0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = bf16_to_f32(own[e / 2] >> (e % 2 * 16) & 0xFFFFu);
-            if (a.norm) {
-                double ss = 0.0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ss = fma(x[e], x[e], ss);
-#pragma unroll
-                for (int m = 1; m < LANES; m <<= 1) ss += __shfl_xor(ss, m);
-                r = 1.0 / sqrt(ss / D + static_cast<double>(a.eps));
+    Target to = {nullptr, 0};
+    if (cached) to = target_of(c, b, D, at);
+    const int64_t head_bytes = cached ? static_cast<int64_t>(c.page_size / kKvTile) * kv_tile_bytes(D) : 0;
+    const int sub = lane % LANES, d0 = sub * 8;
+    const bool inside = d0 < D;
+    const int half = a.rotary_dim / 2;
+    const bool split = !a.interleaved && inside && d0 < a.rotary_dim;
+    const int other = d0 < half ? d0 + half : d0 - half;
+    const bool turns = a.norm || a.rotary_dim;
+    const double mean = 1.0 / D;
+    // units: query heads of every row, key heads of every row, then values, of all rows at once
+    const int nq = (a.q_heads + kHeads - 1) / kHeads, nk = (a.k_heads + kHeads - 1) / kHeads, nv = (a.v_heads + kHeads - 1) / kHeads;
+    const int qk_units = ROWS * (nq + nk), units = qk_units + nv;
+    const int begin = static_cast<int>(blockIdx.y) * units_per_group, end = begin + units_per_group < units ? begin + units_per_group : units;
+    Factors f;
+    int factors_of = -1;                                  // the row and kind that f belongs to
+    for (int u = begin + wave; u < end; u += kHeadWaves) {
+        if (u < qk_units) {
+            const int r = ROWS == 1 ? 0 : u / (nq + nk), in_row = u - r * (nq + nk);
+            const int kind = in_row < nq ? 0 : 1;
+            if (!(have >> r & 1u)) continue;
+            const int h = (kind ? in_row - nq : in_row) * kHeads + lane / LANES;
+            const bool live = inside && h < (kind ? a.k_heads : a.q_heads);
+            const int64_t row = first + r;
+            const uint16_t* src = (kind ? a.k + row * a.k_stride : a.q + row * a.q_stride) + static_cast<int64_t>(h) * D;
+            u32x4_t own = {0, 0, 0, 0}, far = {0, 0, 0, 0};
+            if (live) own = *reinterpret_cast<const u32x4_t*>(src + d0);
+            if (turns) {
+                if (live && split) far = *reinterpret_cast<const u32x4_t*>(src + other);
+                if (factors_of != 2 * r + kind) {
+                    factors_of = 2 * r + kind;
+                    f = make_factors(a, !a.norm ? nullptr : kind ? a.k_gain : a.q_gain, cosine[r], sine[r], d0, inside);
+                }
+                own = turn_head<LANES>(a, f, own, far, inside && d0 < a.rotary_dim, mean);
             }
-            const uint16_t* gain = !a.norm ? nullptr : kind == 0 ? a.q_gain : a.k_gain;
-            u32x4_t gown = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, gfar = gown;
-            if (gain && live) gown = *reinterpret_cast<const u32x4_t*>(gain + d0);
-            if (gain && turned && !a.interleaved) gfar = *reinterpret_cast<const u32x4_t*>(gain + other);
+            uint16_t* out = kind ? a.k_out : a.q_out;
+            if (out) {
+                if (live) *reinterpret_cast<u32x4_t*>(out + row * (kind ? a.k_out_stride : a.q_out_stride) + static_cast<int64_t>(h) * D + d0) = own;
+                continue;
+            }
+            uint32_t scale;
+            const uint32_t word = quantise8(own, boundary[0], threshold[wave], scale);
+            if (live && to.page_tile) store_k(to.page_tile + h * head_bytes, D, to.token + r, d0, word, scale);
+        } else {
+            const int h = (u - qk_units) * kHeads + lane / LANES;
+            const bool live = inside && h < a.v_heads;
+            uint32_t bytes[ROWS], scale[ROWS];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= r * static_cast<double>(bf16_to_f32(gown[e / 2] >> (e % 2 * 16) & 0xFFFFu));
-            if (turned) {
-                if (a.interleaved) {
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const double co = turn[0][(d0 + e) / 2], si = turn[1][(d0 + e) / 2], l = x[e], t = x[e + 1];
-                        x[e] = l * co - t * si;
-                        x[e + 1] = t * co + l * si;
-                    }
-                } else {
-                    const int i0 = d0 < half ? d0 : d0 - half;
-                    const double sign = d0 < half ? -1.0 : 1.0;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const double f = static_cast<double>(bf16_to_f32(far[e / 2] >> (e % 2 * 16) & 0xFFFFu)) *
-                                         (r * static_cast<double>(bf16_to_f32(gfar[e / 2] >> (e % 2 * 16) & 0xFFFFu)));
-                        x[e] = x[e] * turn[0][i0 + e] + sign * (f * turn[1][i0 + e]);
-                    }
+            for (int r = 0; r < ROWS; ++r) {
+                u32x4_t x = {0, 0, 0, 0};
+                if (live && (have >> r & 1u)) x = *reinterpret_cast<const u32x4_t*>(a.v + (first + r) * a.v_stride + static_cast<int64_t>(h) * D + d0);
+                bytes[r] = v_bytes(quantise8(x, boundary[1], threshold[wave], scale[r]), d0);
+            }
+            if (!live || !to.page_tile) continue;
+            uint8_t* tile = to.page_tile + h * head_bytes;
+            const int v0 = kv_v_byte(D, to.token, v_first(d0)), step = D / 8;
+            bool whole = false;
+            if constexpr (ROWS == 4) {                    // whole dwords: bytes of four tokens, for each of four elements
+                whole = have == 15u;
+                if (whole) {
+                    const uint32_t t01 = __builtin_amdgcn_perm(bytes[1], bytes[0], 0x05010400u), t01h = __builtin_amdgcn_perm(bytes[1], bytes[0], 0x07030602u);
+                    const uint32_t t23 = __builtin_amdgcn_perm(bytes[3], bytes[2], 0x05010400u), t23h = __builtin_amdgcn_perm(bytes[3], bytes[2], 0x07030602u);
+                    *reinterpret_cast<uint32_t*>(tile + v0) = __builtin_amdgcn_perm(t23, t01, 0x05040100u);
+                    *reinterpret_cast<uint32_t*>(tile + v0 + step) = __builtin_amdgcn_perm(t23, t01, 0x07060302u);
+                    *reinterpret_cast<uint32_t*>(tile + v0 + 2 * step) = __builtin_amdgcn_perm(t23h, t01h, 0x05040100u);
+                    *reinterpret_cast<uint32_t*>(tile + v0 + 3 * step) = __builtin_amdgcn_perm(t23h, t01h, 0x07060302u);
                 }
             }
+            if (!whole) {
 #pragma unroll
-            for (int e = 0; e < 8; e += 2)
-                own[e / 2] = f32_to_bf16(static_cast<float>(x[e])) | static_cast<uint32_t>(f32_to_bf16(static_cast<float>(x[e + 1]))) << 16;
-        }
-
-        if (kind == 0 || (kind == 1 && a.k_out)) {
-            uint16_t* dst = kind == 0 ? a.q_out + row * a.q_out_stride : a.k_out + row * a.k_out_stride;
-            if (live) *reinterpret_cast<u32x4_t*>(dst + static_cast<int64_t>(hh) * D + d0) = own;
-            continue;
-        }
-        // keys and values of the cache: 8 lanes hold a block of 64 elements (D is a multiple of it here)
-        uint32_t top = 0;
+                for (int r = 0; r < ROWS; ++r)
+                    if (have >> r & 1u) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t m = own[e / 2] >> (e % 2 * 16) & 0x7FFFu;
-            top = m > top ? m : top;
-        }
+                        for (int e = 0; e < 4; ++e) tile[v0 + e * step + r] = static_cast<uint8_t>(bytes[r] >> (8 * e));
+                    }
+            }
+            if (d0 % KMQ_BLOCK == 0) {
 #pragma unroll
-        for (int m = 1; m < 8; m <<= 1) {
-            const uint32_t o = __shfl_xor(top, m);
-            top = o > top ? o : top;
+                for (int r = 0; r < ROWS; ++r)
+                    if (have >> r & 1u) *reinterpret_cast<uint16_t*>(tile + kv_scale(D, to.token + r, 1, d0)) = static_cast<uint16_t>(scale[r]);
+            }
         }
-        const double scale = top ? static_cast<double>(bf16_to_f32(top)) : 1.0;
-        uint32_t word = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            word |= kv_index(boundary[kind - 1], scale, bf16_to_f32(own[e / 2] >> (e % 2 * 16) & 0xFFFFu)) << (4 * e);
-        const uint32_t pair = __shfl_xor(word, 2);        // the elements 16 further on, or back
-        uint8_t* tile = live ? kv_tile(c, b, D, at, hh) : nullptr;
-        if (!tile) continue;
-        const int t = static_cast<int>(at.pos % kKvTile);
-        if (kind == 1) {
-            *reinterpret_cast<uint32_t*>(tile + kv_k_dword(D, t, d0)) = word;
-        } else {
-            const bool upper = d0 & 16;                   // this lane stores bytes 4..7 of the pair's eight
-            const uint32_t lo = (upper ? pair >> 16 : word), hi = (upper ? word >> 16 : pair);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                tile[kv_v_byte(D, t, (d0 & ~16) + (upper ? 4 : 0) + e)] = static_cast<uint8_t>((lo >> (4 * e) & 15u) | (hi >> (4 * e) & 15u) << 4);
-        }
-        if (sub % 8 == 0) *reinterpret_cast<uint16_t*>(tile + kv_scale(D, t, kind - 1, d0)) = static_cast<uint16_t>(top);
     }
 }
 
 // Rows of the cache as bf16: one rounding of centroid * scale; zeros where the page table has no page.
+// A thread takes eight elements of a head, of one row or of four tokens that share V's dwords.
+template <int ROWS>
 __global__ void __launch_bounds__(kHeadThreads) kv_read_kernel(KvCacheArgs c, KvBatchArgs b, uint16_t* k, int64_t k_stride, uint16_t* v, int64_t v_stride) {
     __shared__ float centroid[2 * kKvCentroids];
-    const int64_t row = blockIdx.x;
-    const int tid = threadIdx.x, D = c.head_dim;
+    const int tid = static_cast<int>(threadIdx.x), D = c.head_dim;
     if (tid < 2 * kKvCentroids) centroid[tid] = bf16_to_f32(c.codebooks[tid]);
-    const KvRow at = kv_find_row(b, row);
+    int64_t first;
+    uint32_t have = 1;
+    KvRow at;
+    if constexpr (ROWS == 1) {
+        first = blockIdx.x;
+        at = kv_find_row(b, first);
+    } else {
+        const KvGroup g = kv_find_group(b, static_cast<int>(blockIdx.x));
+        first = g.row;
+        have = g.have;
+        at = {g.seq, g.pos};
+    }
     if (at.seq < 0) return;
     __syncthreads();
-    const int per_head = D / 8, t = static_cast<int>(((at.pos % kKvTile) + kKvTile) % kKvTile);
-    for (int i = tid; i < 2 * c.kv_heads * per_head; i += kHeadThreads) {
-        const int kv = i / (c.kv_heads * per_head), rest = i % (c.kv_heads * per_head), h = rest / per_head, d0 = rest % per_head * 8;
-        const uint8_t* tile = kv_tile(c, b, D, at, h);
-        u32x4_t out = {0, 0, 0, 0};
-        if (tile) {
-            uint32_t word = 0;
-            if (kv == 0) {
-                word = *reinterpret_cast<const uint32_t*>(tile + kv_k_dword(D, t, d0));
-            } else {
+    const Target from = target_of(c, b, D, at);
+    const int64_t head_bytes = static_cast<int64_t>(c.page_size / kKvTile) * kv_tile_bytes(D);
+    const int per_head = D / 8, all = c.kv_heads * per_head;
+    for (int i = tid + static_cast<int>(blockIdx.y) * kHeadThreads; i < 2 * all; i += kHeadThreads * static_cast<int>(gridDim.y)) {
+        const int kv = i >= all, rest = i - kv * all, h = rest / per_head, d0 = (rest - h * per_head) * 8;
+        const uint8_t* tile = from.page_tile + h * head_bytes;
+        uint32_t word[ROWS] = {}, scale[ROWS] = {};
+        if (from.page_tile) {
+            if (kv) {
+                const uint8_t* at_v = tile + kv_v_byte(D, from.token, d0 & ~16);
+                const int shift = d0 & 16 ? 4 : 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    word |= (static_cast<uint32_t>(tile[kv_v_byte(D, t, (d0 & ~16) + e)]) >> (d0 & 16 ? 4 : 0) & 15u) << (4 * e);
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (ROWS == 1) {
+                        word[0] |= (static_cast<uint32_t>(at_v[e * (D / 8)]) >> shift & 15u) << (4 * e);
+                    } else {
+                        const uint32_t w = *reinterpret_cast<const uint32_t*>(at_v + e * (D / 8)) >> shift;
+#pragma unroll
+                        for (int r = 0; r < ROWS; ++r) word[r] |= (w >> (8 * r) & 15u) << (4 * e);
+                    }
+                }
             }
-            const float scale = bf16_to_f32(*reinterpret_cast<const uint16_t*>(tile + kv_scale(D, t, kv, d0)));
 #pragma unroll
-            for (int e = 0; e < 8; e += 2)
-                out[e / 2] = f32_to_bf16(centroid[kv * kKvCentroids + (word >> (4 * e) & 15u)] * scale) |
-                             static_cast<uint32_t>(f32_to_bf16(centroid[kv * kKvCentroids + (word >> (4 * e + 4) & 15u)] * scale)) << 16;
+            for (int r = 0; r < ROWS; ++r) {
+                if (!kv) word[r] = *reinterpret_cast<const uint32_t*>(tile + kv_k_dword(D, from.token + r, d0));
+                scale[r] = *reinterpret_cast<const uint16_t*>(tile + kv_scale(D, from.token + r, kv, d0));
+            }
         }
-        uint16_t* dst = kv ? v + row * v_stride : k + row * k_stride;
-        *reinterpret_cast<u32x4_t*>(dst + static_cast<int64_t>(h) * D + d0) = out;
+        uint16_t* out = (kv ? v + first * v_stride : k + first * k_stride) + static_cast<int64_t>(h) * D + d0;
+        const float* book = centroid + kv * kKvCentroids;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            if (!(have >> r & 1u)) continue;
+            const float s = bf16_to_f32(scale[r]);
+            u32x4_t y = {0, 0, 0, 0};
+            if (from.page_tile) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) y[e / 2] = kv_pack2(book[word[r] >> (4 * e) & 15u] * s, book[word[r] >> (4 * e + 4) & 15u] * s);
+            }
+            *reinterpret_cast<u32x4_t*>(out + r * (kv ? v_stride : k_stride)) = y;
+        }
     }
 }
+
+// Rows in groups of four tokens where sequences have several rows; the groups there can be at most.
+static bool by_groups(const KvBatchArgs& b) { return b.row_starts && b.rows >= 4 * static_cast<int64_t>(b.sequences) && b.rows >= 64; }
+static int64_t most_groups(const KvBatchArgs& b) { return (b.rows + 6 * static_cast<int64_t>(b.sequences)) / kGroupRows; }
 
 hipError_t launch_heads(const HeadsArgs& a, const KvCacheArgs* cache, const KvBatchArgs* batch, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
     const KvCacheArgs c = cache ? *cache : KvCacheArgs{};
     const KvBatchArgs b = batch ? *batch : KvBatchArgs{};
-    const int lanes = a.head_dim <= 64 ? 8 : a.head_dim <= 128 ? 16 : a.head_dim <= 256 ? 32 : 64;
-    const int total = a.q_heads + a.k_heads + a.v_heads, per = kHeadThreads / lanes;
-    const int group = a.rows >= 1024 ? total : per;        // few rows: a workgroup a pass; many: the angles of a row are computed once
-    const dim3 grid(static_cast<unsigned>(a.rows), static_cast<unsigned>((total + group - 1) / group));
+    const int lanes = a.head_dim <= 64 ? 8 : a.head_dim <= 128 ? 16 : a.head_dim <= 256 ? 32 : 64, heads = kWave / lanes;
+    const int units = (a.q_heads + heads - 1) / heads + (a.k_heads + heads - 1) / heads + (a.v_heads + heads - 1) / heads;
+    if (cache && by_groups(b)) {
+        const dim3 grid(static_cast<unsigned>(most_groups(b)));
+        switch (lanes) {
+            case 8: heads_kernel<8, 4><<<grid, kHeadThreads, 0, s>>>(a, c, b, true, 1 << 30); break;
+            case 16: heads_kernel<16, 4><<<grid, kHeadThreads, 0, s>>>(a, c, b, true, 1 << 30); break;
+            default: heads_kernel<32, 4><<<grid, kHeadThreads, 0, s>>>(a, c, b, true, 1 << 30); break;
+        }
+        return hipGetLastError();
+    }
+    const int group = a.rows >= 1024 ? units : kHeadWaves;         // few rows: a workgroup for four units; many: the angles of a row are computed once
+    const dim3 grid(static_cast<unsigned>(a.rows), static_cast<unsigned>((units + group - 1) / group));
     switch (lanes) {
-        case 8: heads_kernel<8><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
-        case 16: heads_kernel<16><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
-        case 32: heads_kernel<32><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
-        default: heads_kernel<64><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
+        case 8: heads_kernel<8, 1><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
+        case 16: heads_kernel<16, 1><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
+        case 32: heads_kernel<32, 1><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
+        default: heads_kernel<64, 1><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
     }
     return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const KvCacheArgs& c, const KvBatchArgs& b, uint16_t* k, int64_t k_stride, uint16_t* v, int64_t v_stride, hipStream_t s) {
     if (b.rows == 0) return hipSuccess;
-    kv_read_kernel<<<dim3(static_cast<unsigned>(b.rows)), kHeadThreads, 0, s>>>(c, b, k, k_stride, v, v_stride);
+    if (by_groups(b)) {
+        kv_read_kernel<4><<<dim3(static_cast<unsigned>(most_groups(b))), kHeadThreads, 0, s>>>(c, b, k, k_stride, v, v_stride);
+    } else {
+        const int work = 2 * c.kv_heads * (c.head_dim / 8), wide = b.rows >= 1024 ? 1 : (work + kHeadThreads - 1) / kHeadThreads;
+        kv_read_kernel<1><<<dim3(static_cast<unsigned>(b.rows), static_cast<unsigned>(wide)), kHeadThreads, 0, s>>>(c, b, k, k_stride, v, v_stride);
+    }
     return hipGetLastError();
 }
 

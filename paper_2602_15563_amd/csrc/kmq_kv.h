@@ -15,6 +15,13 @@ constexpr int kKvCentroids = 16;
 // Bytes of a tile of one head: 16 tokens of K and V at half a byte an element, and their scales.
 KMQ_HD inline int kv_tile_bytes(int head_dim) { return 17 * head_dim; }
 
+// The bf16 in a half of a register as fp32, and two fp32 as bf16 (to nearest even, NaN stays NaN).
+__device__ __forceinline__ float kv_half(uint32_t v, int upper) { return __uint_as_float(upper ? v & 0xFFFF0000u : v << 16); }
+__device__ __forceinline__ uint32_t kv_pack2(float a, float b) {
+    const bf16x2_t v = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+    return __builtin_bit_cast(uint32_t, v);
+}
+
 // Where the row's token belongs: the sequence (-1: the row belongs to none) and the position in it, which may lie outside the cache.
 struct KvRow {
     int seq;
@@ -34,14 +41,59 @@ __device__ __forceinline__ KvRow kv_find_row(const KvBatchArgs& b, int64_t row) 
     return {seq, static_cast<int64_t>(b.lengths[seq]) - b.row_starts[seq + 1] + row};
 }
 
+// Four tokens at positions 4 i .. 4 i + 3 of a sequence, as many of them as have rows.
+struct KvGroup {
+    int seq;               // -1: none
+    int64_t row, pos;      // of the group's first token, which need not have one
+    uint32_t have;         // a bit a token
+};
+// The `at`-th group of the batch (groups are counted through the sequences), found by all lanes of a wave together.
+__device__ __forceinline__ KvGroup kv_find_group(const KvBatchArgs& b, int at) {
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
+    const int most = static_cast<int>(b.rows);
+    int64_t before = 0;                                // groups of the sequences of earlier rounds
+    for (int i = 0; i < b.sequences; i += kWave) {
+        const int s = i + lane;
+        int first = 0, n = 0, lead = 0;                // rows, and the tokens of the first group that stand before them
+        int64_t pos = 0;
+        if (s < b.sequences) {
+            const int v = b.row_starts[s], w = b.row_starts[s + 1];
+            first = v < 0 ? 0 : v > most ? most : v;
+            n = (w < 0 ? 0 : w > most ? most : w) - first;
+            n = n < 0 ? 0 : n;
+            pos = static_cast<int64_t>(b.lengths[s]) - w + first;
+            lead = static_cast<int>(pos & 3);
+        }
+        const int64_t mine = n ? (static_cast<int64_t>(n) + lead + 3) / 4 : 0;
+        int64_t upto = mine;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int64_t o = __shfl_up(upto, d);
+            upto += lane >= d ? o : 0;
+        }
+        const uint64_t past = __ballot(before + upto > at);
+        if (past) {
+            const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
+            const int64_t skip = 4 * (at - before - __shfl(upto - mine, l)) - __shfl(lead, l);     // rows before the group's first token
+            const int rows = __shfl(n, l);
+            uint32_t have = 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) have |= skip + r >= 0 && skip + r < rows ? 1u << r : 0u;
+            return {i + l, __shfl(first, l) + skip, __shfl(pos, l) + skip, have};
+        }
+        before += __shfl(upto, kWave - 1);
+    }
+    return {-1, 0, 0, 0};
+}
+
 // The tile of head `head` that holds position `pos` of sequence `seq`; nullptr where the page table has no page for it.
 __device__ __forceinline__ uint8_t* kv_tile(const KvCacheArgs& c, const KvBatchArgs& b, int head_dim, KvRow r, int head) {
-    if (r.seq < 0 || r.pos < 0) return nullptr;
-    const int64_t slot = r.pos / c.page_size;
+    if (r.seq < 0 || r.pos < 0 || r.pos > 0x7FFFFFFF) return nullptr;
+    const int pos = static_cast<int>(r.pos), slot = pos / c.page_size;
     if (slot >= b.table_width) return nullptr;
     const int64_t page = b.page_table[static_cast<int64_t>(r.seq) * b.table_width + slot];
     if (page < 0 || page >= c.num_pages) return nullptr;
-    const int64_t tile = (page * c.kv_heads + head) * (c.page_size / kKvTile) + r.pos % c.page_size / kKvTile;
+    const int64_t tile = (page * c.kv_heads + head) * (c.page_size / kKvTile) + (pos - slot * c.page_size) / kKvTile;
     return c.pages + tile * kv_tile_bytes(head_dim);
 }
 

@@ -97,3 +97,15 @@ def test_no_rows():
     kmq.qk_norm_rope(x, 128, x, 128, None, 0, 0, 2, 0, 64, rmsnorm=True)
     torch.cuda.synchronize()
     assert (host(x) == NAN16).all()
+
+
+@pytest.mark.parametrize("interleaved", (False, True))
+def test_an_infinity_without_a_norm_reaches_its_partner_and_no_further(interleaved):
+    x = patterns(np.random.default_rng(11).standard_normal((1, 2, 128)))
+    x[0, 0, 100], x[0, 1, 4] = 0x7F80, 0xFF80                     # behind the rotated elements, and among them
+    freq, pos = inv_freq(64), np.array([5], dtype=np.int32)
+    xd, q = dev(x.reshape(1, 256)), torch.zeros((1, 256), dtype=torch.int16, device="cuda")
+    kmq.qk_norm_rope(xd, 256, q, 256, None, 0, 1, 2, 0, 128, positions=dev(pos), inv_freq=dev(freq), rotary_dim=64, interleaved=interleaved)
+    torch.cuda.synchronize()
+    want = okv.round_bf16(okv.turn(x, pos, freq, 64, interleaved)).reshape(1, 256)
+    assert np.array_equal(okv.bf16_value(host(q)), okv.bf16_value(want), equal_nan=True)

@@ -178,3 +178,44 @@ def test_codebooks_from_the_quantiser():
         i2, s2 = okv.quantize(x[:, 0], book)
         assert np.array_equal(i2, idx) and np.array_equal(s2, scale)
     check(c, k, v)
+
+
+GROUPS = [  # rows enough to go four tokens at a time: starts and ends at every place in a group, sequences without rows between
+    ([70, 33], [70, 101], 32, 2, 64, {}),
+    ([65, 0, 66, 67], [66, 5, 70, 70], 64, 3, 128, dict(behind=5)),
+    ([30, 0, 1, 64], [30, 0, 3, 20], 96, 1, 256, {}),            # the last: more rows than tokens
+    ([90], [200], 32, 2, 128, dict(width=5)),
+    ([8] * 90, [8 + i for i in range(90)], 32, 1, 64, dict(behind=2)),
+]
+
+
+@pytest.mark.parametrize("i", range(len(GROUPS)))
+def test_many_rows_written_and_read(i):
+    news, lengths, page, heads, D, more = GROUPS[i]
+    print(f"many rows case {i}", flush=True)
+    c = Case(300 + i, news, lengths, page, heads, D, **more)
+    check(c, *fill(c, 310 + i), 8)
+
+
+@pytest.mark.parametrize("i", range(len(GROUPS)))
+@pytest.mark.parametrize("interleaved", (False, True))
+def test_many_rows_appended(i, interleaved):
+    news, lengths, page, heads, D, more = GROUPS[i]
+    print(f"many rows appended case {i} {interleaved}", flush=True)
+    c = Case(400 + i, news, lengths, page, heads, D, **more)
+    g = np.random.default_rng(410 + i)
+    nq, end = 5, c.starts[-1]
+    x = patterns(g.standard_normal((c.rows, nq + 2 * heads, D)))
+    freq = (10000.0 ** (-np.arange(0, D, 2) / D)).astype(np.float32)
+    gq, gk = patterns(1 + 0.3 * g.standard_normal(D)), patterns(1 + 0.3 * g.standard_normal(D))
+    pos = np.array([c.position(r)[1] for r in range(c.rows)])
+    xd, q = dev(x.reshape(c.rows, -1)), torch.full((c.rows, nq * D), NAN16, dtype=torch.int16, device="cuda")
+    c.to_device()
+    kmq.kv_append(c.cache, c.batch, xd, (nq + 2 * heads) * D, q, nq * D, nq, inv_freq=dev(freq), rotary_dim=D, interleaved=interleaved, q_gain=dev(gq),
+                  k_gain=dev(gk), eps=1e-6)
+    torch.cuda.synchronize()
+    turned = [okv.round_bf16(okv.turn(x[:, a:b], pos, freq, D, interleaved, True, gain, 1e-6)) for a, b, gain in ((0, nq, gq), (nq, nq + heads, gk))]
+    for r, page_, token in c.places():
+        c.pages.write(page_, token, turned[1][r], x[r, nq + heads:], c.books)
+    c.check_pages()
+    assert np.array_equal(host(q)[:end].reshape(end, nq, D), turned[0][:end]) and (host(q)[end:] == NAN16).all()
