@@ -18,6 +18,9 @@
 namespace kmq {
 
 constexpr int kHeadThreads = 256, kHeadWaves = kHeadThreads / kWave;
+#ifndef HW
+#define HW 4
+#endif
 constexpr int kGroupRows = 4;      // tokens whose V indices share a dword of the cache
 
 template <int CTRL>
@@ -45,6 +48,9 @@ __device__ __forceinline__ double inverse_root(double v) {
     for (int i = 0; i < 2; ++i) y *= fma(-0.5 * v * y, y, 1.5);
     return y;
 }
+__device__ __forceinline__ u32x4_t swap_halves(u32x4_t v) {
+    return u32x4_t{v[0] >> 16 | v[0] << 16, v[1] >> 16 | v[1] << 16, v[2] >> 16 | v[2] << 16, v[3] >> 16 | v[3] << 16};
+}
 // The largest of 8 neighbouring lanes' patterns, in all of them.
 __device__ __forceinline__ uint32_t max_over_8(uint32_t v) {
     const auto other = [](uint32_t x, auto ctrl) { return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, 0xF, 0xF, true)); };
@@ -60,22 +66,27 @@ __device__ __forceinline__ uint32_t max_over_8(uint32_t v) {
 struct Factors {
     double own[8], far[8];
 };
-__device__ __forceinline__ Factors make_factors(const HeadsArgs& a, const uint16_t* gain, const double* cosine, const double* sine, int d0, bool live) {
+// `angles`: cosine and sine of every pair, and (1, 0) behind the last for the elements that are not turned.
+__device__ __forceinline__ Factors make_factors(const HeadsArgs& a, const uint16_t* gain, const double2* angles, int d0, bool live) {
     Factors f;
     const int half = a.rotary_dim / 2;
-    const bool turned = live && d0 < a.rotary_dim;
-    const int other = a.interleaved ? d0 : d0 < half ? d0 + half : d0 - half, i0 = a.interleaved ? d0 / 2 : d0 < half ? d0 : d0 - half;
+    const bool turned = live && d0 < a.rotary_dim, left = d0 < half;
     u32x4_t g = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, go = g;
-    if (gain && live) g = *reinterpret_cast<const u32x4_t*>(gain + d0);
-    if (gain && turned) go = *reinterpret_cast<const u32x4_t*>(gain + other);
+    if (gain && live) g = go = *reinterpret_cast<const u32x4_t*>(gain + d0);
+    if (a.interleaved) {
+        go = swap_halves(go);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) go[e] ^= 0x00008000u;                     // the even element takes its partner's sine with a minus
+    } else {
+        if (gain && turned) go = *reinterpret_cast<const u32x4_t*>(gain + (left ? d0 + half : d0 - half));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) go[e] ^= left ? 0x80008000u : 0u;
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int i = a.interleaved ? i0 + e / 2 : i0 + e;
-        const bool left = a.interleaved ? e % 2 == 0 : d0 < half;
-        const double c = turned ? cosine[i] : 1.0, s = turned ? sine[i] : 0.0;
-        const float partner = a.interleaved ? kv_half(go[(e ^ 1) / 2], (e ^ 1) % 2) : kv_half(go[e / 2], e % 2);
-        f.own[e] = static_cast<double>(kv_half(g[e / 2], e % 2)) * c;
-        f.far[e] = static_cast<double>(partner) * (left ? -s : s);
+        const double2 t = angles[!turned ? half : a.interleaved ? d0 / 2 + e / 2 : (left ? d0 : d0 - half) + e];
+        f.own[e] = static_cast<double>(kv_half(g[e / 2], e % 2)) * t.x;
+        f.far[e] = static_cast<double>(kv_half(go[e / 2], e % 2)) * t.y;
     }
     return f;
 }
@@ -83,7 +94,7 @@ __device__ __forceinline__ Factors make_factors(const HeadsArgs& a, const uint16
 // One head's elements of a lane, turned.  `far` are its partners in the split form; `mean` is 1 / D.
 template <int LANES>
 __device__ __forceinline__ u32x4_t turn_head(const HeadsArgs& a, const Factors& f, u32x4_t own, u32x4_t far, bool turned, double mean) {
-    if (a.interleaved && turned) far = u32x4_t{own[0] >> 16 | own[0] << 16, own[1] >> 16 | own[1] << 16, own[2] >> 16 | own[2] << 16, own[3] >> 16 | own[3] << 16};
+    if (a.interleaved && turned) far = swap_halves(own);
     double r = 1.0;
     if (a.norm) {
         double ss = 0.0;
@@ -109,49 +120,49 @@ __device__ __forceinline__ u32x4_t turn_head(const HeadsArgs& a, const Factors& 
     return out;
 }
 
-// A boundary's place among bf16 values once it is scaled: x > b * s exactly where x > threshold.  The product is rounded to
-// nearest; where it was rounded up to a value that x may have, one step down.
-__device__ __forceinline__ float kv_threshold(float b, float s) {
-    const double exact = static_cast<double>(b) * static_cast<double>(s);      // 24 and 8 bits
-    float p = static_cast<float>(exact);
-    if (static_cast<double>(p) > exact) {
-        const uint32_t u = __float_as_uint(p);
-        p = p == 0.f ? -__uint_as_float(1u) : __uint_as_float(p > 0.f ? u - 1u : u + 1u);
-    }
-    return p;
-}
-
 // Eight elements of a block of 64 (8 neighbouring lanes) -> their indices in the nibbles of a dword, and the block's scale.
-// `place`: this wave's thresholds in shared memory, 16 of each of its 8 blocks.  Four comparisons an element, the boundaries
-// ascending: the first two against registers, the others against shared memory.
+// `boundary`: the boundaries as a binary tree, node n's children 2 n and 2 n + 1, root 1.  `place`: this wave's thresholds in
+// shared memory, a tree for each of its 8 blocks.  A threshold is b * s rounded to nearest, and one step down where that rounded it up
+// to a value that a bf16 may have: then x > threshold exactly where x > b * s.  An element walks down the tree, and where it
+// arrives is 16 + its index.
 __device__ __forceinline__ uint32_t quantise8(u32x4_t x, const float* boundary, float* place, uint32_t& scale) {
+    typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
     const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), sub = lane & 7;
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const uint32_t l = x[e] & 0x7FFFu, h = x[e] >> 16 & 0x7FFFu, m = l > h ? l : h;
-        top = m > top ? m : top;
-    }
-    top = max_over_8(top);
+    const auto size = [](uint32_t v) { return __builtin_bit_cast(u16x2_t, v & 0x7FFF7FFFu); };
+    const u16x2_t m = __builtin_elementwise_max(__builtin_elementwise_max(size(x[0]), size(x[1])), __builtin_elementwise_max(size(x[2]), size(x[3])));
+    const uint32_t top = max_over_8(m[0] > m[1] ? m[0] : m[1]);
     scale = top;
     const float s = top ? bf16_to_f32(top) : 1.f;
-    float* mine = place + lane / 8 * 16;
-    mine[2 * sub] = kv_threshold(boundary[2 * sub], s);
-    mine[2 * sub + 1] = kv_threshold(boundary[2 * sub + 1], s);               // (the sixteenth is never looked at)
+    float* const tree = place + lane / 8 * 16;
+    float t[2];
+    bool rare = false;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        t[k] = boundary[2 * sub + k] * s;
+        rare |= (__float_as_uint(t[k]) & 0xFFFFu) == 0u;
+    }
+    if (__ballot(rare)) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (static_cast<double>(t[k]) > static_cast<double>(boundary[2 * sub + k]) * static_cast<double>(s))     // (exact: 24 and 8 bits)
+                t[k] = t[k] == 0.f ? -__uint_as_float(1u) : __uint_as_float(__float_as_uint(t[k]) + (t[k] > 0.f ? -1 : 1));
+    }
+    tree[2 * sub] = t[0];                                 // (entry 0 is not looked at)
+    tree[2 * sub + 1] = t[1];
     __builtin_amdgcn_wave_barrier();
-    const float t3 = mine[3], t7 = mine[7], t11 = mine[11];
+    const float t1 = tree[1], t2 = tree[2], t3 = tree[3];
     uint32_t word = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float v = kv_half(x[e / 2], e % 2);
-        const bool b3 = v > t7, b2 = v > (b3 ? t11 : t3);
-        uint32_t i = (b3 ? 8u : 0u) + (b2 ? 4u : 0u);
-        i += v > mine[i + 1] ? 2u : 0u;
-        i += v > mine[i] ? 1u : 0u;
-        word |= i << (4 * e);
+        const bool first = v > t1;
+        uint32_t n = (first ? 6u : 4u) + (v > (first ? t3 : t2) ? 1u : 0u);
+        n = 2 * n + (v > tree[n] ? 1u : 0u);
+        n = 2 * n + (v > tree[n] ? 1u : 0u);
+        word += n << (4 * e);
     }
     __builtin_amdgcn_wave_barrier();
-    return word;
+    return word - 0x11111110u;                            // less the sixteens
 }
 
 // Where a row's token goes: the first tile of its page's heads, and its place in the tile.
@@ -184,11 +195,10 @@ __device__ __forceinline__ int v_first(int d0) { return (d0 & ~16) + (d0 & 16 ? 
 
 // LANES lanes hold a head, 8 elements each; a head never crosses a wave.  ROWS = 1: a workgroup takes a row, or with few rows a
 // part of its heads.  ROWS = 4 (cached): the rows of four tokens that share V's dwords, of one sequence.
-template <int LANES, int ROWS>
-__global__ void __launch_bounds__(kHeadThreads) heads_kernel(HeadsArgs a, KvCacheArgs c, KvBatchArgs b, bool cached, int units_per_group) {
+template <int LANES, int ROWS, bool TURNS>
+__global__ void __launch_bounds__(kHeadThreads, HW) heads_kernel(HeadsArgs a, KvCacheArgs c, KvBatchArgs b, bool cached, int units_per_group) {
     constexpr int kHeads = kWave / LANES;                 // heads of a unit: what a wave takes at once
-    constexpr int kPairs = LANES * 4;     // of a head of LANES * 8 elements
-    __shared__ double cosine[ROWS][kPairs], sine[ROWS][kPairs];
+    __shared__ double2 angles[ROWS][LANES * 4 + 1];        // a head has LANES * 8 elements at most
     __shared__ float boundary[2][kKvCentroids], threshold[kHeadWaves][8 * 16];
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int D = a.head_dim;
@@ -209,18 +219,22 @@ __global__ void __launch_bounds__(kHeadThreads) heads_kernel(HeadsArgs a, KvCach
         at = {g.seq, g.pos};
     }
     const int pairs = a.rotary_dim / 2;
-    if (pairs) {
+    if (TURNS && pairs) {
         for (int i = tid; i < ROWS * pairs; i += kHeadThreads) {
             const int r = ROWS == 1 ? 0 : i / pairs, p = i - r * pairs;
             if (!(have >> r & 1u)) continue;
             const double pos = a.positions ? static_cast<double>(a.positions[first + r]) : static_cast<double>(at.pos + r);
-            sincos(pos * static_cast<double>(a.inv_freq[p]), &sine[r][p], &cosine[r][p]);
+            double2 t;
+            sincos(pos * static_cast<double>(a.inv_freq[p]), &t.y, &t.x);
+            angles[r][p] = t;
         }
     }
+    if (TURNS && tid < ROWS) angles[tid][pairs] = double2{1.0, 0.0};
     if (cached && tid < 2 * kKvCentroids) {
         const int kv = tid / kKvCentroids, i = tid % kKvCentroids;
         const uint16_t* book = c.codebooks + kv * kKvCentroids;
-        boundary[kv][i] = i + 1 < kKvCentroids ? (bf16_to_f32(book[i]) + bf16_to_f32(book[i + 1])) * 0.5f : 0.f;
+        const int level = 31 - __clz(i | 1), j = (2 * (i - (1 << level)) + 1) * (8 >> level) - 1;      // node i of the tree is boundary j
+        boundary[kv][i] = i ? (bf16_to_f32(book[j]) + bf16_to_f32(book[j + 1])) * 0.5f : 0.f;
     }
     __syncthreads();
 
@@ -232,7 +246,6 @@ __global__ void __launch_bounds__(kHeadThreads) heads_kernel(HeadsArgs a, KvCach
     const int half = a.rotary_dim / 2;
     const bool split = !a.interleaved && inside && d0 < a.rotary_dim;
     const int other = d0 < half ? d0 + half : d0 - half;
-    const bool turns = a.norm || a.rotary_dim;
     const double mean = 1.0 / D;
     // units: query heads of every row, key heads of every row, then values, of all rows at once
     const int nq = (a.q_heads + kHeads - 1) / kHeads, nk = (a.k_heads + kHeads - 1) / kHeads, nv = (a.v_heads + kHeads - 1) / kHeads;
@@ -251,11 +264,11 @@ __global__ void __launch_bounds__(kHeadThreads) heads_kernel(HeadsArgs a, KvCach
             const uint16_t* src = (kind ? a.k + row * a.k_stride : a.q + row * a.q_stride) + static_cast<int64_t>(h) * D;
             u32x4_t own = {0, 0, 0, 0}, far = {0, 0, 0, 0};
             if (live) own = *reinterpret_cast<const u32x4_t*>(src + d0);
-            if (turns) {
+            if constexpr (TURNS) {
                 if (live && split) far = *reinterpret_cast<const u32x4_t*>(src + other);
                 if (factors_of != 2 * r + kind) {
                     factors_of = 2 * r + kind;
-                    f = make_factors(a, !a.norm ? nullptr : kind ? a.k_gain : a.q_gain, cosine[r], sine[r], d0, inside);
+                    f = make_factors(a, !a.norm ? nullptr : kind ? a.k_gain : a.q_gain, angles[r], d0, inside);
                 }
                 own = turn_head<LANES>(a, f, own, far, inside && d0 < a.rotary_dim, mean);
             }
@@ -378,28 +391,35 @@ __global__ void __launch_bounds__(kHeadThreads) kv_read_kernel(KvCacheArgs c, Kv
 static bool by_groups(const KvBatchArgs& b) { return b.row_starts && b.rows >= 4 * static_cast<int64_t>(b.sequences) && b.rows >= 64; }
 static int64_t most_groups(const KvBatchArgs& b) { return (b.rows + 6 * static_cast<int64_t>(b.sequences)) / kGroupRows; }
 
+template <int LANES, int ROWS>
+static void start(bool turns, dim3 grid, hipStream_t s, const HeadsArgs& a, const KvCacheArgs& c, const KvBatchArgs& b, bool cached, int units) {
+    if (turns) heads_kernel<LANES, ROWS, true><<<grid, kHeadThreads, 0, s>>>(a, c, b, cached, units);
+    else heads_kernel<LANES, ROWS, false><<<grid, kHeadThreads, 0, s>>>(a, c, b, cached, units);
+}
+
 hipError_t launch_heads(const HeadsArgs& a, const KvCacheArgs* cache, const KvBatchArgs* batch, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
     const KvCacheArgs c = cache ? *cache : KvCacheArgs{};
     const KvBatchArgs b = batch ? *batch : KvBatchArgs{};
     const int lanes = a.head_dim <= 64 ? 8 : a.head_dim <= 128 ? 16 : a.head_dim <= 256 ? 32 : 64, heads = kWave / lanes;
     const int units = (a.q_heads + heads - 1) / heads + (a.k_heads + heads - 1) / heads + (a.v_heads + heads - 1) / heads;
+    const bool turns = a.norm || a.rotary_dim;
     if (cache && by_groups(b)) {
         const dim3 grid(static_cast<unsigned>(most_groups(b)));
         switch (lanes) {
-            case 8: heads_kernel<8, 4><<<grid, kHeadThreads, 0, s>>>(a, c, b, true, 1 << 30); break;
-            case 16: heads_kernel<16, 4><<<grid, kHeadThreads, 0, s>>>(a, c, b, true, 1 << 30); break;
-            default: heads_kernel<32, 4><<<grid, kHeadThreads, 0, s>>>(a, c, b, true, 1 << 30); break;
+            case 8: start<8, 4>(turns, grid, s, a, c, b, true, 1 << 30); break;
+            case 16: start<16, 4>(turns, grid, s, a, c, b, true, 1 << 30); break;
+            default: start<32, 4>(turns, grid, s, a, c, b, true, 1 << 30); break;
         }
         return hipGetLastError();
     }
     const int group = a.rows >= 1024 ? units : kHeadWaves;         // few rows: a workgroup for four units; many: the angles of a row are computed once
     const dim3 grid(static_cast<unsigned>(a.rows), static_cast<unsigned>((units + group - 1) / group));
     switch (lanes) {
-        case 8: heads_kernel<8, 1><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
-        case 16: heads_kernel<16, 1><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
-        case 32: heads_kernel<32, 1><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
-        default: heads_kernel<64, 1><<<grid, kHeadThreads, 0, s>>>(a, c, b, cache != nullptr, group); break;
+        case 8: start<8, 1>(turns, grid, s, a, c, b, cache != nullptr, group); break;
+        case 16: start<16, 1>(turns, grid, s, a, c, b, cache != nullptr, group); break;
+        case 32: start<32, 1>(turns, grid, s, a, c, b, cache != nullptr, group); break;
+        default: start<64, 1>(turns, grid, s, a, c, b, cache != nullptr, group); break;
     }
     return hipGetLastError();
 }
