@@ -9,8 +9,6 @@
 // as they are, because V is stored in that order of tokens (kmq_kv.h): no probability crosses a lane.
 // Maxima, sums and products are kept in 32 bits; queries and centroids are bf16 as they come, and p * sV is rounded to
 // bf16 for the second product (off by 2^-8 of itself at most, to either side; the sum of p that divides it is not rounded).
-#include <type_traits>
-
 #include "kmq_kv.h"
 
 namespace kmq {
@@ -98,44 +96,14 @@ __device__ __forceinline__ float sum_over_quarters(float v) {
 }
 
 // The columns a workgroup takes: a tile of the (row, query head) pairs of one sequence and one key head.
-struct Tile {
-    int seq, index;        // sequence (-1: none), tile in it
-    int start, count;      // rows of the sequence
-};
-__device__ __forceinline__ int clamped_start(const KvBatchArgs& b, int i) {
-    const int v = b.row_starts[i], most = static_cast<int>(b.rows);
-    return v < 0 ? 0 : v > most ? most : v;
-}
-__device__ __forceinline__ Tile find_tile(const KvBatchArgs& b, int group, int columns, int at) {
+__device__ __forceinline__ KvPiece find_tile(const KvBatchArgs& b, int group, int columns, int at) {
     if (!b.row_starts) {
-        const int per = (group + columns - 1) / columns;
-        return {at / per, at % per, at / per, 1};
+        const int per = (group + columns - 1) / columns, seq = at / per;
+        return {seq, at - seq * per, seq, 1};
     }
-    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
-    int64_t before = 0;                                        // tiles of the sequences of earlier rounds
-    for (int i = 0; i < b.sequences; i += kWave) {
-        const int s = i + lane;
-        int first = 0, n = 0;
-        if (s < b.sequences) {
-            first = clamped_start(b, s);
-            n = clamped_start(b, s + 1) - first;
-            n = n < 0 ? 0 : n;
-        }
-        const int64_t mine = (static_cast<int64_t>(n) * group + columns - 1) / columns;
-        int64_t upto = mine;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int64_t o = __shfl_up(upto, d);
-            upto += lane >= d ? o : 0;
-        }
-        const uint64_t past = __ballot(before + upto > at);
-        if (past) {
-            const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
-            return {i + l, static_cast<int>(at - before - __shfl(upto - mine, l)), __shfl(first, l), __shfl(n, l)};
-        }
-        before += __shfl(upto, kWave - 1);
-    }
-    return {-1, 0, 0, 0};
+    KvPiece p = kv_find_piece(b, at, columns, group, columns - 1);
+    if (p.index * static_cast<int64_t>(columns) >= static_cast<int64_t>(p.count) * group) p.seq = -1;
+    return p;
 }
 
 struct AttnArgs {
@@ -224,6 +192,19 @@ struct Walk {
     }
 };
 
+// Probabilities times the scales of V, as bf16.  In a masked step a zero stays zero: what a token that is not seen holds may be anything.
+__device__ __forceinline__ u32x4_t weigh(const float (&p)[8], const float (&sv)[8], bool masked) {
+    u32x4_t r;
+    if (masked) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) r[e / 2] = kv_pack2(p[e] == 0.f ? 0.f : p[e] * sv[e], p[e + 1] == 0.f ? 0.f : p[e + 1] * sv[e + 1]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) r[e / 2] = kv_pack2(p[e] * sv[e], p[e + 1] * sv[e + 1]);
+    }
+    return r;
+}
+
 // Scores of CT columns (base 2, this lane's four tokens of each of a step's tiles) on their way to the second product.  The running
 // maxima m and sums l, and what is accumulated already, are brought to new maxima where a score passes an old one by kSlack;
 // then scores become exp2(score - maximum) and are added up.
@@ -278,7 +259,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     const int col = lane & 15, quarter = lane >> 4;
     const int head = static_cast<int>(blockIdx.x) % a.cache.kv_heads;
     const int group = a.q_heads / a.cache.kv_heads;
-    const Tile tile = find_tile(b, group, kAttnColumns, static_cast<int>(blockIdx.x) / a.cache.kv_heads);
+    const KvPiece tile = find_tile(b, group, kAttnColumns, static_cast<int>(blockIdx.x) / a.cache.kv_heads);
     if (tile.seq < 0) return;
 
     // this lane's column, and the tokens it may see
@@ -356,22 +337,19 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int e = 0; e < 8; ++e) sv[n][e] = kv_half(now.sc[e / 4][(NB + n) * 2 + e % 4 / 2], e % 2);
-        if (step < steps.whole_from || step >= steps.whole_to || !at.there) {
+        const bool masked = step < steps.whole_from || step >= steps.whole_to || !at.there;
+        if (masked) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
                 const bool seen = at.there && j >= see_from && j < see_to;
                 s[0][e] = seen ? s[0][e] : -INFINITY;
-#pragma unroll
-                for (int n = 0; n < NB; ++n) sv[n][e] = seen ? sv[n][e] : 0.f;       // (what lies behind a sequence may be anything)
             }
         }
         soften<1, DT>(s, m, l, o);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-            u32x4_t p;
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) p[e / 2] = kv_pack2(s[0][e] * sv[n][e], s[0][e + 1] * sv[n][e + 1]);
+            const u32x4_t p = weigh(s[0], sv[n], masked);
 #pragma unroll
             for (int j = 2 * n; j < 2 * n + 2; ++j) {
                 const u32x4_t x = decode8(cv, vw[0][j]), y = decode8(cv, vw[1][j]);
@@ -458,7 +436,7 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
     const int head = static_cast<int>(blockIdx.x) % a.cache.kv_heads;
     const int group = a.q_heads / a.cache.kv_heads;
     // the last tiles first: they see most
-    const Tile tile = find_tile(b, group, kColumns, static_cast<int>(gridDim.x / a.cache.kv_heads - 1 - blockIdx.x / a.cache.kv_heads));
+    const KvPiece tile = find_tile(b, group, kColumns, static_cast<int>(gridDim.x / a.cache.kv_heads - 1 - blockIdx.x / a.cache.kv_heads));
     if (tile.seq < 0) return;
 
     const int columns = tile.count * group;
@@ -538,7 +516,7 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
             scales[buffer][2 * tid + 1] = kv_half(sw, 1) * sf;
         }
     };
-    const auto multiply = [&](int step, int buffer, bool there, auto masked) {
+    const auto multiply = [&](int step, int buffer, bool there) {
         float s[CT][8];
         __builtin_amdgcn_s_setprio(1);                           // the waves of a unit out of step: one multiplies while another computes exponentials
 #pragma unroll
@@ -557,37 +535,25 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
                 }
             }
         __builtin_amdgcn_s_setprio(0);
-        uint32_t unseen[CT] = {};                                // a bit a token of this lane
+        const bool masked = step < own.whole_from || step >= own.whole_to || !there;
+        if (masked) {
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            if constexpr (masked) {
+            for (int c = 0; c < CT; ++c)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
-                    const bool seen = there && j >= see_from[c] && j < see_to[c];
-                    s[c][e] = seen ? s[c][e] : -INFINITY;
-                    unseen[c] |= seen ? 0u : 1u << e;
+                    s[c][e] = there && j >= see_from[c] && j < see_to[c] ? s[c][e] : -INFINITY;
                 }
-            }
         }
         soften<CT, DT>(s, m, l, o);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             u32x4_t p[CT];
-            f32x4_t sv[2];
+            float sv[8];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) sv[t] = *reinterpret_cast<const f32x4_t*>(&scales[buffer][t * (D / 2) + quarter * (D / 8) + 4 * (NB + n)]);
+            for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4_t*>(sv + 4 * t) = *reinterpret_cast<const f32x4_t*>(&scales[buffer][t * (D / 2) + quarter * (D / 8) + 4 * (NB + n)]);
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                float w[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    w[e] = s[c][e] * sv[e / 4][e % 4];
-                    if constexpr (masked) w[e] = unseen[c] >> e & 1u ? 0.f : w[e];           // (what lies behind a sequence may be anything)
-                }
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) p[c][e / 2] = kv_pack2(w[e], w[e + 1]);
-            }
+            for (int c = 0; c < CT; ++c) p[c] = weigh(s[c], sv, masked);
 #pragma unroll
             for (int d = 4 * n; d < 4 * n + 4; ++d) {
                 const u32x4_t v = vf[buffer][d][lane];
@@ -606,6 +572,7 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
         if (steps.from + 1 < steps.to) load(next.base);
     }
     __syncthreads();
+#pragma unroll 1
     for (int step = steps.from, buffer = 0; step < steps.to; ++step, buffer ^= 1) {
         const bool there = decoded;
         if (step + 1 < steps.to) {
@@ -615,10 +582,7 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
             coming = next.there;
             if (step + 2 < steps.to) load(next.base);
         }
-        if (busy && step >= own.from && step < own.to) {
-            if (step < own.whole_from || step >= own.whole_to || !there) multiply(step, buffer, there, std::true_type{});
-            else multiply(step, buffer, there, std::false_type{});
-        }
+        if (busy && step >= own.from && step < own.to) multiply(step, buffer, there);
         __syncthreads();
     }
 
@@ -766,8 +730,7 @@ __global__ void __launch_bounds__(kAttnThreads) attn_join_few_kernel(AttnArgs A)
 
 static int64_t column_tiles(const KvBatchArgs& b, int group, int columns) {
     if (!b.row_starts) return b.rows * ((group + columns - 1) / columns);
-    const int64_t used = b.rows < b.sequences ? b.rows : b.sequences;       // sequences that have rows, at most
-    return (b.rows * group + (columns - 1) * used) / columns;
+    return kv_pieces(b.rows, b.sequences, columns, group, columns - 1);
 }
 
 #ifndef TARGET

@@ -21,7 +21,6 @@ constexpr int kHeadThreads = 256, kHeadWaves = kHeadThreads / kWave;
 #ifndef HW
 #define HW 4
 #endif
-constexpr int kGroupRows = 4;      // tokens whose V indices share a dword of the cache
 
 template <int CTRL>
 __device__ __forceinline__ double dpp_move64(double v) {
@@ -122,8 +121,7 @@ __device__ __forceinline__ u32x4_t turn_head(const HeadsArgs& a, const Factors& 
 
 // Eight elements of a block of 64 (8 neighbouring lanes) -> their indices in the nibbles of a dword, and the block's scale.
 // `boundary`: the boundaries as a binary tree, node n's children 2 n and 2 n + 1, root 1.  `place`: this wave's thresholds in
-// shared memory, a tree for each of its 8 blocks.  A threshold is b * s rounded to nearest, and one step down where that rounded it up
-// to a value that a bf16 may have: then x > threshold exactly where x > b * s.  An element walks down the tree, and where it
+// shared memory, a tree for each of its 8 blocks.  A threshold is b * s rounded down: then x > threshold exactly where x > b * s.  An element walks down the tree, and where it
 // arrives is 16 + its index.
 __device__ __forceinline__ uint32_t quantise8(u32x4_t x, const float* boundary, float* place, uint32_t& scale) {
     typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
@@ -135,17 +133,20 @@ __device__ __forceinline__ uint32_t quantise8(u32x4_t x, const float* boundary, 
     const float s = top ? bf16_to_f32(top) : 1.f;
     float* const tree = place + lane / 8 * 16;
     float t[2];
-    bool rare = false;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        t[k] = boundary[2 * sub + k] * s;
-        rare |= (__float_as_uint(t[k]) & 0xFFFFu) == 0u;
+        const float edge = boundary[2 * sub + k];
+        t[k] = edge * s;
+        if (fmaf(edge, s, -t[k]) < 0.f) t[k] = __uint_as_float(__float_as_uint(t[k]) + (t[k] > 0.f ? -1 : 1));
     }
-    if (__ballot(rare)) {
+    if (__ballot(s < 0x1p-60f)) {                         // (where what the rounding took away may be too small for 32 bits)
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (static_cast<double>(t[k]) > static_cast<double>(boundary[2 * sub + k]) * static_cast<double>(s))     // (exact: 24 and 8 bits)
+        for (int k = 0; k < 2; ++k) {
+            const double exact = static_cast<double>(boundary[2 * sub + k]) * static_cast<double>(s);             // 24 and 8 bits
+            t[k] = static_cast<float>(exact);
+            if (static_cast<double>(t[k]) > exact)
                 t[k] = t[k] == 0.f ? -__uint_as_float(1u) : __uint_as_float(__float_as_uint(t[k]) + (t[k] > 0.f ? -1 : 1));
+        }
     }
     tree[2 * sub] = t[0];                                 // (entry 0 is not looked at)
     tree[2 * sub + 1] = t[1];
@@ -389,7 +390,7 @@ __global__ void __launch_bounds__(kHeadThreads) kv_read_kernel(KvCacheArgs c, Kv
 
 // Rows in groups of four tokens where sequences have several rows; the groups there can be at most.
 static bool by_groups(const KvBatchArgs& b) { return b.row_starts && b.rows >= 4 * static_cast<int64_t>(b.sequences) && b.rows >= 64; }
-static int64_t most_groups(const KvBatchArgs& b) { return (b.rows + 6 * static_cast<int64_t>(b.sequences)) / kGroupRows; }
+static int64_t most_groups(const KvBatchArgs& b) { return kv_pieces(b.rows, b.sequences, 4, 1, kKvGroupSlack); }
 
 template <int LANES, int ROWS>
 static void start(bool turns, dim3 grid, hipStream_t s, const HeadsArgs& a, const KvCacheArgs& c, const KvBatchArgs& b, bool cached, int units) {

@@ -41,49 +41,45 @@ __device__ __forceinline__ KvRow kv_find_row(const KvBatchArgs& b, int64_t row) 
     return {seq, static_cast<int64_t>(b.lengths[seq]) - b.row_starts[seq + 1] + row};
 }
 
-// Four tokens at positions 4 i .. 4 i + 3 of a sequence, as many of them as have rows.
-struct KvGroup {
-    int seq;               // -1: none
-    int64_t row, pos;      // of the group's first token, which need not have one
-    uint32_t have;         // a bit a token
+// Workgroups that take `size` rows-times-`each` of one sequence at a time, without a sum over the sequences before theirs: sequence b has
+// the places from (row_starts[b] * each + slack * b) / size on.  With slack >= size - 1 + what may stand before a sequence's first
+// row that is room for all of its pieces, and a place behind them belongs to nobody.  Found by all lanes of a wave together.
+struct KvPiece {
+    int seq, index;        // sequence (-1: none), piece in it (there may be no such piece)
+    int start, count;      // rows of the sequence, inside the batch's
 };
-// The `at`-th group of the batch (groups are counted through the sequences), found by all lanes of a wave together.
-__device__ __forceinline__ KvGroup kv_find_group(const KvBatchArgs& b, int at) {
-    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
-    const int most = static_cast<int>(b.rows);
-    int64_t before = 0;                                // groups of the sequences of earlier rounds
+KMQ_HD inline int64_t kv_pieces(int64_t rows, int64_t sequences, int size, int each, int slack) { return (rows * each + slack * sequences) / size; }
+__device__ __forceinline__ KvPiece kv_find_piece(const KvBatchArgs& b, int at, int size, int each, int slack) {
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), most = static_cast<int>(b.rows);
+    const int64_t reach = static_cast<int64_t>(at) * size + size - 1;
+    int seq = -1;
     for (int i = 0; i < b.sequences; i += kWave) {
         const int s = i + lane;
-        int first = 0, n = 0, lead = 0;                // rows, and the tokens of the first group that stand before them
-        int64_t pos = 0;
-        if (s < b.sequences) {
-            const int v = b.row_starts[s], w = b.row_starts[s + 1];
-            first = v < 0 ? 0 : v > most ? most : v;
-            n = (w < 0 ? 0 : w > most ? most : w) - first;
-            n = n < 0 ? 0 : n;
-            pos = static_cast<int64_t>(b.lengths[s]) - w + first;
-            lead = static_cast<int>(pos & 3);
-        }
-        const int64_t mine = n ? (static_cast<int64_t>(n) + lead + 3) / 4 : 0;
-        int64_t upto = mine;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const int64_t o = __shfl_up(upto, d);
-            upto += lane >= d ? o : 0;
-        }
-        const uint64_t past = __ballot(before + upto > at);
-        if (past) {
-            const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
-            const int64_t skip = 4 * (at - before - __shfl(upto - mine, l)) - __shfl(lead, l);     // rows before the group's first token
-            const int rows = __shfl(n, l);
-            uint32_t have = 0;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) have |= skip + r >= 0 && skip + r < rows ? 1u << r : 0u;
-            return {i + l, __shfl(first, l) + skip, __shfl(pos, l) + skip, have};
-        }
-        before += __shfl(upto, kWave - 1);
+        const int64_t first = s < b.sequences ? static_cast<int64_t>(b.row_starts[s]) * each + static_cast<int64_t>(slack) * s : reach + 1;
+        seq += __popcll(__ballot(first <= reach));
     }
-    return {-1, 0, 0, 0};
+    if (seq < 0) return {-1, 0, 0, 0};
+    const int v = b.row_starts[seq], w = b.row_starts[seq + 1];
+    const int start = v < 0 ? 0 : v > most ? most : v, end = w < start ? start : w > most ? most : w;
+    return {seq, at - static_cast<int>((static_cast<int64_t>(v) * each + static_cast<int64_t>(slack) * seq) / size), start, end - start};
+}
+
+// Four tokens at positions 4 i .. 4 i + 3 of a sequence, as many of them as have rows.
+constexpr int kKvGroupSlack = 6;
+struct KvGroup {
+    int seq;               // -1: none
+    int64_t row, pos;      // of the group's first token, which need not have a row
+    uint32_t have;         // a bit a token
+};
+__device__ __forceinline__ KvGroup kv_find_group(const KvBatchArgs& b, int at) {
+    const KvPiece p = kv_find_piece(b, at, 4, 1, kKvGroupSlack);
+    if (p.seq < 0) return {-1, 0, 0, 0};
+    const int64_t pos = static_cast<int64_t>(b.lengths[p.seq]) - b.row_starts[p.seq + 1] + p.start;
+    const int64_t skip = 4 * static_cast<int64_t>(p.index) - (pos & 3);           // rows before the group's first token
+    uint32_t have = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) have |= skip + r >= 0 && skip + r < p.count ? 1u << r : 0u;
+    return {have ? p.seq : -1, p.start + skip, pos + skip, have};
 }
 
 // The tile of head `head` that holds position `pos` of sequence `seq`; nullptr where the page table has no page for it.
