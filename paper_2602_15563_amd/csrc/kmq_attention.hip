@@ -156,7 +156,8 @@ __device__ __forceinline__ void take_part(Steps& s, int splits, int part) {
     s.to = s.to - s.from < per ? s.to : s.from + per;
 }
 
-// Walks the page table along steps that are `stride` apart.
+// Walks the page table along steps.  64 page numbers are read at once, one a lane: a number read by itself for every step would be waited
+// for, and read as a scalar it would make every wait for shared memory a wait for all of it.
 struct Place {
     const uint8_t* base;   // of a step's two tiles
     bool there;
@@ -166,79 +167,109 @@ struct Walk {
     const int32_t* table;
     const uint8_t* head_base;
     int64_t page_stride;
-    int64_t num_pages;
-    int slot, within, steps_per_page;
+    int width, num_pages, steps_per_page;
+    int slot, within;      // of the step that the walk stands at
+    int first_slot, pages; // of lane 0, and this lane's number
     __device__ __forceinline__ Walk(const AttentionArgs& a, int seq, int head, int step) {
         const int tiles = a.cache.page_size / kKvTile;
         table = a.batch.page_table + static_cast<int64_t>(seq) * a.batch.table_width;
+        width = a.batch.table_width;
+        num_pages = static_cast<int>(a.cache.num_pages);
         page_stride = static_cast<int64_t>(a.cache.kv_heads) * tiles * (17 * D);
         head_base = a.cache.pages + static_cast<int64_t>(head) * tiles * (17 * D);
-        num_pages = a.cache.num_pages;
         steps_per_page = tiles / 2;
         slot = step / steps_per_page;
         within = step - slot * steps_per_page;
+        read();
     }
-    // the place of the step that the walk stands at, which lies on the table only where `inside`; then on by `stride`
-    __device__ __forceinline__ Place next(bool inside, int stride) {
-        const int page = inside ? table[slot] : 0;
-        const bool there = page >= 0 && page < num_pages;
-        const uint8_t* base = head_base + (there ? page : 0) * page_stride + static_cast<int64_t>(within) * (2 * 17 * D);
+    __device__ __forceinline__ void read() {
+        const int at = slot + (static_cast<int>(threadIdx.x) & (kWave - 1));
+        first_slot = slot;
+        pages = at < width ? table[at] : -1;
+    }
+    // The place of the step that the walk stands at (one that is not there reads the first page, and nothing of it is used).
+    __device__ __forceinline__ Place place(bool inside) {
+        if (slot - first_slot >= kWave) read();
+        const int page = __builtin_amdgcn_readlane(pages, slot - first_slot);
+        const bool there = inside && page >= 0 && page < num_pages;
+        return {head_base + (there ? page : 0) * page_stride + static_cast<int64_t>(within) * (2 * 17 * D), there};
+    }
+    __device__ __forceinline__ void on(int stride) {
         within += stride;
         while (within >= steps_per_page) {
             within -= steps_per_page;
             ++slot;
         }
-        return {base, there};
     }
 };
 
-// Probabilities times the scales of V, as bf16.  In a masked step a zero stays zero: what a token that is not seen holds may be anything.
-__device__ __forceinline__ u32x4_t weigh(const float (&p)[8], const float (&sv)[8], bool masked) {
+// Probabilities times the scales of V, as bf16.
+__device__ __forceinline__ u32x4_t weigh(const float (&p)[8], const float (&sv)[8]) {
     u32x4_t r;
-    if (masked) {
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) r[e / 2] = kv_pack2(p[e] == 0.f ? 0.f : p[e] * sv[e], p[e + 1] == 0.f ? 0.f : p[e + 1] * sv[e + 1]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) r[e / 2] = kv_pack2(p[e] * sv[e], p[e + 1] * sv[e + 1]);
-    }
+    for (int e = 0; e < 8; e += 2) r[e / 2] = kv_pack2(p[e] * sv[e], p[e + 1] * sv[e + 1]);
     return r;
 }
+// A probability of zero stays zero whatever the scale: what a token that is not seen holds may be anything.
+__device__ __forceinline__ void clear_unseen(u32x4_t& w, const float (&p)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) w[e / 2] &= (p[e] == 0.f ? 0u : 0x0000FFFFu) | (p[e + 1] == 0.f ? 0u : 0xFFFF0000u);
+}
 
-// Scores of CT columns (base 2, this lane's four tokens of each of a step's tiles) on their way to the second product.  The running
-// maxima m and sums l, and what is accumulated already, are brought to new maxima where a score passes an old one by kSlack;
-// then scores become exp2(score - maximum) and are added up.
-template <int CT, int DT>
-__device__ __forceinline__ void soften(float (&s)[CT][8], float (&m)[CT], float (&l)[CT], f32x4_t (&o)[CT][DT]) {
-    float top[CT];
-    bool past = false;
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        top[c] = s[c][0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) top[c] = fmaxf(top[c], s[c][e]);
-        past |= top[c] > m[c] + kSlack;
-    }
-    if (__ballot(past)) {
+// CT columns' running maxima, sums, and how far a score (base 2, less the maximum) may be up before everything is brought to a new
+// maximum: kSlack, and before the first token anything that is a number.
+template <int CT>
+struct Running {
+    float m[CT], l[CT], limit[CT];
+    __device__ __forceinline__ Running() {
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
-            const float to = fmaxf(m[c], max_over_quarters(top[c])), shrink = __builtin_amdgcn_exp2f(m[c] - to);
-            m[c] = to;
-            l[c] *= shrink;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[c][d][e] *= shrink;
+            m[c] = l[c] = 0.f;
+            limit[c] = kLowest;
         }
     }
+    __device__ __forceinline__ float maximum(int c) const { return limit[c] == kLowest ? kLowest : m[c]; }
+    // The maxima follow the scores of a step: this lane's four tokens of each of its tiles.
+    template <int DT>
+    __device__ __forceinline__ void follow(float (&s)[CT][8], f32x4_t (&o)[CT][DT]) {
+        float top[CT];
+        bool past = false;
 #pragma unroll
-    for (int c = 0; c < CT; ++c)
+        for (int c = 0; c < CT; ++c) {
+            top[c] = s[c][0];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s[c][e] = __builtin_amdgcn_exp2f(s[c][e] - m[c]);
-            l[c] += s[c][e];
+            for (int e = 1; e < 8; ++e) top[c] = fmaxf(top[c], s[c][e]);
+            past |= top[c] > limit[c];
         }
-}
+        if (__ballot(past)) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const bool first = limit[c] == kLowest;           // (nothing is accumulated yet, and the maximum may be far below 0)
+                const float to = max_over_quarters(top[c]), up = to > (first ? kLowest : 0.f) ? to : 0.f;
+                const float shrink = first ? 1.f : __builtin_amdgcn_exp2f(-up);
+                limit[c] = to > kLowest ? kSlack : limit[c];
+                m[c] += up;
+                l[c] *= shrink;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[c][e] -= up;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[c][d][e] *= shrink;
+            }
+        }
+    }
+    // Scores become probabilities, and are added up.
+    __device__ __forceinline__ void soften(float (&s)[CT][8]) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                s[c][e] = __builtin_amdgcn_exp2f(s[c][e]);
+                l[c] += s[c][e];
+            }
+    }
+};
 
 // Few columns a sequence (single tokens, drafts): a workgroup takes 16 columns, and its waves take the steps in turn.  A wave reads
 // and decodes for itself, K by a table of index pairs in shared memory, V by byte permutes from registers: either way alone
@@ -299,11 +330,11 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     f32x4_t o[1][DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[0][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float m[1] = {kLowest}, l[1] = {0.f};
+    Running<1> run;
 
     int step = steps.from + wave;
     Walk<D> walk(a, tile.seq, head, step);
-    Place at = walk.next(step < steps.to, kAttnWaves), next = walk.next(step + kAttnWaves < steps.to, kAttnWaves);
+    Place at = walk.place(step < steps.to);
     KWords<D> kw;
     if (step < steps.to) kw.load(at.base, lane, quarter);
     for (; step < steps.to; step += kAttnWaves) {
@@ -311,8 +342,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) load_words<D / 32>(vw[t], at.base + t * kTile + 8 * D + lane * (D / 8));
         const KWords<D> now = kw;
+        walk.on(kAttnWaves);
+        const Place next = walk.place(step + kAttnWaves < steps.to);
         if (step + kAttnWaves < steps.to) kw.load(next.base, lane, quarter);
-        const Place after = walk.next(step + 2 * kAttnWaves < steps.to, kAttnWaves);
 
         float s[1][8];
 #pragma unroll
@@ -330,7 +362,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
                 for (int e = 0; e < 4; ++e) sum[e] = fmaf(acc[e], kv_half(now.sc[t][n * 2 + e / 2], e % 2), sum[e]);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[0][4 * t + e] = sum[e] * scale;
+            for (int e = 0; e < 4; ++e) s[0][4 * t + e] = fmaf(sum[e], scale, -run.m[0]);
         }
         float sv[NB][8];
 #pragma unroll
@@ -346,10 +378,12 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
                 s[0][e] = seen ? s[0][e] : -INFINITY;
             }
         }
-        soften<1, DT>(s, m, l, o);
+        run.follow<DT>(s, o);
+        run.soften(s);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-            const u32x4_t p = weigh(s[0], sv[n], masked);
+            u32x4_t p = weigh(s[0], sv[n]);
+            if (masked) clear_unseen(p, s[0]);
 #pragma unroll
             for (int j = 2 * n; j < 2 * n + 2; ++j) {
                 const u32x4_t x = decode8(cv, vw[0][j]), y = decode8(cv, vw[1][j]);
@@ -358,13 +392,12 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
             }
         }
         at = next;
-        next = after;
     }
 
     // the waves' results joined: every wave's on the scale of the largest maximum
-    const float sum_l = sum_over_quarters(l[0]);
+    const float m = run.maximum(0), sum_l = sum_over_quarters(run.l[0]);
     if (quarter == 0) {
-        stat[0][wave][col] = m[0];
+        stat[0][wave][col] = m;
         stat[1][wave][col] = sum_l;
     }
     __syncthreads();
@@ -385,7 +418,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
             a.lse[pair] = none ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kLn2;
         }
     }
-    const float weight = __builtin_amdgcn_exp2f(m[0] - most), norm = none ? 0.f : 1.f / all;
+    const float weight = __builtin_amdgcn_exp2f(m - most), norm = none ? 0.f : 1.f / all;
 #pragma unroll
     for (int c0 = 0; c0 < D; c0 += DC) {
         if (c0) __syncthreads();
@@ -419,16 +452,15 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
 // together, an equal share of it each, into shared memory in the order of the first product's and the second product's first operand.
 // Two such buffers: the next step is decoded into one while the products read the other.
 template <int D, int CT, int WAVES>
-__global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_kernel(AttnArgs A) {
+__global__ void __launch_bounds__(WAVES * kWave, 2) attn_tile_kernel(AttnArgs A) {
     constexpr int NB = D / KMQ_BLOCK, DT = D / 16, KF = D / 32;
     constexpr int kTile = 17 * D, kColumns = WAVES * 16 * CT;
-    // a wave's dwords a lane: of K in one tile (a share of it), of V in both tiles (of fewer than there are waves: half of the nibbles)
+    // a wave's dwords a lane: of K in one tile (a share of it), of V in both tiles (where waves are more than those: half of the nibbles of one)
     constexpr int kShares = WAVES / 2, KD = KF / kShares;
     constexpr bool kHalves = KF < WAVES;
-    constexpr int VD = kHalves ? 1 : KF / WAVES;
-    static_assert(KD >= 1 && (!kHalves || WAVES == 2 * KF), "a share is a dword at least");
+    static_assert(KD >= 1 && (kHalves ? WAVES == 2 * KF : WAVES == KF), "an equal share");
     __shared__ u32x4_t kf[2][2 * KF][kWave], vf[2][DT][kWave];
-    __shared__ float scales[2][2 * D / 2];                              // in the tiles' order, K's times the scale of the scores
+    __shared__ float scales[2][D];                                   // in the tiles' order, K's times the scale of the scores
     const AttentionArgs& a = A.a;
     const KvBatchArgs& b = a.batch;
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -443,7 +475,7 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
     const int first_column = tile.index * kColumns, mine = first_column + wave * 16 * CT;
     const int last_column = first_column + kColumns < columns ? first_column + kColumns - 1 : columns - 1;
     const int my_last = mine + 16 * CT < columns ? mine + 16 * CT - 1 : columns - 1;
-    const bool busy = mine < columns;                                // a wave without columns decodes all the same
+    const bool busy = mine < columns;                                // a wave without columns works all the same, and stores nothing
     const Sight sight = sight_of(a, tile.seq);
     Steps steps = steps_of(sight, first_column / group, last_column / group);
     Steps own = steps_of(sight, (busy ? mine : first_column) / group, (busy ? my_last : first_column) / group);
@@ -451,7 +483,7 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
 
     u32x4_t q[CT][2 * NB];
     f32x4_t o[CT][DT];
-    float m[CT], l[CT];
+    Running<CT> run;
     int see_from[CT], see_to[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
@@ -469,44 +501,34 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[c][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        m[c] = kLowest;
-        l[c] = 0.f;
     }
     const Centroids ck = load_centroids(a.cache.codebooks), cv = load_centroids(a.cache.codebooks + kKvCentroids);
 
     // this wave's share of a step
     const int kt = wave / kShares, k0 = wave % kShares * KD;
-    const int v0 = kHalves ? wave >> 1 : wave * VD;
-    uint32_t kw[KD], vw[2][VD], sw = 0;
-    const auto load = [&](const uint8_t* base) {
+    const int v0 = kHalves ? wave >> 1 : wave, v_shift = (wave & 1) * 4;
+    const float sf = tid / (2 * NB) & 1 ? 1.f : a.scale * kLog2e;     // (dword tid of a step's scales: a quarter's K, then its V)
+    uint32_t kw[KD], vw[2], sw = 0;
+    const auto load = [&](const uint8_t* base) __attribute__((always_inline)) {
         const uint8_t* k = base + kt * kTile + lane * (D / 8) + 4 * k0;
         if constexpr (KD == 1) kw[0] = *reinterpret_cast<const uint32_t*>(k);
         else load_words<KD>(kw, k);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const uint8_t* v = base + t * kTile + 8 * D + lane * (D / 8) + 4 * v0;
-            if constexpr (VD == 1) vw[t][0] = *reinterpret_cast<const uint32_t*>(v);
-            else load_words<VD>(vw[t], v);
-        }
+        for (int t = 0; t < 2; ++t) vw[t] = *reinterpret_cast<const uint32_t*>(base + t * kTile + 8 * D + lane * (D / 8) + 4 * v0);
         if (tid < D / 2) sw = *reinterpret_cast<const uint32_t*>(base + tid / (D / 4) * kTile + 16 * D + tid % (D / 4) * 4);
     };
-    const float sf = tid / (2 * NB) & 1 ? 1.f : a.scale * kLog2e;     // (dword tid of the scales: its quarter's K, then V)
-    const auto decode = [&](int buffer) {
+    const auto decode = [&](int buffer) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < KD; ++i) kf[buffer][kt * KF + k0 + i][lane] = decode8(ck, kw[i]);
         if constexpr (!kHalves) {
-#pragma unroll
-            for (int i = 0; i < VD; ++i) {
-                const u32x4_t x = decode8(cv, vw[0][i]), y = decode8(cv, vw[1][i]);
-                vf[buffer][2 * (v0 + i)][lane] = u32x4_t{x[0], x[1], y[0], y[1]};
-                vf[buffer][2 * (v0 + i) + 1][lane] = u32x4_t{x[2], x[3], y[2], y[3]};
-            }
+            const u32x4_t x = decode8(cv, vw[0]), y = decode8(cv, vw[1]);
+            vf[buffer][2 * v0][lane] = u32x4_t{x[0], x[1], y[0], y[1]};
+            vf[buffer][2 * v0 + 1][lane] = u32x4_t{x[2], x[3], y[2], y[3]};
         } else {
-            const int shift = (wave & 1) * 4;
             uint32_t r[4];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const uint32_t w = vw[t][0] >> shift;
+                const uint32_t w = vw[t] >> v_shift;
                 decode4(cv, w & 0x07070707u, (w >> 1 & 0x04040404u) | 0x03020100u, r[2 * t], r[2 * t + 1]);
             }
             vf[buffer][wave][lane] = u32x4_t{r[0], r[1], r[2], r[3]};
@@ -516,9 +538,9 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
             scales[buffer][2 * tid + 1] = kv_half(sw, 1) * sf;
         }
     };
-    const auto multiply = [&](int step, int buffer, bool there) {
+    const auto multiply = [&](int step, int buffer, bool there) __attribute__((always_inline)) {
         float s[CT][8];
-        __builtin_amdgcn_s_setprio(1);                           // the waves of a unit out of step: one multiplies while another computes exponentials
+        __builtin_amdgcn_s_setprio(1);                               // the waves of a unit out of step: one multiplies while another computes exponentials
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -531,12 +553,13 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
                     acc = mfma(a0, q[c][2 * n], acc);
                     acc = mfma(a1, q[c][2 * n + 1], acc);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[c][4 * t + e] = n ? fmaf(acc[e], sk[e], s[c][4 * t + e]) : acc[e] * sk[e];
+                    for (int e = 0; e < 4; ++e) s[c][4 * t + e] = fmaf(acc[e], sk[e], n ? s[c][4 * t + e] : -run.m[c]);
                 }
             }
         __builtin_amdgcn_s_setprio(0);
         const bool masked = step < own.whole_from || step >= own.whole_to || !there;
         if (masked) {
+            asm volatile("");                                        // (kept a branch: few steps are masked)
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
@@ -545,52 +568,63 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
                     s[c][e] = there && j >= see_from[c] && j < see_to[c] ? s[c][e] : -INFINITY;
                 }
         }
-        soften<CT, DT>(s, m, l, o);
+        run.template follow<DT>(s, o);
+        run.soften(s);
+        u32x4_t p[NB][CT];
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-            u32x4_t p[CT];
             float sv[8];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4_t*>(sv + 4 * t) = *reinterpret_cast<const f32x4_t*>(&scales[buffer][t * (D / 2) + quarter * (D / 8) + 4 * (NB + n)]);
+            for (int t = 0; t < 2; ++t)
+                *reinterpret_cast<f32x4_t*>(sv + 4 * t) = *reinterpret_cast<const f32x4_t*>(&scales[buffer][t * (D / 2) + quarter * (D / 8) + 4 * (NB + n)]);
 #pragma unroll
-            for (int c = 0; c < CT; ++c) p[c] = weigh(s[c], sv, masked);
+            for (int c = 0; c < CT; ++c) p[n][c] = weigh(s[c], sv);
+        }
+        if (masked) {
+            asm volatile("");
 #pragma unroll
-            for (int d = 4 * n; d < 4 * n + 4; ++d) {
-                const u32x4_t v = vf[buffer][d][lane];
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int c = 0; c < CT; ++c) o[c][d] = mfma(v, p[c], o[c][d]);
-            }
+                for (int c = 0; c < CT; ++c) clear_unseen(p[n][c], s[c]);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const u32x4_t v = vf[buffer][d][lane];
+#pragma unroll
+            for (int c = 0; c < CT; ++c) o[c][d] = mfma(v, p[d / 4][c], o[c][d]);
         }
     };
 
-    Walk<D> walk(a, tile.seq, head, steps.from);
-    Place at = walk.next(steps.from < steps.to, 1), next = walk.next(steps.from + 1 < steps.to, 1);
-    bool decoded = at.there, coming = next.there;                    // whether the step in the buffer, and the one in registers, is in the cache
-    if (steps.from < steps.to) {
-        load(at.base);
+    const int last = steps.to - 1;
+    if (steps.from <= last) {
+        Walk<D> walk(a, tile.seq, head, steps.from);
+        Place place = walk.place(true);
+        bool there = place.there;                                    // whether the step in the buffer, and the one in registers, is in the cache
+        load(place.base);
+        walk.on(1);
+        place = walk.place(steps.from < last);
         decode(0);
-        if (steps.from + 1 < steps.to) load(next.base);
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int step = steps.from, buffer = 0; step < steps.to; ++step, buffer ^= 1) {
-        const bool there = decoded;
-        if (step + 1 < steps.to) {
-            decode(buffer ^ 1);
-            decoded = coming;
-            next = walk.next(step + 2 < steps.to, 1);
-            coming = next.there;
-            if (step + 2 < steps.to) load(next.base);
-        }
-        if (busy && step >= own.from && step < own.to) multiply(step, buffer, there);
+        load(place.base);
+        bool coming = place.there;
         __syncthreads();
+#pragma unroll 1
+        for (int step = steps.from, buffer = 0; step <= last; ++step, buffer ^= 1) {
+            decode(buffer ^ 1);                                      // the next step's
+            walk.on(1);
+            place = walk.place(step + 2 <= last);
+            load(place.base);
+            if (busy && step >= own.from && step < own.to) multiply(step, buffer, there);
+            there = coming;
+            coming = place.there;
+            __syncthreads();
+        }
     }
 
     const bool whole = A.splits == 1;
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
         const int column = mine + 16 * c + col;
-        const float all = sum_over_quarters(l[c]);
+        const float all = sum_over_quarters(run.l[c]), most = run.maximum(c);
         if (column >= columns) continue;
         const bool none = all == 0.f;
         const float norm = none ? 0.f : 1.f / all;
@@ -600,10 +634,10 @@ __global__ void __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 2) attn_tile_k
         if (quarter == 0) {
             if (!whole) {
                 float* ml = A.part_ml + (static_cast<int64_t>(blockIdx.y) * b.rows * a.q_heads + pair) * 2;
-                ml[0] = m[c];
+                ml[0] = most;
                 ml[1] = all;
             } else if (a.lse) {
-                a.lse[pair] = none ? -INFINITY : (m[c] + __builtin_amdgcn_logf(all)) * kLn2;
+                a.lse[pair] = none ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kLn2;
             }
         }
 #pragma unroll
@@ -742,18 +776,16 @@ static int64_t column_tiles(const KvBatchArgs& b, int group, int columns) {
 #ifndef CT1
 #define CT1 2
 #endif
-#ifndef WIDE
-#define WIDE 32
+#ifndef TW64
+#define TW64 4
 #endif
-#ifndef TW
-#define TW 8
-#endif
-template <int D> constexpr int kTW = D == 64 ? 4 : TW;
-template <int D> constexpr int kCT = D == 256 ? 1 : CT1;
-inline int tile_columns(int D) { return D == 64 ? kTW<64> * 16 * kCT<64> : D == 128 ? kTW<128> * 16 * kCT<128> : kTW<256> * 16 * kCT<256>; }
+template <int D> constexpr int kTileWaves = D == 64 ? TW64 : 8;
+template <int D> constexpr int kColumnTiles = D == 256 ? 1 : CT1;      // of 16 columns a wave: what its registers hold
+template <int D> constexpr int kTileColumns = kTileWaves<D> * 16 * kColumnTiles<D>;
+static int tile_columns(int D) { return D == 64 ? kTileColumns<64> : D == 128 ? kTileColumns<128> : kTileColumns<256>; }
 AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
     const int group = q_heads / c.kv_heads;
-    const bool wide = b.rows * group > static_cast<int64_t>(WIDE) * b.sequences;
+    const bool wide = b.rows * group > static_cast<int64_t>(32) * b.sequences;
     AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? tile_columns(c.head_dim) : kAttnColumns, 1, 0};
     const int64_t items = column_tiles(b, group, p.columns) * c.kv_heads;
     const int64_t steps = static_cast<int64_t>(b.table_width) * (c.page_size / kKvStep);
@@ -774,7 +806,7 @@ static hipError_t launch_attn(const AttnArgs& A, const AttentionPlan& p, hipStre
     const int64_t items = column_tiles(b, A.a.q_heads / A.a.cache.kv_heads, p.columns) * A.a.cache.kv_heads;
     const dim3 grid(static_cast<unsigned>(items), static_cast<unsigned>(A.splits));
     if (p.columns == kAttnColumns) attn_kernel<D><<<grid, kAttnThreads, 0, s>>>(A);
-    else attn_tile_kernel<D, kCT<D>, kTW<D>><<<grid, kTW<D> * kWave, 0, s>>>(A);
+    else attn_tile_kernel<D, kColumnTiles<D>, kTileWaves<D>><<<grid, kTileWaves<D> * kWave, 0, s>>>(A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits == 1) return e;
     const int64_t pairs = b.rows * A.a.q_heads, at_once = kAttnThreads / (D / 4);
