@@ -185,7 +185,9 @@ struct Walk {
     __device__ __forceinline__ void read() {
         const int at = slot + (static_cast<int>(threadIdx.x) & (kWave - 1));
         first_slot = slot;
-        pages = at < width ? table[at] : -1;
+        int v = at < width ? table[at] : -1;
+        asm volatile("" : "+v"(v));                       // (waited for here, and not wherever the number is used)
+        pages = v;
     }
     // The place of the step that the walk stands at (one that is not there reads the first page, and nothing of it is used).
     __device__ __forceinline__ Place place(bool inside) {
