@@ -15,7 +15,8 @@ namespace kmq {
 
 constexpr int kAttnWaves = 4, kAttnThreads = kAttnWaves * kWave;
 constexpr int kAttnColumns = 16;              // columns of a workgroup: one matrix-core tile
-constexpr int kAttnMinSteps = 2 * kAttnWaves; // steps of a part at least: fewer are not worth the joining
+// Steps of a part at least (us with 8 / 16: one sequence of 4096 tokens, 8 key heads 10.9 / 14.5; one of 16000 16.7 / 14.9).
+constexpr int kAttnMinSteps = 2 * kAttnWaves;
 constexpr float kLowest = -3.402823466e38f;   // start of a running maximum: finite, so that differences from it are no NaN
 constexpr float kSlack = 8.f;                 // scores (base 2) may pass the running maximum by this before everything is rescaled
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -53,6 +54,12 @@ __device__ __forceinline__ u32x4_t decode8(const Centroids& c, uint32_t w) {
 // The same from a table of all pairs in shared memory: a byte's two indices are a register's two bf16, in their order.
 __device__ __forceinline__ u32x4_t decode8_table(const uint32_t* table, uint32_t w) {
     return u32x4_t{table[w & 0xFFu], table[w >> 8 & 0xFFu], table[w >> 16 & 0xFFu], table[w >> 24]};
+}
+// Of V, whose bytes hold elements d and d + 16 of a token: tokens side by side, as decode8 leaves them.
+__device__ __forceinline__ u32x4_t decode8_table_of_v(const uint32_t* table, uint32_t w) {
+    const u32x4_t r = decode8_table(table, w);
+    return u32x4_t{__builtin_amdgcn_perm(r[1], r[0], 0x05040100u), __builtin_amdgcn_perm(r[3], r[2], 0x05040100u),
+                   __builtin_amdgcn_perm(r[1], r[0], 0x07060302u), __builtin_amdgcn_perm(r[3], r[2], 0x07060302u)};
 }
 // Eight bf16 in the order in which decode8 leaves a dword's indices: even ones, then odd ones.
 __device__ __forceinline__ u32x4_t even_odd(u32x4_t v) {
@@ -274,9 +281,9 @@ struct Running {
 };
 
 // Few columns a sequence (single tokens, drafts): a workgroup takes 16 columns, and its waves take the steps in turn.  A wave reads
-// and decodes for itself, K by a table of index pairs in shared memory, V by byte permutes from registers: either way alone
-// keeps its unit busier than the memory (16 contexts of 32768 tokens: 134 us so, 151 by permutes alone, before the
-// accumulators were kept out of the second register file, which took it to 113).
+// and decodes for itself, K and half of V by tables of index pairs in shared memory, the other half of V by byte permutes from
+// registers: any more of one alone keeps its unit busier than the memory (16 contexts of 32768 tokens: 112 us so, 121 with K alone by
+// the table, 118 with all of V too; nothing by it 151, when K alone took 134).
 template <int D>
 __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     constexpr int NB = D / KMQ_BLOCK, DT = D / 16;
@@ -285,7 +292,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     const KvBatchArgs& b = a.batch;
     constexpr int DC = D < 128 ? D : 128;            // elements joined at a time
     __shared__ float part[kAttnWaves][kAttnColumns][DC + 4];
-    __shared__ uint32_t table[256];
+    __shared__ uint32_t table[2][256];                // pairs of centroids of K, and of V
     __shared__ float stat[2][kAttnWaves][kAttnColumns];
 
     const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
@@ -324,7 +331,11 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
         if (live) v = *reinterpret_cast<const u32x4_t*>(a.q + row * a.q_stride + static_cast<int64_t>(qh) * D + s / 2 * 64 + quarter * 16 + s % 2 * 8);
         q[s] = v;
     }
-    table[threadIdx.x] = a.cache.codebooks[threadIdx.x & 15] | static_cast<uint32_t>(a.cache.codebooks[threadIdx.x >> 4]) << 16;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+        const uint16_t* book = a.cache.codebooks + kv * kKvCentroids;
+        table[kv][threadIdx.x] = book[threadIdx.x & 15] | static_cast<uint32_t>(book[threadIdx.x >> 4]) << 16;
+    }
     __syncthreads();
     const Centroids cv = load_centroids(a.cache.codebooks + kKvCentroids);
     const float scale = a.scale * kLog2e;
@@ -358,7 +369,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const uint32_t w = now.k[t][2 * n + j];
-                    acc = mfma(decode8_table(table, w), q[2 * n + j], acc);
+                    acc = mfma(decode8_table(table[0], w), q[2 * n + j], acc);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[e] = fmaf(acc[e], kv_half(now.sc[t][n * 2 + e / 2], e % 2), sum[e]);
@@ -388,7 +399,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
             if (masked) clear_unseen(p, s[0]);
 #pragma unroll
             for (int j = 2 * n; j < 2 * n + 2; ++j) {
-                const u32x4_t x = decode8(cv, vw[0][j]), y = decode8(cv, vw[1][j]);
+                const u32x4_t x = decode8_table_of_v(table[1], vw[0][j]), y = decode8(cv, vw[1][j]);
                 o[0][2 * j] = mfma(u32x4_t{x[0], x[1], y[0], y[1]}, p, o[0][2 * j]);
                 o[0][2 * j + 1] = mfma(u32x4_t{x[2], x[3], y[2], y[3]}, p, o[0][2 * j + 1]);
             }
@@ -769,29 +780,25 @@ static int64_t column_tiles(const KvBatchArgs& b, int group, int columns) {
     return kv_pieces(b.rows, b.sequences, columns, group, columns - 1);
 }
 
-#ifndef TARGET
-#define TARGET 768
-#endif
-#ifndef TTARGET
-#define TTARGET 512
-#endif
-#ifndef CT1
-#define CT1 2
-#endif
-#ifndef TW64
-#define TW64 4
-#endif
-template <int D> constexpr int kTileWaves = D == 64 ? TW64 : 8;
-template <int D> constexpr int kColumnTiles = D == 256 ? 1 : CT1;      // of 16 columns a wave: what its registers hold
+template <int D> constexpr int kTileWaves = D == 64 ? 4 : 8;
+template <int D> constexpr int kColumnTiles = D == 256 ? 1 : 2;        // of 16 columns a wave: what its registers hold
 template <int D> constexpr int kTileColumns = kTileWaves<D> * 16 * kColumnTiles<D>;
 static int tile_columns(int D) { return D == 64 ? kTileColumns<64> : D == 128 ? kTileColumns<128> : kTileColumns<256>; }
+
+// Which kernel, and into how many parts the tokens go.  More than 32 columns a sequence on average go to the tiles: (measured, us,
+// tiles / turns of waves) 2 x 512 rows of 32 heads, 64 elements, window 4096: 75 / 106; 4096 rows, 128 elements: 211 / 419.
+// Parts: as many workgroups as the compute units hold at once (three of the waves' turns a unit, two where the head is wide; of the tiles
+// two); more would begin when the first end (131071 tokens, 8 key heads: 96 parts 42, 192 parts 50).  But sequences of
+// different lengths end at different times: where their parts are long, twice as many (16 x 32768 tokens: 6 parts 115, 12 parts 107).
 AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
     const int group = q_heads / c.kv_heads;
     const bool wide = b.rows * group > static_cast<int64_t>(32) * b.sequences;
     AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? tile_columns(c.head_dim) : kAttnColumns, 1, 0};
     const int64_t items = column_tiles(b, group, p.columns) * c.kv_heads;
     const int64_t steps = static_cast<int64_t>(b.table_width) * (c.page_size / kKvStep);
-    int64_t splits = ((wide ? TTARGET : TARGET) + items - 1) / (items > 0 ? items : 1);
+    const int64_t at_once = 256 * (wide || c.head_dim == 256 ? 2 : 3);
+    int64_t splits = (at_once + items - 1) / (items > 0 ? items : 1);
+    if (!wide && b.sequences > 1 && steps >= 96 * splits) splits *= 2;
     const int64_t most = (steps + kAttnMinSteps - 1) / kAttnMinSteps;
     if (splits > most) splits = most;
     if (splits > kAttnThreads) splits = kAttnThreads;              // (the joining kernel has a thread a part)
