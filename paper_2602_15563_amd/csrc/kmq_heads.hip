@@ -245,52 +245,83 @@ __global__ void __launch_bounds__(kHeadThreads, HW) heads_kernel(HeadsArgs a, Kv
     const int sub = lane % LANES, d0 = sub * 8;
     const bool inside = d0 < D;
     const int half = a.rotary_dim / 2;
-    const bool split = !a.interleaved && inside && d0 < a.rotary_dim;
-    const int other = d0 < half ? d0 + half : d0 - half;
+    const bool turned = inside && d0 < a.rotary_dim;
+    const int partner = (lane + (turned ? (d0 < half ? half : -half) / 8 : 0)) * 4;      // the lane of the split form's partners, as a byte address
     const double mean = 1.0 / D;
     // units: query heads of every row, key heads of every row, then values, of all rows at once
     const int nq = (a.q_heads + kHeads - 1) / kHeads, nk = (a.k_heads + kHeads - 1) / kHeads, nv = (a.v_heads + kHeads - 1) / kHeads;
     const int qk_units = ROWS * (nq + nk), units = qk_units + nv;
     const int begin = static_cast<int>(blockIdx.y) * units_per_group, end = begin + units_per_group < units ? begin + units_per_group : units;
+    struct Unit {
+        int row, kind, head;
+        bool live;
+    };
+    const auto unit = [&](int u) __attribute__((always_inline)) {
+        const int r = ROWS == 1 ? 0 : u / (nq + nk), in_row = u - r * (nq + nk), kind = in_row < nq ? 0 : 1;
+        const int h = (kind ? in_row - nq : in_row) * kHeads + lane / LANES;
+        return Unit{r, kind, h, inside && h < (kind ? a.k_heads : a.q_heads) && (have >> r & 1u)};
+    };
+    const auto read = [&](const Unit& w) __attribute__((always_inline)) {
+        const int64_t row = first + w.row;
+        const uint16_t* src = (w.kind ? a.k + row * a.k_stride : a.q + row * a.q_stride) + static_cast<int64_t>(w.head) * D;
+        u32x4_t v = {0, 0, 0, 0};
+        if (w.live) v = *reinterpret_cast<const u32x4_t*>(src + d0);
+        return v;
+    };
     Factors f;
     int factors_of = -1;                                  // the row and kind that f belongs to
-    for (int u = begin + wave; u < end; u += kHeadWaves) {
-        if (u < qk_units) {
-            const int r = ROWS == 1 ? 0 : u / (nq + nk), in_row = u - r * (nq + nk);
-            const int kind = in_row < nq ? 0 : 1;
-            if (!(have >> r & 1u)) continue;
-            const int h = (kind ? in_row - nq : in_row) * kHeads + lane / LANES;
-            const bool live = inside && h < (kind ? a.k_heads : a.q_heads);
-            const int64_t row = first + r;
-            const uint16_t* src = (kind ? a.k + row * a.k_stride : a.q + row * a.q_stride) + static_cast<int64_t>(h) * D;
-            u32x4_t own = {0, 0, 0, 0}, far = {0, 0, 0, 0};
-            if (live) own = *reinterpret_cast<const u32x4_t*>(src + d0);
-            if constexpr (TURNS) {
-                if (live && split) far = *reinterpret_cast<const u32x4_t*>(src + other);
-                if (factors_of != 2 * r + kind) {
-                    factors_of = 2 * r + kind;
-                    f = make_factors(a, !a.norm ? nullptr : kind ? a.k_gain : a.q_gain, angles[r], d0, inside);
+    int u = begin + wave;
+    const int qk_end = end < qk_units ? end : qk_units;
+    if (u < qk_end) {
+        Unit w = unit(u);
+        u32x4_t own = read(w);
+#pragma unroll 1
+        for (; u < qk_end; u += kHeadWaves) {
+            const Unit next = unit(u + kHeadWaves);
+            u32x4_t coming = {0, 0, 0, 0};
+            if (u + kHeadWaves < qk_end) coming = read(next);
+            if (have >> w.row & 1u) {
+                if constexpr (TURNS) {
+                    u32x4_t far = {0, 0, 0, 0};
+                    if (!a.interleaved && a.rotary_dim) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t v = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(partner, static_cast<int>(own[e])));
+                            far[e] = turned ? v : 0u;
+                        }
+                    }
+                    if (factors_of != 2 * w.row + w.kind) {
+                        factors_of = 2 * w.row + w.kind;
+                        f = make_factors(a, !a.norm ? nullptr : w.kind ? a.k_gain : a.q_gain, angles[w.row], d0, inside);
+                    }
+                    own = turn_head<LANES>(a, f, own, far, turned, mean);
                 }
-                own = turn_head<LANES>(a, f, own, far, inside && d0 < a.rotary_dim, mean);
+                uint16_t* out = w.kind ? a.k_out : a.q_out;
+                if (out) {
+                    if (w.live) *reinterpret_cast<u32x4_t*>(out + (first + w.row) * (w.kind ? a.k_out_stride : a.q_out_stride) + static_cast<int64_t>(w.head) * D + d0) = own;
+                } else {
+                    uint32_t scale;
+                    const uint32_t word = quantise8(own, boundary[0], threshold[wave], scale);
+                    if (w.live && to.page_tile) store_k(to.page_tile + w.head * head_bytes, D, to.token + w.row, d0, word, scale);
+                }
             }
-            uint16_t* out = kind ? a.k_out : a.q_out;
-            if (out) {
-                if (live) *reinterpret_cast<u32x4_t*>(out + row * (kind ? a.k_out_stride : a.q_out_stride) + static_cast<int64_t>(h) * D + d0) = own;
-                continue;
-            }
-            uint32_t scale;
-            const uint32_t word = quantise8(own, boundary[0], threshold[wave], scale);
-            if (live && to.page_tile) store_k(to.page_tile + h * head_bytes, D, to.token + r, d0, word, scale);
-        } else {
+            w = next;
+            own = coming;
+        }
+    }
+    {
+        for (; u < end; u += kHeadWaves) {
             const int h = (u - qk_units) * kHeads + lane / LANES;
             const bool live = inside && h < a.v_heads;
             uint32_t bytes[ROWS], scale[ROWS];
+            u32x4_t x[ROWS];
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
-                u32x4_t x = {0, 0, 0, 0};
-                if (live && (have >> r & 1u)) x = *reinterpret_cast<const u32x4_t*>(a.v + (first + r) * a.v_stride + static_cast<int64_t>(h) * D + d0);
-                bytes[r] = v_bytes(quantise8(x, boundary[1], threshold[wave], scale[r]), d0);
+                x[r] = u32x4_t{0, 0, 0, 0};
+                if (live && (have >> r & 1u)) x[r] = *reinterpret_cast<const u32x4_t*>(a.v + (first + r) * a.v_stride + static_cast<int64_t>(h) * D + d0);
             }
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) bytes[r] = v_bytes(quantise8(x[r], boundary[1], threshold[wave], scale[r]), d0);
             if (!live || !to.page_tile) continue;
             uint8_t* tile = to.page_tile + h * head_bytes;
             const int v0 = kv_v_byte(D, to.token, v_first(d0)), step = D / 8;
