@@ -18,9 +18,6 @@
 namespace kmq {
 
 constexpr int kHeadThreads = 256, kHeadWaves = kHeadThreads / kWave;
-#ifndef HW
-#define HW 4
-#endif
 
 template <int CTRL>
 __device__ __forceinline__ double dpp_move64(double v) {
@@ -197,7 +194,7 @@ __device__ __forceinline__ int v_first(int d0) { return (d0 & ~16) + (d0 & 16 ? 
 // LANES lanes hold a head, 8 elements each; a head never crosses a wave.  ROWS = 1: a workgroup takes a row, or with few rows a
 // part of its heads.  ROWS = 4 (cached): the rows of four tokens that share V's dwords, of one sequence.
 template <int LANES, int ROWS, bool TURNS>
-__global__ void __launch_bounds__(kHeadThreads, HW) heads_kernel(HeadsArgs a, KvCacheArgs c, KvBatchArgs b, bool cached, int units_per_group) {
+__global__ void __launch_bounds__(kHeadThreads, 4) heads_kernel(HeadsArgs a, KvCacheArgs c, KvBatchArgs b, bool cached, int units_per_group) {
     constexpr int kHeads = kWave / LANES;                 // heads of a unit: what a wave takes at once
     __shared__ double2 angles[ROWS][LANES * 4 + 1];        // a head has LANES * 8 elements at most
     __shared__ float boundary[2][kKvCentroids], threshold[kHeadWaves][8 * 16];
@@ -212,22 +209,53 @@ __global__ void __launch_bounds__(kHeadThreads, HW) heads_kernel(HeadsArgs a, Kv
         first = blockIdx.x;
         if (cached) at = kv_find_row(b, first);
         if (at.seq < 0) return;                           // (the same for the whole workgroup)
-    } else {
+    } else if (cached) {
         const KvGroup g = kv_find_group(b, static_cast<int>(blockIdx.x));
         if (g.seq < 0) return;
         first = g.row;
         have = g.have;
         at = {g.seq, g.pos};
+    } else {
+        first = static_cast<int64_t>(blockIdx.x) * ROWS;
+        have = a.rows - first >= ROWS ? 15u : (1u << (a.rows - first)) - 1u;
     }
-    const int pairs = a.rotary_dim / 2;
+    const int sub = lane % LANES, d0 = sub * 8;
+    const bool inside = d0 < D;
+    const int pairs = a.rotary_dim / 2, half = pairs;
+    const bool turned = inside && d0 < a.rotary_dim;
+    const int partner = (lane + (turned ? (d0 < half ? half : -half) / 8 : 0)) * 4;      // the lane of the split form's partners, as a byte address
+
+    // units: what a wave takes at once.  Query and key heads of a row: ROWS = 4: a wave takes the units of its row one after the other,
+    // ROWS = 1: they are dealt to the waves in turn.  Then values, of all rows at once.
+    const int nq = (a.q_heads + kHeads - 1) / kHeads, nk = (a.k_heads + kHeads - 1) / kHeads, nv = (a.v_heads + kHeads - 1) / kHeads;
+    const int units = nq + nk + nv, stride = ROWS == 1 ? kHeadWaves : 1;
+    const int begin = static_cast<int>(blockIdx.y) * units_per_group, end = begin + units_per_group < units ? begin + units_per_group : units;
+    const int r = ROWS == 1 ? 0 : wave;                   // this wave's row of queries and keys
+    const bool mine = have >> r & 1u;
+    const int qk_end = !mine ? 0 : end < nq + nk ? end : nq + nk;
+    const int64_t row = first + r;
+    const auto head_of = [&](int u) __attribute__((always_inline)) { return (u < nq ? u : u - nq) * kHeads + lane / LANES; };
+    const auto read = [&](int u) __attribute__((always_inline)) {
+        const int h = head_of(u);
+        u32x4_t v = {0, 0, 0, 0};
+        if (u < qk_end && inside && h < (u < nq ? a.q_heads : a.k_heads))
+            v = *reinterpret_cast<const u32x4_t*>((u < nq ? a.q + row * a.q_stride : a.k + row * a.k_stride) + static_cast<int64_t>(h) * D + d0);
+        return v;
+    };
+    int u = begin + (ROWS == 1 ? wave : 0);
+    u32x4_t own = read(u);                                // asked for before the angles are computed
+
     if (TURNS && pairs) {
-        for (int i = tid; i < ROWS * pairs; i += kHeadThreads) {
-            const int r = ROWS == 1 ? 0 : i / pairs, p = i - r * pairs;
-            if (!(have >> r & 1u)) continue;
-            const double pos = a.positions ? static_cast<double>(a.positions[first + r]) : static_cast<double>(at.pos + r);
+        const auto angle = [&](int of, int p) __attribute__((always_inline)) {
+            const double pos = a.positions ? static_cast<double>(a.positions[first + of]) : static_cast<double>(at.pos + of);
             double2 t;
             sincos(pos * static_cast<double>(a.inv_freq[p]), &t.y, &t.x);
-            angles[r][p] = t;
+            angles[of][p] = t;
+        };
+        if constexpr (ROWS == 1) {
+            for (int p = tid; p < pairs; p += kHeadThreads) angle(0, p);
+        } else if (mine) {
+            for (int p = lane; p < pairs; p += kWave) angle(r, p);
         }
     }
     if (TURNS && tid < ROWS) angles[tid][pairs] = double2{1.0, 0.0};
@@ -237,81 +265,48 @@ __global__ void __launch_bounds__(kHeadThreads, HW) heads_kernel(HeadsArgs a, Kv
         const int level = 31 - __clz(i | 1), j = (2 * (i - (1 << level)) + 1) * (8 >> level) - 1;      // node i of the tree is boundary j
         boundary[kv][i] = i ? (bf16_to_f32(book[j]) + bf16_to_f32(book[j + 1])) * 0.5f : 0.f;
     }
-    __syncthreads();
-
     Target to = {nullptr, 0};
     if (cached) to = target_of(c, b, D, at);
     const int64_t head_bytes = cached ? static_cast<int64_t>(c.page_size / kKvTile) * kv_tile_bytes(D) : 0;
-    const int sub = lane % LANES, d0 = sub * 8;
-    const bool inside = d0 < D;
-    const int half = a.rotary_dim / 2;
-    const bool turned = inside && d0 < a.rotary_dim;
-    const int partner = (lane + (turned ? (d0 < half ? half : -half) / 8 : 0)) * 4;      // the lane of the split form's partners, as a byte address
     const double mean = 1.0 / D;
-    // units: query heads of every row, key heads of every row, then values, of all rows at once
-    const int nq = (a.q_heads + kHeads - 1) / kHeads, nk = (a.k_heads + kHeads - 1) / kHeads, nv = (a.v_heads + kHeads - 1) / kHeads;
-    const int qk_units = ROWS * (nq + nk), units = qk_units + nv;
-    const int begin = static_cast<int>(blockIdx.y) * units_per_group, end = begin + units_per_group < units ? begin + units_per_group : units;
-    struct Unit {
-        int row, kind, head;
-        bool live;
-    };
-    const auto unit = [&](int u) __attribute__((always_inline)) {
-        const int r = ROWS == 1 ? 0 : u / (nq + nk), in_row = u - r * (nq + nk), kind = in_row < nq ? 0 : 1;
-        const int h = (kind ? in_row - nq : in_row) * kHeads + lane / LANES;
-        return Unit{r, kind, h, inside && h < (kind ? a.k_heads : a.q_heads) && (have >> r & 1u)};
-    };
-    const auto read = [&](const Unit& w) __attribute__((always_inline)) {
-        const int64_t row = first + w.row;
-        const uint16_t* src = (w.kind ? a.k + row * a.k_stride : a.q + row * a.q_stride) + static_cast<int64_t>(w.head) * D;
-        u32x4_t v = {0, 0, 0, 0};
-        if (w.live) v = *reinterpret_cast<const u32x4_t*>(src + d0);
-        return v;
-    };
+    __syncthreads();
+
     Factors f;
-    int factors_of = -1;                                  // the row and kind that f belongs to
-    int u = begin + wave;
-    const int qk_end = end < qk_units ? end : qk_units;
-    if (u < qk_end) {
-        Unit w = unit(u);
-        u32x4_t own = read(w);
+    int factors_of = -1;                                  // the kind that f belongs to
 #pragma unroll 1
-        for (; u < qk_end; u += kHeadWaves) {
-            const Unit next = unit(u + kHeadWaves);
-            u32x4_t coming = {0, 0, 0, 0};
-            if (u + kHeadWaves < qk_end) coming = read(next);
-            if (have >> w.row & 1u) {
-                if constexpr (TURNS) {
-                    u32x4_t far = {0, 0, 0, 0};
-                    if (!a.interleaved && a.rotary_dim) {
+    for (; u < qk_end; u += stride) {
+        const u32x4_t coming = read(u + stride);
+        const int kind = u < nq ? 0 : 1, h = head_of(u);
+        const bool live = inside && h < (kind ? a.k_heads : a.q_heads);
+        if constexpr (TURNS) {
+            u32x4_t far = {0, 0, 0, 0};
+            if (!a.interleaved && pairs) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t v = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(partner, static_cast<int>(own[e])));
-                            far[e] = turned ? v : 0u;
-                        }
-                    }
-                    if (factors_of != 2 * w.row + w.kind) {
-                        factors_of = 2 * w.row + w.kind;
-                        f = make_factors(a, !a.norm ? nullptr : w.kind ? a.k_gain : a.q_gain, angles[w.row], d0, inside);
-                    }
-                    own = turn_head<LANES>(a, f, own, far, turned, mean);
-                }
-                uint16_t* out = w.kind ? a.k_out : a.q_out;
-                if (out) {
-                    if (w.live) *reinterpret_cast<u32x4_t*>(out + (first + w.row) * (w.kind ? a.k_out_stride : a.q_out_stride) + static_cast<int64_t>(w.head) * D + d0) = own;
-                } else {
-                    uint32_t scale;
-                    const uint32_t word = quantise8(own, boundary[0], threshold[wave], scale);
-                    if (w.live && to.page_tile) store_k(to.page_tile + w.head * head_bytes, D, to.token + w.row, d0, word, scale);
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t v = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(partner, static_cast<int>(own[e])));
+                    far[e] = turned ? v : 0u;
                 }
             }
-            w = next;
-            own = coming;
+            if (factors_of != kind) {
+                factors_of = kind;
+                f = make_factors(a, !a.norm ? nullptr : kind ? a.k_gain : a.q_gain, angles[r], d0, inside);
+            }
+            own = turn_head<LANES>(a, f, own, far, turned, mean);
         }
+        uint16_t* out = kind ? a.k_out : a.q_out;
+        if (out) {
+            if (live) *reinterpret_cast<u32x4_t*>(out + row * (kind ? a.k_out_stride : a.q_out_stride) + static_cast<int64_t>(h) * D + d0) = own;
+        } else {
+            uint32_t scale;
+            const uint32_t word = quantise8(own, boundary[0], threshold[wave], scale);
+            if (live && to.page_tile) store_k(to.page_tile + h * head_bytes, D, to.token + r, d0, word, scale);
+        }
+        own = coming;
     }
     {
-        for (; u < end; u += kHeadWaves) {
-            const int h = (u - qk_units) * kHeads + lane / LANES;
+        const int lo = begin > nq + nk ? begin : nq + nk;
+        for (int v = lo + ((wave - (lo - begin)) & (kHeadWaves - 1)); v < end; v += kHeadWaves) {
+            const int h = (v - nq - nk) * kHeads + lane / LANES;
             const bool live = inside && h < a.v_heads;
             uint32_t bytes[ROWS], scale[ROWS];
             u32x4_t x[ROWS];
@@ -436,12 +431,13 @@ hipError_t launch_heads(const HeadsArgs& a, const KvCacheArgs* cache, const KvBa
     const int lanes = a.head_dim <= 64 ? 8 : a.head_dim <= 128 ? 16 : a.head_dim <= 256 ? 32 : 64, heads = kWave / lanes;
     const int units = (a.q_heads + heads - 1) / heads + (a.k_heads + heads - 1) / heads + (a.v_heads + heads - 1) / heads;
     const bool turns = a.norm || a.rotary_dim;
-    if (cache && by_groups(b)) {
-        const dim3 grid(static_cast<unsigned>(most_groups(b)));
+    if (cache ? by_groups(b) : a.rows >= 1024) {
+        const dim3 grid(static_cast<unsigned>(cache ? most_groups(b) : (a.rows + 3) / 4));
         switch (lanes) {
-            case 8: start<8, 4>(turns, grid, s, a, c, b, true, 1 << 30); break;
-            case 16: start<16, 4>(turns, grid, s, a, c, b, true, 1 << 30); break;
-            default: start<32, 4>(turns, grid, s, a, c, b, true, 1 << 30); break;
+            case 8: start<8, 4>(turns, grid, s, a, c, b, cache != nullptr, units); break;
+            case 16: start<16, 4>(turns, grid, s, a, c, b, cache != nullptr, units); break;
+            case 32: start<32, 4>(turns, grid, s, a, c, b, cache != nullptr, units); break;
+            default: start<64, 4>(turns, grid, s, a, c, b, cache != nullptr, units); break;
         }
         return hipGetLastError();
     }
