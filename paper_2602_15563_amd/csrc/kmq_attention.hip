@@ -187,18 +187,20 @@ struct Walk {
         steps_per_page = tiles / 2;
         slot = step / steps_per_page;
         within = step - slot * steps_per_page;
-        read();
+        pages = read();
     }
-    __device__ __forceinline__ void read() {
+    __device__ __forceinline__ int read() {
         const int at = slot + (static_cast<int>(threadIdx.x) & (kWave - 1));
         first_slot = slot;
-        int v = at < width ? table[at] : -1;
-        asm volatile("" : "+v"(v));                       // (waited for here, and not wherever the number is used)
-        pages = v;
+        return at < width ? table[at] : -1;
     }
     // The place of the step that the walk stands at (one that is not there reads the first page, and nothing of it is used).
     __device__ __forceinline__ Place place(bool inside) {
-        if (slot - first_slot >= kWave) read();
+        if (slot - first_slot >= kWave) {
+            int v = read();
+            asm volatile("" : "+v"(v));                   // (waited for here, and not wherever the number is used)
+            pages = v;
+        }
         const int page = __builtin_amdgcn_readlane(pages, slot - first_slot);
         const bool there = inside && page >= 0 && page < num_pages;
         return {head_base + (there ? page : 0) * page_stride + static_cast<int64_t>(within) * (2 * 17 * D), there};
@@ -323,6 +325,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
         return;
     }
 
+    // what is read first is asked for together: page numbers, queries, codebooks, and then the first step
+    int step = steps.from + wave;
+    Walk<D> walk(a, tile.seq, head, step);
     // queries as the first product's second operand: lane (column, quarter) holds elements 64 b + 16 quarter + 8 j + e
     u32x4_t q[2 * NB];
 #pragma unroll
@@ -331,13 +336,19 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
         if (live) v = *reinterpret_cast<const u32x4_t*>(a.q + row * a.q_stride + static_cast<int64_t>(qh) * D + s / 2 * 64 + quarter * 16 + s % 2 * 8);
         q[s] = v;
     }
+    uint32_t pairs[2];
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
         const uint16_t* book = a.cache.codebooks + kv * kKvCentroids;
-        table[kv][threadIdx.x] = book[threadIdx.x & 15] | static_cast<uint32_t>(book[threadIdx.x >> 4]) << 16;
+        pairs[kv] = book[threadIdx.x & 15] | static_cast<uint32_t>(book[threadIdx.x >> 4]) << 16;
     }
-    __syncthreads();
     const Centroids cv = load_centroids(a.cache.codebooks + kKvCentroids);
+    Place at = walk.place(step < steps.to);
+    KWords<D> kw;
+    if (step < steps.to) kw.load(at.base, lane, quarter);
+    table[0][threadIdx.x] = pairs[0];
+    table[1][threadIdx.x] = pairs[1];
+    __syncthreads();
     const float scale = a.scale * kLog2e;
 
     f32x4_t o[1][DT];
@@ -345,11 +356,6 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     for (int d = 0; d < DT; ++d) o[0][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     Running<1> run;
 
-    int step = steps.from + wave;
-    Walk<D> walk(a, tile.seq, head, step);
-    Place at = walk.place(step < steps.to);
-    KWords<D> kw;
-    if (step < steps.to) kw.load(at.base, lane, quarter);
     for (; step < steps.to; step += kAttnWaves) {
         uint32_t vw[2][D / 32];
 #pragma unroll
