@@ -197,3 +197,43 @@ def test_a_workspace_larger_than_asked_for_and_one_byte_too_small():
     kmq.kv_attention(c.cache, c.batch, q, 64, out, 64, 1, 0.1, workspace=torch.empty(need + 100, dtype=torch.uint8, device="cuda"))
     torch.cuda.synchronize()
     assert not np.isnan(okv.bf16_value(host(out))).any()
+
+
+@pytest.mark.parametrize("D", (64, 128, 256))
+@pytest.mark.parametrize("window", (0, 700))
+def test_pieces_of_prompts_split_over_workgroups(D, window):
+    """Many rows after a long context: the tokens go into parts, some of which a row does not see."""
+    c, _, _ = check(400 + D, [40, 9], [1500, 900], 64, 1, 3, D, window=window)
+    assert kmq.kernel_name_kv_attention(c.cache, c.batch, 3) == "kv_attention_tile"
+    assert kmq.kv_attention_workspace_bytes(c.cache, c.batch, 3) > 0
+
+
+@pytest.mark.parametrize("group", (1, 3, 7, 16, 20))
+def test_query_heads_a_key_head_in_tiles(group):
+    check(420 + group, [300 // group + 37, 0, 50], [350, 7, 77], 32, 2, group, 64)
+
+
+@pytest.mark.parametrize("rows", (1, 21))
+@pytest.mark.parametrize("window", (0, 900))
+def test_more_pages_than_are_read_at_once(rows, window):
+    """A sequence of 69 pages whose tokens one workgroup walks through: the bits of the same tokens on one long page."""
+    heads, D, pages, n = 96, 64, 69, 8
+    g = torch.Generator(device="cuda").manual_seed(5)
+    small = torch.randint(0, 256, (n * pages, heads, 2, 17 * D), dtype=torch.uint8, device="cuda", generator=g)
+    small[..., 16 * D:] = (0.5 + torch.rand((n * pages, heads, 2, D // 2), device="cuda", generator=g)).to(torch.bfloat16).view(torch.uint8)
+    table = torch.randperm(n * pages, device="cuda", generator=g).to(torch.int32).view(n, pages)
+    long = small[table.long()].permute(0, 2, 1, 3, 4).contiguous()
+    books = dev(np.sort(np.random.default_rng(6).uniform(-1, 1, (2, 16)), axis=1).astype(np.float32).view(np.uint32) >> 16).to(torch.int16)
+    lengths = dev(np.array([2208 - 100 * i for i in range(n)], dtype=np.int32))
+    starts = dev(np.arange(0, n * rows + 1, rows, dtype=np.int32)) if rows > 1 else None
+    q = torch.randn((n * rows, 2 * heads * D), device="cuda", generator=g).to(torch.bfloat16)
+    outs = []
+    for data, per, tab in ((small, 32, table), (long, 32 * pages, torch.arange(n, dtype=torch.int32, device="cuda").view(n, 1))):
+        cache = kmq.KvCache(data, books, data.shape[0], per, heads, D)
+        batch = kmq.KvBatch(tab, lengths, starts, n * rows)
+        assert kmq.kv_attention_workspace_bytes(cache, batch, 2 * heads) == 0                # one part
+        out = torch.zeros_like(q)
+        kmq.kv_attention(cache, batch, q, 2 * heads * D, out, 2 * heads * D, 2 * heads, 0.2, window=window)
+        outs.append(out)
+    torch.cuda.synchronize()
+    assert torch.equal(*outs) and bool(outs[0].isfinite().all()) and float(outs[0].float().abs().mean()) > 1e-3
