@@ -791,14 +791,18 @@ template <int D> constexpr int kColumnTiles = D == 256 ? 1 : 2;        // of 16 
 template <int D> constexpr int kTileColumns = kTileWaves<D> * 16 * kColumnTiles<D>;
 static int tile_columns(int D) { return D == 64 ? kTileColumns<64> : D == 128 ? kTileColumns<128> : kTileColumns<256>; }
 
-// Which kernel, and into how many parts the tokens go.  More than 32 columns a sequence on average go to the tiles: (measured, us,
-// tiles / turns of waves) 2 x 512 rows of 32 heads, 64 elements, window 4096: 75 / 106; 4096 rows, 128 elements: 211 / 419.
+// Which kernel, and into how many parts the tokens go.  The tiles decode a step once for all of their columns and are worth it where they
+// are full: from 384 columns a sequence on, from 128 where there is one sequence alone.  Measured, us, tiles / turns of waves (8 key
+// heads, 8000 tokens, 128 elements): one sequence, 64 columns 22 / 20, 128 columns 25 / 26, 256 columns 35 / 41; eight sequences,
+// 128 columns 108 / 81, 256 columns 160 / 138, 384 columns 197 / 193, 512 columns 253 / 252; 2 x 2048 columns of 64 elements under a
+// window of 4096 75 / 106; a prompt of 16384 columns 210 / 419.
 // Parts: as many workgroups as the compute units hold at once (three of the waves' turns a unit, two where the head is wide; of the tiles
 // two); more would begin when the first end (131071 tokens, 8 key heads: 96 parts 42, 192 parts 50).  But sequences of
 // different lengths end at different times: where their parts are long, twice as many (16 x 32768 tokens: 6 parts 115, 12 parts 107).
 AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
     const int group = q_heads / c.kv_heads;
-    const bool wide = b.rows * group > static_cast<int64_t>(32) * b.sequences;
+    const int64_t columns = b.rows * group;
+    const bool wide = b.sequences == 1 ? columns > 128 : columns > 384 * static_cast<int64_t>(b.sequences);
     AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? tile_columns(c.head_dim) : kAttnColumns, 1, 0};
     const int64_t items = column_tiles(b, group, p.columns) * c.kv_heads;
     const int64_t steps = static_cast<int64_t>(b.table_width) * (c.page_size / kKvStep);

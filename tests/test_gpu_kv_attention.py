@@ -15,9 +15,11 @@ def queries(seed, rows, heads, D, size=1.0):
     return patterns(np.random.default_rng(seed).standard_normal((rows, heads, D)) * size)
 
 
-def check(seed, news, lengths, page, kv_heads, group, D, causal=True, window=0, size=1.0, scale=None, stride=None, lse=True, **more):
+def check(seed, news, lengths, page, kv_heads, group, D, causal=True, window=0, size=1.0, scale=None, stride=None, lse=True, tiles=None, **more):
     print(f"attention seed={seed} news={news[:8]} lengths={lengths[:8]} page={page} kv={kv_heads} group={group} D={D} causal={causal} window={window}", flush=True)
     c = Case(seed, news, lengths, page, kv_heads, D, **more).to_device()
+    if tiles is not None:                                        # the case is meant for one of the two kernels
+        assert (kmq.kernel_name_kv_attention(c.cache, c.batch, kv_heads * group) == "kv_attention_tile") == tiles
     q = queries(seed + 1, c.rows, kv_heads * group, D, size)
     return c, q, check_attention(c, q, D ** -0.5 if scale is None else scale, causal, window, stride=stride, lse=lse, label=f"seed {seed}")
 
@@ -37,7 +39,8 @@ def test_query_heads_a_key_head(group, n):
 @pytest.mark.parametrize("D", (64, 128, 256))
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 40), (False, 33), (True, 5000)])
 def test_rows_of_a_prompt(D, causal, window):
-    check(200 + D + window, [150, 70], [150, 190], 32, 2, 2, D, causal, window)
+    check(200 + D + window, [150, 70], [150, 190], 32, 2, 4, D, causal, window, tiles=True)
+    check(250 + D + window, [50, 20], [50, 90], 32, 2, 2, D, causal, window, tiles=False)
 
 
 @pytest.mark.parametrize("causal", (True, False))
@@ -45,10 +48,12 @@ def test_rows_that_see_nothing(causal):
     """Empty sequences, more rows than tokens, and lengths of zero: rows of zeros."""
     check(300, [3, 0, 5, 1], [0, 10, 3, 1], 32, 2, 2, 64, causal)
     check(301, [1, 1], [0, 4], 32, 1, 4, 128, causal, starts=False)
+    check(309, [130, 0, 60], [0, 10, 40], 32, 2, 8, 64, causal, tiles=True)
 
 
 def test_rows_behind_the_last_sequence_and_strides():
     check(302, [4, 20], [40, 20], 32, 2, 2, 128, behind=9, stride=4 * 128 + 40)
+    check(308, [100, 130], [140, 130], 32, 2, 4, 128, behind=9, stride=8 * 128 + 40, tiles=True)
     check(303, [1, 1, 1], [400, 1, 77], 32, 2, 2, 64, behind=40, stride=4 * 64 + 8)
 
 
@@ -58,7 +63,7 @@ def test_without_log_sum_exp():
 
 def test_pages_that_are_none():
     """Tokens on pages that the table does not have are passed over; so is what lies beyond the table."""
-    for seed, news in ((305, [40]), (306, [1])):
+    for seed, news in ((305, [80]), (306, [1])):
         c = Case(seed, news, [200], 32, 2, 128)
         c.table[0, 1], c.table[0, 5] = -1, c.num_pages
         c.to_device()
@@ -88,7 +93,8 @@ def test_many_sequences():
 @pytest.mark.parametrize("size", (0.0, 8.0, 60.0))
 def test_flat_and_peaked_scores(size):
     """Queries of zeros (the mean of the values), and scores so far apart that one token takes all."""
-    check(330, [20], [300], 32, 2, 2, 128, size=size)
+    check(330, [80], [300], 32, 2, 2, 128, size=size, tiles=True)
+    check(329, [20], [300], 32, 2, 2, 128, size=size, tiles=False)
     check(331, [1], [700], 32, 2, 4, 128, size=size)
 
 
@@ -97,7 +103,7 @@ def test_negative_and_zero_scale():
     check(333, [5], [80], 32, 1, 2, 64, scale=0.0)
 
 
-@pytest.mark.parametrize("n", (1, 30))
+@pytest.mark.parametrize("n", (1, 70))
 def test_maxima_that_grow_and_fall(n):
     """Keys whose scores rise along the tokens (every step a new maximum) and fall (none after the first)."""
     for order in (1, -1):
@@ -152,7 +158,7 @@ def test_a_nan_query_stays_in_its_row():
 
 
 def test_the_same_call_twice_gives_the_same_bits():
-    for news, lengths in (([1, 1], [2000, 900]), ([100, 3], [150, 700])):
+    for news, lengths in (([1, 1], [2000, 900]), ([250, 3], [300, 700])):
         c = Case(370, news, lengths, 64, 2, 128).to_device()
         q = queries(371, c.rows, 8, 128)
         first = run_attention(c, q, 8, 0.09)
@@ -169,8 +175,8 @@ def test_one_token_decides(D, n):
     g = np.random.default_rng(381)
     direction = np.where(g.random(D) < 0.5, -1.0, 1.0)
     values = patterns(g.standard_normal((tokens, 1, D)))
-    q = patterns(np.tile(direction, (n, 1, 1)))
-    for hot in range(tokens - n + 1 if n == 1 else tokens - n + 1):
+    q = patterns(np.tile(direction, (n, 4, 1)))
+    for hot in range(tokens - n + 1):
         for p in range(tokens):
             page, token = okv.place(c.table[0], 32, c.num_pages, p)
             c.pages.write(page, token, patterns(direction * (30.0 if p == hot else -30.0)).reshape(1, D), values[p], c.books)
@@ -203,17 +209,17 @@ def test_a_workspace_larger_than_asked_for_and_one_byte_too_small():
 @pytest.mark.parametrize("window", (0, 700))
 def test_pieces_of_prompts_split_over_workgroups(D, window):
     """Many rows after a long context: the tokens go into parts, some of which a row does not see."""
-    c, _, _ = check(400 + D, [40, 9], [1500, 900], 64, 1, 3, D, window=window)
-    assert kmq.kernel_name_kv_attention(c.cache, c.batch, 3) == "kv_attention_tile"
+    c, _, _ = check(400 + D, [250, 60], [1500, 900], 64, 1, 3, D, window=window, tiles=True)
     assert kmq.kv_attention_workspace_bytes(c.cache, c.batch, 3) > 0
 
 
 @pytest.mark.parametrize("group", (1, 3, 7, 16, 20))
 def test_query_heads_a_key_head_in_tiles(group):
-    check(420 + group, [300 // group + 37, 0, 50], [350, 7, 77], 32, 2, group, 64)
+    n = 1200 // group + 37
+    check(420 + group, [n, 0, 50], [n + 13, 7, 77], 32, 1, group, 64, tiles=True)
 
 
-@pytest.mark.parametrize("rows", (1, 21))
+@pytest.mark.parametrize("rows", (1, 21, 200))
 @pytest.mark.parametrize("window", (0, 900))
 def test_more_pages_than_are_read_at_once(rows, window):
     """A sequence of 69 pages whose tokens one workgroup walks through: the bits of the same tokens on one long page."""
