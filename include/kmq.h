@@ -422,7 +422,10 @@ kmq_status kmq_kv_append(const kmq_kv_cache* cache, const kmq_kv_batch* batch, c
  *   lse        rows x q_heads fp32, log sum_j exp(S_j) (minus infinity where none is seen), or NULL
  *   workspace  kmq_kv_attention_workspace_bytes() bytes, 16-byte aligned, not initialised: where the rows are too few to fill the
  *              compute units, the tokens are split over workgroups, and a second kernel joins the parts in their order
- * The size depends on the structures' numbers alone, not on lengths, so a captured call may be replayed with others. */
+ * The size depends on the structures' numbers alone, not on lengths, so a captured call may be replayed with others; 0 on bad
+ * arguments.  Tokens that no row sees, and what lies behind a sequence, may hold anything, NaN and infinities too.
+ * KMQ_ERR_SHAPE: q_heads no multiple of kv_heads, rows * q_heads > 2^30, more than 2^22 workgroups (sequences, or 16 (row, query head)
+ * pairs of a sequence and a key head, times kv_heads), scale not finite, window < 0. */
 size_t kmq_kv_attention_workspace_bytes(const kmq_kv_cache* cache, const kmq_kv_batch* batch, int q_heads);
 kmq_status kmq_kv_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch, const uint16_t* q, int64_t q_stride, int q_heads,
                             float scale, int causal, int window, uint16_t* out, int64_t out_stride, float* lse,

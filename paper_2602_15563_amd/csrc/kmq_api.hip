@@ -547,9 +547,9 @@ kmq_status kmq_kv_append(const kmq_kv_cache* cache, const kmq_kv_batch* batch, c
     return kmq::hip_status(kmq::launch_heads(a, &ca, &ba, static_cast<hipStream_t>(hip_stream)));
 }
 
-// The shapes an attention can have: (rows, query heads) pairs and their partial results are counted in 64 bits, workgroups in 31.
 static kmq_status check_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch, int q_heads) {
     if (q_heads < 1 || q_heads > kmq::kMaxHeads || q_heads % cache->kv_heads || batch->rows * q_heads > (int64_t(1) << 30)) return KMQ_ERR_SHAPE;
+    if (kmq::attention_plan(kmq::cache_args(cache), kmq::batch_args(batch), q_heads).workgroups > kmq::kMaxAttentionWorkgroups) return KMQ_ERR_SHAPE;
     return KMQ_OK;
 }
 

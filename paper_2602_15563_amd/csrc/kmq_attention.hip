@@ -803,8 +803,8 @@ AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_h
     const int group = q_heads / c.kv_heads;
     const int64_t columns = b.rows * group;
     const bool wide = b.sequences == 1 ? columns > 128 : columns > 384 * static_cast<int64_t>(b.sequences);
-    AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? tile_columns(c.head_dim) : kAttnColumns, 1, 0};
-    const int64_t items = column_tiles(b, group, p.columns) * c.kv_heads;
+    AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? tile_columns(c.head_dim) : kAttnColumns, 1, 0, 0};
+    const int64_t items = p.workgroups = column_tiles(b, group, p.columns) * c.kv_heads;
     const int64_t steps = static_cast<int64_t>(b.table_width) * (c.page_size / kKvStep);
     const int64_t at_once = 256 * (wide || c.head_dim == 256 ? 2 : 3);
     int64_t splits = (at_once + items - 1) / (items > 0 ? items : 1);
@@ -822,8 +822,7 @@ AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_h
 template <int D>
 static hipError_t launch_attn(const AttnArgs& A, const AttentionPlan& p, hipStream_t s) {
     const KvBatchArgs& b = A.a.batch;
-    const int64_t items = column_tiles(b, A.a.q_heads / A.a.cache.kv_heads, p.columns) * A.a.cache.kv_heads;
-    const dim3 grid(static_cast<unsigned>(items), static_cast<unsigned>(A.splits));
+    const dim3 grid(static_cast<unsigned>(p.workgroups), static_cast<unsigned>(A.splits));
     if (p.columns == kAttnColumns) attn_kernel<D><<<grid, kAttnThreads, 0, s>>>(A);
     else attn_tile_kernel<D, kColumnTiles<D>, kTileWaves<D>><<<grid, kTileWaves<D> * kWave, 0, s>>>(A);
     const hipError_t e = hipGetLastError();

@@ -161,7 +161,9 @@ struct AttentionPlan {
     int columns;                         // (row, query head) pairs a workgroup takes
     int splits;                          // parts of the tokens, joined by a second kernel
     size_t workspace_bytes;
+    int64_t workgroups;                  // a part
 };
+constexpr int64_t kMaxAttentionWorkgroups = int64_t(1) << 22;    // (threads of a launch are counted in 32 bits: 512 of them each, and a factor of two)
 AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads);
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t s);
 

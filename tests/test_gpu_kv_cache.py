@@ -219,3 +219,21 @@ def test_many_rows_appended(i, interleaved):
         c.pages.write(page_, token, turned[1][r], x[r, nq + heads:], c.books)
     c.check_pages()
     assert np.array_equal(host(q)[:end].reshape(end, nq, D), turned[0][:end]) and (host(q)[end:] == NAN16).all()
+
+
+@pytest.mark.parametrize("news,lengths", [([1, 1], [9, 40]), ([70, 33], [70, 50])])
+def test_queries_appended_in_place(news, lengths):
+    """The queries' own places as their output: what a separate output gives, and keys and values stay as they were."""
+    g = np.random.default_rng(500)
+    x = patterns(g.standard_normal((sum(news), 10, 64)))
+    freq = dev((10000.0 ** (-np.arange(0, 64, 2) / 64)).astype(np.float32))
+    results = []
+    for own in (False, True):
+        c = Case(501, news, lengths, 32, 2, 64).to_device()
+        xd = dev(x.reshape(len(x), 640))
+        q, stride = (xd, 640) if own else (torch.zeros((len(x), 384), dtype=torch.int16, device="cuda"), 384)
+        kmq.kv_append(c.cache, c.batch, xd, 640, q, stride, 6, inv_freq=freq, rotary_dim=64, rmsnorm=True, eps=1e-6)
+        torch.cuda.synchronize()
+        results.append((host(q)[:, :384], c.pages_d))
+        assert np.array_equal(host(xd)[:, 384:], x.reshape(len(x), 640)[:, 384:])
+    assert np.array_equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])

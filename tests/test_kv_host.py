@@ -113,6 +113,10 @@ def test_attention():
         assert attend(**bad) == SHAPE, bad
     for bad in (dict(q=A + 8), dict(out=A + 2), dict(lse=A + 2)):
         assert attend(**bad) == ALIGN, bad
+    wide = dict(c=cache(heads=4096), nq=4096, qs=1 << 18, os=1 << 18)                # more workgroups than a launch takes
+    assert attend(b=batch(rows=1 << 18, sequences=1 << 18, starts=None), **wide) == SHAPE
+    assert attend(b=batch(rows=1024, sequences=1 << 20), **wide) == SHAPE
+    assert lib.kmq_kv_attention_workspace_bytes(ref(cache(heads=4096)), ref(batch(rows=1024, sequences=1 << 20)), 4096) == 0
     long = batch(rows=1, sequences=1, width=4096)
     need = lib.kmq_kv_attention_workspace_bytes(ref(cache()), ref(long), 4)
     assert need > 0
