@@ -235,7 +235,7 @@ def _prepare_decoder(case, g):
     def step():
         for l in range(layers):
             kmq.gemv_fused(*Wq[l], hs[l], yq[l], qkv, h, bits, norm_weight=gains[l][0], eps=eps)
-            # attention is not part of this library: its value slice stands in for its output
+            # attention has timed cases of its own (perf/operators.py): here its value slice stands in for its output
             kmq.gemv_fused(*Wo[l], yq[l, qkv - h:], mid[l], h, h, bits, residual=hs[l])
             kmq.gemv_swiglu_rmsnorm(*Wg[l], *Wu[l], mid[l], gains[l][1], eps, ym[l], mlp, h, bits)
             kmq.gemv_fused(*Wd[l], ym[l], hs[l + 1], h, mlp, bits, residual=mid[l])
