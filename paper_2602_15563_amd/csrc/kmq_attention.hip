@@ -285,7 +285,8 @@ struct Running {
 // Few columns a sequence (single tokens, drafts): a workgroup takes 16 columns, and its waves take the steps in turn.  A wave reads
 // and decodes for itself, K and half of V by tables of index pairs in shared memory, the other half of V by byte permutes from
 // registers: any more of one alone keeps its unit busier than the memory (16 contexts of 32768 tokens: 112 us so, 121 with K alone by
-// the table, 118 with all of V too; nothing by it 151, when K alone took 134).
+// the table, 118 with all of V too; nothing by it 151, when K alone took 134).  16 x 32768 tokens take 105 us now, 4.3 TB/s of cache (a copy
+// takes 91): vector issue is busy for 75 % of that and the tables for 67 % (46 % lanes that want the same bank).
 template <int D>
 __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     constexpr int NB = D / KMQ_BLOCK, DT = D / 16;
@@ -469,7 +470,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
 
 // Many columns a sequence (prompts, long drafts): a workgroup takes 16 x CT columns a wave, and its waves decode every step
 // together, an equal share of it each, into shared memory in the order of the first product's and the second product's first operand.
-// Two such buffers: the next step is decoded into one while the products read the other.
+// Two such buffers: the next step is decoded into one while the products read the other.  A prompt of 4096 tokens (32 query heads of
+// 128 elements) takes 211 us, 650 TFLOP/s: vector issue (exponentials, scales, roundings, decode) is busy for 57 % of it and the
+// matrix cores for 28 %, and two waves a unit, which is what the registers allow, seldom overlap them.
 template <int D, int CT, int WAVES>
 __global__ void __launch_bounds__(WAVES * kWave, 2) attn_tile_kernel(AttnArgs A) {
     constexpr int NB = D / KMQ_BLOCK, DT = D / 16, KF = D / 32;

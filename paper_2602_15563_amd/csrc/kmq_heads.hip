@@ -11,6 +11,9 @@
 // multiply and add 64-bit floats at the rate of 32-bit ones.)  With r = 1 / sqrt(..) an element is
 //     y_e = r * (x_e A_e + x_partner B_e),   A_e = gain_e cos,  B_e = +-gain_partner sin,
 // and A and B are the same for all query heads of a row, and for all its key heads: three operations an element.
+//
+// 4001 rows of 64 query and 8 key heads take 39 us, 3.8 TB/s read and written (a copy of them 31).  A write of keys and values alone is
+// bound by vector issue: 10004 rows of 8 + 8 heads 23.5 us, 75 % of it issuing the 17 operations that an element takes.
 #include <type_traits>
 
 #include "kmq_kv.h"
@@ -118,8 +121,8 @@ __device__ __forceinline__ u32x4_t turn_head(const HeadsArgs& a, const Factors& 
 
 // Eight elements of a block of 64 (8 neighbouring lanes) -> their indices in the nibbles of a dword, and the block's scale.
 // `boundary`: the boundaries as a binary tree, node n's children 2 n and 2 n + 1, root 1.  `place`: this wave's thresholds in
-// shared memory, a tree for each of its 8 blocks.  A threshold is b * s rounded down: then x > threshold exactly where x > b * s.  An element walks down the tree, and where it
-// arrives is 16 + its index.
+// shared memory, a tree for each of its 8 blocks.  A threshold is b * s rounded down: then x > threshold exactly where x > b * s.
+// An element walks down the tree, and where it arrives is 16 + its index.
 __device__ __forceinline__ uint32_t quantise8(u32x4_t x, const float* boundary, float* place, uint32_t& scale) {
     typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
     const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), sub = lane & 7;
