@@ -799,9 +799,32 @@ static int tile_columns(int D) { return D == 64 ? kTileColumns<64> : D == 128 ? 
 // heads, 8000 tokens, 128 elements): one sequence, 64 columns 22 / 20, 128 columns 25 / 26, 256 columns 35 / 41; eight sequences,
 // 128 columns 108 / 81, 256 columns 160 / 138, 384 columns 197 / 193, 512 columns 253 / 252; 2 x 2048 columns of 64 elements under a
 // window of 4096 75 / 106; a prompt of 16384 columns 210 / 419.
-// Parts: as many workgroups as the compute units hold at once (three of the waves' turns a unit, two where the head is wide; of the tiles
-// two); more would begin when the first end (131071 tokens, 8 key heads: 96 parts 42, 192 parts 50).  But sequences of
+// Parts of the waves' turns: as many workgroups as the compute units hold at once (three a unit, two where the head is wide); more would
+// begin when the first end (131071 tokens, 8 key heads: 96 parts 42, 192 parts 50).  But sequences of
 // different lengths end at different times: where their parts are long, twice as many (16 x 32768 tokens: 6 parts 115, 12 parts 107).
+// Parts of the tiles: a unit holds one workgroup (three at 64 elements), and what counts is how many turns of them there are and how long
+// each is: turns * (steps of a part + 4 to begin with), and a step for a million elements of the parts' results, written and read.  One
+// more workgroup than the units hold makes it two turns.  us at 8000 tokens and 8 key heads: one sequence of 1600 columns, 4 parts (224
+// workgroups) 108, 5 (280) 149; of 4000 columns 1 / 2 / 4 parts 359 / 196 / 207; two of 2048 and 1536 columns 2 / 3 / 5 parts 195 / 230 /
+// 223; 256 elements, 1500 columns 2 / 3 / 5 / 6 parts 219 / 282 / 192 / 237; 64 elements, 1600 columns 5 / 7 / 8 parts 81 / 65 / 79.
+static int64_t tile_splits(const KvCacheArgs& c, const KvBatchArgs& b, int group, int64_t steps, int64_t most) {
+    const int64_t columns = tile_columns(c.head_dim), at_once = 256 * (c.head_dim == 64 ? 3 : 1);
+    int64_t tiles = (b.rows * group + columns - 1) / columns + b.sequences / 2;     // (half a tile of every sequence without columns)
+    if (tiles > column_tiles(b, group, columns)) tiles = column_tiles(b, group, columns);
+    const int64_t items = tiles * c.kv_heads;
+    int64_t best = 1;
+    double least = 0;
+    for (int64_t parts = 1; parts <= most && (parts == 1 || items * parts <= 4 * at_once); ++parts) {
+        const int64_t turns = (items * parts + at_once - 1) / at_once, own = (steps + parts - 1) / parts;
+        const double cost = static_cast<double>(turns) * (own + 4) + (parts > 1 ? parts * static_cast<double>(b.rows) * group * c.kv_heads * c.head_dim * 1e-6 : 0);
+        if (parts == 1 || cost < least) {
+            least = cost;
+            best = parts;
+        }
+    }
+    return best;
+}
+
 AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
     const int group = q_heads / c.kv_heads;
     const int64_t columns = b.rows * group;
@@ -809,12 +832,17 @@ AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_h
     AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? tile_columns(c.head_dim) : kAttnColumns, 1, 0, 0};
     const int64_t items = p.workgroups = column_tiles(b, group, p.columns) * c.kv_heads;
     const int64_t steps = static_cast<int64_t>(b.table_width) * (c.page_size / kKvStep);
-    const int64_t at_once = 256 * (wide || c.head_dim == 256 ? 2 : 3);
-    int64_t splits = (at_once + items - 1) / (items > 0 ? items : 1);
-    if (!wide && b.sequences > 1 && steps >= 96 * splits) splits *= 2;
-    const int64_t most = (steps + kAttnMinSteps - 1) / kAttnMinSteps;
-    if (splits > most) splits = most;
-    if (splits > kAttnThreads) splits = kAttnThreads;              // (the joining kernel has a thread a part)
+    int64_t most = (steps + kAttnMinSteps - 1) / kAttnMinSteps;
+    if (most > kAttnThreads) most = kAttnThreads;                  // (the joining kernel has a thread a part)
+    int64_t splits;
+    if (wide) {
+        splits = tile_splits(c, b, group, steps, most);
+    } else {
+        const int64_t at_once = 256 * (c.head_dim == 256 ? 2 : 3);
+        splits = (at_once + items - 1) / (items > 0 ? items : 1);
+        if (b.sequences > 1 && steps >= 96 * splits) splits *= 2;
+        if (splits > most) splits = most;
+    }
     if (splits > 1) {
         p.splits = static_cast<int>(splits);
         p.workspace_bytes = static_cast<size_t>(splits) * b.rows * q_heads * (c.head_dim + 2) * sizeof(float);
