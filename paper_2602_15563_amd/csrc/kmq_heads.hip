@@ -195,7 +195,8 @@ __device__ __forceinline__ uint32_t v_bytes(uint32_t word, int d0) {
 __device__ __forceinline__ int v_first(int d0) { return (d0 & ~16) + (d0 & 16 ? 4 : 0); }
 
 // LANES lanes hold a head, 8 elements each; a head never crosses a wave.  ROWS = 1: a workgroup takes a row, or with few rows a
-// part of its heads.  ROWS = 4 (cached): the rows of four tokens that share V's dwords, of one sequence.
+// part of its heads.  ROWS = 4: four rows, cached those of four tokens that share V's dwords, of one sequence; with few of them a part
+// of their heads.
 template <int LANES, int ROWS, bool TURNS>
 __global__ void __launch_bounds__(kHeadThreads, 4) heads_kernel(HeadsArgs a, KvCacheArgs c, KvBatchArgs b, bool cached, int units_per_group) {
     constexpr int kHeads = kWave / LANES;                 // heads of a unit: what a wave takes at once
@@ -421,6 +422,15 @@ __global__ void __launch_bounds__(kHeadThreads) kv_read_kernel(KvCacheArgs c, Kv
 static bool by_groups(const KvBatchArgs& b) { return b.row_starts && b.rows >= 4 * static_cast<int64_t>(b.sequences) && b.rows >= 64; }
 static int64_t most_groups(const KvBatchArgs& b) { return kv_pieces(b.rows, b.sequences, 4, 1, kKvGroupSlack); }
 
+// Units of a group's heads that a workgroup takes: where groups are fewer than 512 workgroups a part of them, `least` at least.  Append
+// and read back, us, whole groups / parts: 37 sequences of 9 rows (192 + 24 + 24 heads) 60 / 27, a piece of 300 rows (32 + 8 + 8)
+// 18.7 / 14.0, of 1024 rows 22 / 19.7; parts up to 1024 workgroups 25, 14.3 and 18.7, but 41.9 for 37 where a piece has 4000 rows.
+constexpr int64_t kFewGroups = 512;
+static int part_of(int units, int64_t groups, int least) {
+    const int64_t parts = groups < kFewGroups ? (kFewGroups + groups - 1) / groups : 1, part = (units + parts - 1) / parts;
+    return static_cast<int>(part > least ? part : least < units ? least : units > 0 ? units : 1);
+}
+
 template <int LANES, int ROWS>
 static void start(bool turns, dim3 grid, hipStream_t s, const HeadsArgs& a, const KvCacheArgs& c, const KvBatchArgs& b, bool cached, int units) {
     if (turns) heads_kernel<LANES, ROWS, true><<<grid, kHeadThreads, 0, s>>>(a, c, b, cached, units);
@@ -435,12 +445,14 @@ hipError_t launch_heads(const HeadsArgs& a, const KvCacheArgs* cache, const KvBa
     const int units = (a.q_heads + heads - 1) / heads + (a.k_heads + heads - 1) / heads + (a.v_heads + heads - 1) / heads;
     const bool turns = a.norm || a.rotary_dim;
     if (cache ? by_groups(b) : a.rows >= 1024) {
-        const dim3 grid(static_cast<unsigned>(cache ? most_groups(b) : (a.rows + 3) / 4));
+        const int64_t groups = cache ? most_groups(b) : (a.rows + 3) / 4;
+        const int group = part_of(units, groups, 4);
+        const dim3 grid(static_cast<unsigned>(groups), static_cast<unsigned>((units + group - 1) / group));
         switch (lanes) {
-            case 8: start<8, 4>(turns, grid, s, a, c, b, cache != nullptr, units); break;
-            case 16: start<16, 4>(turns, grid, s, a, c, b, cache != nullptr, units); break;
-            case 32: start<32, 4>(turns, grid, s, a, c, b, cache != nullptr, units); break;
-            default: start<64, 4>(turns, grid, s, a, c, b, cache != nullptr, units); break;
+            case 8: start<8, 4>(turns, grid, s, a, c, b, cache != nullptr, group); break;
+            case 16: start<16, 4>(turns, grid, s, a, c, b, cache != nullptr, group); break;
+            case 32: start<32, 4>(turns, grid, s, a, c, b, cache != nullptr, group); break;
+            default: start<64, 4>(turns, grid, s, a, c, b, cache != nullptr, group); break;
         }
         return hipGetLastError();
     }
@@ -458,7 +470,11 @@ hipError_t launch_heads(const HeadsArgs& a, const KvCacheArgs* cache, const KvBa
 hipError_t launch_kv_read(const KvCacheArgs& c, const KvBatchArgs& b, uint16_t* k, int64_t k_stride, uint16_t* v, int64_t v_stride, hipStream_t s) {
     if (b.rows == 0) return hipSuccess;
     if (by_groups(b)) {
-        kv_read_kernel<4><<<dim3(static_cast<unsigned>(most_groups(b))), kHeadThreads, 0, s>>>(c, b, k, k_stride, v, v_stride);
+        const int units = (2 * c.kv_heads * (c.head_dim / 8) + kHeadThreads - 1) / kHeadThreads;
+        const int64_t groups = most_groups(b);
+        const int group = part_of(units, groups, 1);
+        const dim3 grid(static_cast<unsigned>(groups), static_cast<unsigned>((units + group - 1) / group));
+        kv_read_kernel<4><<<grid, kHeadThreads, 0, s>>>(c, b, k, k_stride, v, v_stride);
     } else {
         const int work = 2 * c.kv_heads * (c.head_dim / 8), wide = b.rows >= 1024 ? 1 : (work + kHeadThreads - 1) / kHeadThreads;
         kv_read_kernel<1><<<dim3(static_cast<unsigned>(b.rows), static_cast<unsigned>(wide)), kHeadThreads, 0, s>>>(c, b, k, k_stride, v, v_stride);
