@@ -795,10 +795,11 @@ template <int D> constexpr int kTileColumns = kTileWaves<D> * 16 * kColumnTiles<
 static int tile_columns(int D) { return D == 64 ? kTileColumns<64> : D == 128 ? kTileColumns<128> : kTileColumns<256>; }
 
 // Which kernel, and into how many parts the tokens go.  The tiles decode a step once for all of their columns and are worth it where they
-// are full: from 384 columns a sequence on, from 128 where there is one sequence alone.  Measured, us, tiles / turns of waves (8 key
-// heads, 8000 tokens, 128 elements): one sequence, 64 columns 22 / 20, 128 columns 25 / 26, 256 columns 35 / 41; eight sequences,
-// 128 columns 108 / 81, 256 columns 160 / 138, 384 columns 197 / 193, 512 columns 253 / 252; 2 x 2048 columns of 64 elements under a
-// window of 4096 75 / 106; a prompt of 16384 columns 210 / 419.
+// are full and few: from 128 columns a sequence on where there is one sequence alone, from 256 where there are two, else from 384.
+// Measured, us, tiles / turns of waves (8 key heads, 128 elements, 8000 tokens; of several sequences the first, the others down to half
+// of its columns and tokens): one sequence, 256 columns 33 / 38, 512 columns 46 / 60; two, 160 columns 51 / 45, 256 columns 55 / 58,
+// 320 columns 64 / 67, 384 columns of 30000 tokens 184 / 225; four, 320 columns 105 / 102; eight, 256 columns 160 / 139, 384 columns
+// 192 / 195, 512 columns 251 / 252; 2 x 2048 columns of 64 elements under a window of 4096 79 / 112; a prompt of 16384 columns 210 / 399.
 // Parts of the waves' turns: as many workgroups as the compute units hold at once (three a unit, two where the head is wide); more would
 // begin when the first end (131071 tokens, 8 key heads: 96 parts 42, 192 parts 50).  But sequences of
 // different lengths end at different times: where their parts are long, twice as many (16 x 32768 tokens: 6 parts 115, 12 parts 107).
@@ -828,7 +829,7 @@ static int64_t tile_splits(const KvCacheArgs& c, const KvBatchArgs& b, int group
 AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
     const int group = q_heads / c.kv_heads;
     const int64_t columns = b.rows * group;
-    const bool wide = b.sequences == 1 ? columns > 128 : columns > 384 * static_cast<int64_t>(b.sequences);
+    const bool wide = columns > static_cast<int64_t>(b.sequences) * (b.sequences == 1 ? 128 : b.sequences == 2 ? 256 : 384);
     AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? tile_columns(c.head_dim) : kAttnColumns, 1, 0, 0};
     const int64_t items = p.workgroups = column_tiles(b, group, p.columns) * c.kv_heads;
     const int64_t steps = static_cast<int64_t>(b.table_width) * (c.page_size / kKvStep);
