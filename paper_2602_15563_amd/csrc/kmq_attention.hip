@@ -282,44 +282,53 @@ struct Running {
     }
 };
 
-// Few columns a sequence (single tokens, drafts): a workgroup takes 16 columns, and its waves take the steps in turn.  A wave reads
+// Few columns a sequence (single tokens, drafts): a workgroup takes 16 x CT columns, and its waves take the steps in turn.  A wave reads
 // and decodes for itself, K and half of V by tables of index pairs in shared memory, the other half of V by byte permutes from
 // registers: any more of one alone keeps its unit busier than the memory (16 contexts of 32768 tokens: 112 us so, 121 with K alone by
 // the table, 118 with all of V too; nothing by it 151, when K alone took 134).  16 x 32768 tokens take 105 us now, 4.3 TB/s of cache (a copy
 // takes 91): vector issue is busy for 75 % of that and the tables for 67 % (46 % lanes that want the same bank).
-template <int D>
+template <int D, int CT>
 __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     constexpr int NB = D / KMQ_BLOCK, DT = D / 16;
-    constexpr int kTile = 17 * D;
+    constexpr int kTile = 17 * D, kColumns = kAttnColumns * CT;
     const AttentionArgs& a = A.a;
     const KvBatchArgs& b = a.batch;
     constexpr int DC = D < 128 ? D : 128;            // elements joined at a time
     __shared__ float part[kAttnWaves][kAttnColumns][DC + 4];
     __shared__ uint32_t table[2][256];                // pairs of centroids of K, and of V
-    __shared__ float stat[2][kAttnWaves][kAttnColumns];
+    __shared__ float stat[2][kAttnWaves][kColumns];
 
     const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
     const int col = lane & 15, quarter = lane >> 4;
     const int head = static_cast<int>(blockIdx.x) % a.cache.kv_heads;
     const int group = a.q_heads / a.cache.kv_heads;
-    const KvPiece tile = find_tile(b, group, kAttnColumns, static_cast<int>(blockIdx.x) / a.cache.kv_heads);
+    const KvPiece tile = find_tile(b, group, kColumns, static_cast<int>(blockIdx.x) / a.cache.kv_heads);
     if (tile.seq < 0) return;
 
-    // this lane's column, and the tokens it may see
-    const int first_column = tile.index * kAttnColumns, columns = tile.count * group;      // (fewer than 2^30: kmq_kv_attention sees to it)
-    const bool live = first_column + col < columns;
-    const int column = live ? first_column + col : first_column, i = column / group;
-    const int64_t row = tile.start + i;
-    const int qh = head * group + column - i * group;
+    // this lane's columns, and the tokens they may see
+    const int first_column = tile.index * kColumns, columns = tile.count * group;      // (fewer than 2^30: kmq_kv_attention sees to it)
     const Sight sight = sight_of(a, tile.seq);
-    const int see_from = static_cast<int>(sight.begin(i)), see_to = static_cast<int>(sight.end(i));
-    const int last_column = first_column + kAttnColumns < columns ? first_column + kAttnColumns - 1 : columns - 1;
+    bool live[CT];
+    int64_t row[CT];
+    int qh[CT], see_from[CT], see_to[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        live[c] = first_column + 16 * c + col < columns;
+        const int column = live[c] ? first_column + 16 * c + col : first_column, i = column / group;
+        row[c] = tile.start + i;
+        qh[c] = head * group + column - i * group;
+        see_from[c] = static_cast<int>(sight.begin(i));
+        see_to[c] = static_cast<int>(sight.end(i));
+    }
+    const int last_column = first_column + kColumns < columns ? first_column + kColumns - 1 : columns - 1;
     Steps steps = steps_of(sight, first_column / group, last_column / group);
     take_part(steps, A.splits, static_cast<int>(blockIdx.y));
 
     if (A.splits > 1 && steps.from >= steps.to) {                              // a part without tokens
-        if (wave == 0 && quarter == 0 && live) {
-            float* ml = A.part_ml + ((static_cast<int64_t>(blockIdx.y) * b.rows + row) * a.q_heads + qh) * 2;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            if (wave || quarter || !live[c]) continue;
+            float* ml = A.part_ml + ((static_cast<int64_t>(blockIdx.y) * b.rows + row[c]) * a.q_heads + qh[c]) * 2;
             ml[0] = kLowest;
             ml[1] = 0.f;
         }
@@ -330,13 +339,15 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     int step = steps.from + wave;
     Walk<D> walk(a, tile.seq, head, step);
     // queries as the first product's second operand: lane (column, quarter) holds elements 64 b + 16 quarter + 8 j + e
-    u32x4_t q[2 * NB];
+    u32x4_t q[CT][2 * NB];
 #pragma unroll
-    for (int s = 0; s < 2 * NB; ++s) {
-        u32x4_t v = {0, 0, 0, 0};
-        if (live) v = *reinterpret_cast<const u32x4_t*>(a.q + row * a.q_stride + static_cast<int64_t>(qh) * D + s / 2 * 64 + quarter * 16 + s % 2 * 8);
-        q[s] = v;
-    }
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int s = 0; s < 2 * NB; ++s) {
+            u32x4_t v = {0, 0, 0, 0};
+            if (live[c]) v = *reinterpret_cast<const u32x4_t*>(a.q + row[c] * a.q_stride + static_cast<int64_t>(qh[c]) * D + s / 2 * 64 + quarter * 16 + s % 2 * 8);
+            q[c][s] = v;
+        }
     uint32_t pairs[2];
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
@@ -352,10 +363,12 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     __syncthreads();
     const float scale = a.scale * kLog2e;
 
-    f32x4_t o[1][DT];
+    f32x4_t o[CT][DT];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[0][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    Running<1> run;
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[c][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    Running<CT> run;
 
     for (; step < steps.to; step += kAttnWaves) {
         uint32_t vw[2][D / 32];
@@ -366,23 +379,28 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
         const Place next = walk.place(step + kAttnWaves < steps.to);
         if (step + kAttnWaves < steps.to) kw.load(next.base, lane, quarter);
 
-        float s[1][8];
+        float s[CT][8];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+            f32x4_t sum[CT];
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+                f32x4_t acc[CT];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint32_t w = now.k[t][2 * n + j];
-                    acc = mfma(decode8_table(table[0], w), q[2 * n + j], acc);
+                    const u32x4_t w = decode8_table(table[0], now.k[t][2 * n + j]);
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) acc[c] = mfma(w, q[c][2 * n + j], j ? acc[c] : f32x4_t{0.f, 0.f, 0.f, 0.f});
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[e] = fmaf(acc[e], kv_half(now.sc[t][n * 2 + e / 2], e % 2), sum[e]);
+                for (int c = 0; c < CT; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[c][e] = fmaf(acc[c][e], kv_half(now.sc[t][n * 2 + e / 2], e % 2), n ? sum[c][e] : 0.f);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[0][4 * t + e] = fmaf(sum[e], scale, -run.m[0]);
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[c][4 * t + e] = fmaf(sum[c][e], scale, -run.m[c]);
         }
         float sv[NB][8];
 #pragma unroll
@@ -392,77 +410,95 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
         const bool masked = step < steps.whole_from || step >= steps.whole_to || !at.there;
         if (masked) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
-                const bool seen = at.there && j >= see_from && j < see_to;
-                s[0][e] = seen ? s[0][e] : -INFINITY;
-            }
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
+                    const bool seen = at.there && j >= see_from[c] && j < see_to[c];
+                    s[c][e] = seen ? s[c][e] : -INFINITY;
+                }
         }
-        run.follow<DT>(s, o);
+        run.template follow<DT>(s, o);
         run.soften(s);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-            u32x4_t p = weigh(s[0], sv[n]);
-            if (masked) clear_unseen(p, s[0]);
+            u32x4_t p[CT];
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                p[c] = weigh(s[c], sv[n]);
+                if (masked) clear_unseen(p[c], s[c]);
+            }
 #pragma unroll
             for (int j = 2 * n; j < 2 * n + 2; ++j) {
                 const u32x4_t x = decode8_table_of_v(table[1], vw[0][j]), y = decode8(cv, vw[1][j]);
-                o[0][2 * j] = mfma(u32x4_t{x[0], x[1], y[0], y[1]}, p, o[0][2 * j]);
-                o[0][2 * j + 1] = mfma(u32x4_t{x[2], x[3], y[2], y[3]}, p, o[0][2 * j + 1]);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    o[c][2 * j] = mfma(u32x4_t{x[0], x[1], y[0], y[1]}, p[c], o[c][2 * j]);
+                    o[c][2 * j + 1] = mfma(u32x4_t{x[2], x[3], y[2], y[3]}, p[c], o[c][2 * j + 1]);
+                }
             }
         }
         at = next;
     }
 
     // the waves' results joined: every wave's on the scale of the largest maximum
-    const float m = run.maximum(0), sum_l = sum_over_quarters(run.l[0]);
-    if (quarter == 0) {
-        stat[0][wave][col] = m;
-        stat[1][wave][col] = sum_l;
-    }
-    __syncthreads();
-    float most = stat[0][0][col], all = 0.f;
+    float m[CT];
 #pragma unroll
-    for (int w = 1; w < kAttnWaves; ++w) most = fmaxf(most, stat[0][w][col]);
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) all += stat[1][w][col] * __builtin_amdgcn_exp2f(stat[0][w][col] - most);
-    const int64_t pair = row * a.q_heads + qh;                       // (this lane's column; every wave's lanes have the same ones)
-    const bool whole = A.splits == 1;
-    const bool none = !(all > 0.f) && !(all != all);                 // nothing seen (a NaN sum stays one)
-    if (wave == 0 && quarter == 0 && live) {
-        if (!whole) {
-            float* ml = A.part_ml + (static_cast<int64_t>(blockIdx.y) * b.rows * a.q_heads + pair) * 2;
-            ml[0] = most;
-            ml[1] = all;
-        } else if (a.lse) {
-            a.lse[pair] = none ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kLn2;
+    for (int c = 0; c < CT; ++c) {
+        const float sum_l = sum_over_quarters(run.l[c]);
+        m[c] = run.maximum(c);
+        if (quarter == 0) {
+            stat[0][wave][16 * c + col] = m[c];
+            stat[1][wave][16 * c + col] = sum_l;
         }
     }
-    const float weight = __builtin_amdgcn_exp2f(m - most), norm = none ? 0.f : 1.f / all;
+    __syncthreads();
+    const bool whole = A.splits == 1;
 #pragma unroll
-    for (int c0 = 0; c0 < D; c0 += DC) {
-        if (c0) __syncthreads();
+    for (int c = 0; c < CT; ++c) {
+        const int place = 16 * c + col;
+        float most = stat[0][0][place], all = 0.f;
 #pragma unroll
-        for (int d = 0; d < DC / 16; ++d)
+        for (int w = 1; w < kAttnWaves; ++w) most = fmaxf(most, stat[0][w][place]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[wave][col][16 * d + 4 * quarter + e] = o[0][c0 / 16 + d][e] * weight;
-        __syncthreads();
-        // a wave's lane writes its column's elements 4 x (wave * 4 + quarter) + 64 x n
+        for (int w = 0; w < kAttnWaves; ++w) all += stat[1][w][place] * __builtin_amdgcn_exp2f(stat[0][w][place] - most);
+        const int64_t pair = row[c] * a.q_heads + qh[c];             // (this lane's column; every wave's lanes have the same ones)
+        const bool none = !(all > 0.f) && !(all != all);             // nothing seen (a NaN sum stays one)
+        if (wave == 0 && quarter == 0 && live[c]) {
+            if (!whole) {
+                float* ml = A.part_ml + (static_cast<int64_t>(blockIdx.y) * b.rows * a.q_heads + pair) * 2;
+                ml[0] = most;
+                ml[1] = all;
+            } else if (a.lse) {
+                a.lse[pair] = none ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kLn2;
+            }
+        }
+        const float weight = __builtin_amdgcn_exp2f(m[c] - most), norm = none ? 0.f : 1.f / all;
 #pragma unroll
-        for (int n = 0; n < DC / 64; ++n) {
-            const int d = n * 64 + (wave * 4 + quarter) * 4;
-            f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+        for (int c0 = 0; c0 < D; c0 += DC) {
+            if (c || c0) __syncthreads();
 #pragma unroll
-            for (int w = 0; w < kAttnWaves; ++w)
+            for (int d = 0; d < DC / 16; ++d)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[e] += part[w][col][d + e];
-            if (!live) continue;
-            if (whole) {
-                const u32x2_t r = {kv_pack2(none ? 0.f : sum[0] * norm, none ? 0.f : sum[1] * norm),
-                                   kv_pack2(none ? 0.f : sum[2] * norm, none ? 0.f : sum[3] * norm)};
-                *reinterpret_cast<u32x2_t*>(a.out + row * a.out_stride + static_cast<int64_t>(qh) * D + c0 + d) = r;
-            } else {
-                *reinterpret_cast<f32x4_t*>(A.part_o + (static_cast<int64_t>(blockIdx.y) * b.rows * a.q_heads + pair) * D + c0 + d) = sum;
+                for (int e = 0; e < 4; ++e) part[wave][col][16 * d + 4 * quarter + e] = o[c][c0 / 16 + d][e] * weight;
+            __syncthreads();
+            // a wave's lane writes its column's elements 4 x (wave * 4 + quarter) + 64 x n
+#pragma unroll
+            for (int n = 0; n < DC / 64; ++n) {
+                const int d = n * 64 + (wave * 4 + quarter) * 4;
+                f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < kAttnWaves; ++w)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] += part[w][col][d + e];
+                if (!live[c]) continue;
+                if (whole) {
+                    const u32x2_t r = {kv_pack2(none ? 0.f : sum[0] * norm, none ? 0.f : sum[1] * norm),
+                                       kv_pack2(none ? 0.f : sum[2] * norm, none ? 0.f : sum[3] * norm)};
+                    *reinterpret_cast<u32x2_t*>(a.out + row[c] * a.out_stride + static_cast<int64_t>(qh[c]) * D + c0 + d) = r;
+                } else {
+                    *reinterpret_cast<f32x4_t*>(A.part_o + (static_cast<int64_t>(blockIdx.y) * b.rows * a.q_heads + pair) * D + c0 + d) = sum;
+                }
             }
         }
     }
@@ -794,13 +830,17 @@ template <int D> constexpr int kColumnTiles = D == 256 ? 1 : 2;        // of 16 
 template <int D> constexpr int kTileColumns = kTileWaves<D> * 16 * kColumnTiles<D>;
 static int tile_columns(int D) { return D == 64 ? kTileColumns<64> : D == 128 ? kTileColumns<128> : kTileColumns<256>; }
 
-// Which kernel, and into how many parts the tokens go.  The tiles decode a step once for all of their columns and are worth it where they
-// are full and few: from 128 columns a sequence on where there is one sequence alone, from 256 where there are two, else from 384.
-// Measured, us, tiles / turns of waves (8 key heads, 128 elements, 8000 tokens; of several sequences the first, the others down to half
-// of its columns and tokens): one sequence, 256 columns 33 / 38, 512 columns 46 / 60; two, 160 columns 51 / 45, 256 columns 55 / 58,
-// 320 columns 64 / 67, 384 columns of 30000 tokens 184 / 225; four, 320 columns 105 / 102; eight, 256 columns 160 / 139, 384 columns
-// 192 / 195, 512 columns 251 / 252; 2 x 2048 columns of 64 elements under a window of 4096 79 / 112; a prompt of 16384 columns 210 / 399.
-// Parts of the waves' turns: as many workgroups as the compute units hold at once (three a unit, two where the head is wide); more would
+// Which kernel, and into how many parts the tokens go.  Turns of waves with two column tiles decode half as often, but leave half as many
+// workgroups and fewer waves a unit: from 2048 tokens on, where there are more columns than one tile, at up to 128 elements.  The tiles
+// decode a step once for all of their columns and are worth it where they are full and few.  Measured, us, one column tile / two / the
+// tiles (8 key heads, 128 elements, 8000 tokens; of several sequences the first, the others down to half of its columns and tokens):
+//     one sequence: 256 columns 38 / 31 / 33, 1600 columns 192 / 140 / 108, a prompt of 16384 columns 399 / 296 / 210
+//     two: 160 columns 45 / 43 / 51, 256 columns 58 / 49 / 55, 320 columns 67 / 57 / 63, 2048 columns 291 / 211 / 195
+//     four, 320 columns 102 / 85 / 106; eight: 192 columns 112 / 93 / 176, 256 columns 138 / 111 / 160, 384 columns 195 / 157 / 193,
+//     512 columns 252 / 193 / 251, 640 columns - / 241 / 264
+//     eight drafts of 8 tokens (32 columns) on 4000 tokens 28 / 25 / -; of 1000 tokens: four, 256 columns 26 / 27 / 28, eight, 64 elements, 256 columns 16 / 24 / 26
+//     256 elements: two, 200 columns 96 / - / 68, four, 120 columns 103 / - / 98, eight, 256 columns 278 / - / 323
+// Parts of the waves' turns: as many workgroups as the compute units hold at once (three a unit, two where the head or the tile is wide); more would
 // begin when the first end (131071 tokens, 8 key heads: 96 parts 42, 192 parts 50).  But sequences of
 // different lengths end at different times: where their parts are long, twice as many (16 x 32768 tokens: 6 parts 115, 12 parts 107).
 // Parts of the tiles: a unit holds one workgroup (three at 64 elements), and what counts is how many turns of them there are and how long
@@ -829,17 +869,22 @@ static int64_t tile_splits(const KvCacheArgs& c, const KvBatchArgs& b, int group
 AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
     const int group = q_heads / c.kv_heads;
     const int64_t columns = b.rows * group;
-    const bool wide = columns > static_cast<int64_t>(b.sequences) * (b.sequences == 1 ? 128 : b.sequences == 2 ? 256 : 384);
-    AttentionPlan p{wide ? "kv_attention_tile" : "kv_attention", wide ? tile_columns(c.head_dim) : kAttnColumns, 1, 0, 0};
-    const int64_t items = p.workgroups = column_tiles(b, group, p.columns) * c.kv_heads;
     const int64_t steps = static_cast<int64_t>(b.table_width) * (c.page_size / kKvStep);
+    const bool longer = c.head_dim <= 128 && steps >= 64;
+    const bool two = longer && columns > static_cast<int64_t>(b.sequences) * kAttnColumns;
+    const int least = (b.sequences == 1 ? 128 : b.sequences == 2 ? 256 : 384) * (longer ? 2 : 1);
+    const bool wide = columns > static_cast<int64_t>(b.sequences) * least;
+    AttentionPlan p{"kv_attention", kAttnColumns, 1, 0, 0};
+    if (wide) p = {"kv_attention_tile", tile_columns(c.head_dim), 1, 0, 0};
+    else if (two) p = {"kv_attention_two", 2 * kAttnColumns, 1, 0, 0};
+    const int64_t items = p.workgroups = column_tiles(b, group, p.columns) * c.kv_heads;
     int64_t most = (steps + kAttnMinSteps - 1) / kAttnMinSteps;
     if (most > kAttnThreads) most = kAttnThreads;                  // (the joining kernel has a thread a part)
     int64_t splits;
     if (wide) {
         splits = tile_splits(c, b, group, steps, most);
     } else {
-        const int64_t at_once = 256 * (c.head_dim == 256 ? 2 : 3);
+        const int64_t at_once = 256 * (c.head_dim == 256 || two ? 2 : 3);
         splits = (at_once + items - 1) / (items > 0 ? items : 1);
         if (b.sequences > 1 && steps >= 96 * splits) splits *= 2;
         if (splits > most) splits = most;
@@ -855,7 +900,11 @@ template <int D>
 static hipError_t launch_attn(const AttnArgs& A, const AttentionPlan& p, hipStream_t s) {
     const KvBatchArgs& b = A.a.batch;
     const dim3 grid(static_cast<unsigned>(p.workgroups), static_cast<unsigned>(A.splits));
-    if (p.columns == kAttnColumns) attn_kernel<D><<<grid, kAttnThreads, 0, s>>>(A);
+    if (p.columns == kAttnColumns) {
+        attn_kernel<D, 1><<<grid, kAttnThreads, 0, s>>>(A);
+    } else if (p.columns == 2 * kAttnColumns) {
+        if constexpr (D <= 128) attn_kernel<D, 2><<<grid, kAttnThreads, 0, s>>>(A);
+    }
     else attn_tile_kernel<D, kColumnTiles<D>, kTileWaves<D>><<<grid, kTileWaves<D> * kWave, 0, s>>>(A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.splits == 1) return e;
