@@ -287,6 +287,7 @@ struct Running {
 // registers: any more of one alone keeps its unit busier than the memory (16 contexts of 32768 tokens: 112 us so, 121 with K alone by
 // the table, 118 with all of V too; nothing by it 151, when K alone took 134).  16 x 32768 tokens take 105 us now, 4.3 TB/s of cache (a copy
 // takes 91): vector issue is busy for 75 % of that and the tables for 67 % (46 % lanes that want the same bank).
+// Two column tiles take 221 registers at 128 elements (two waves a unit, not three) and decode half as often.
 template <int D, int CT>
 __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     constexpr int NB = D / KMQ_BLOCK, DT = D / 16;
