@@ -237,3 +237,27 @@ def test_queries_appended_in_place(news, lengths):
         results.append((host(q)[:, :384], c.pages_d))
         assert np.array_equal(host(xd)[:, 384:], x.reshape(len(x), 640)[:, 384:])
     assert np.array_equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+
+
+@pytest.mark.parametrize("D,nq,heads", [(64, 40, 33), (128, 21, 9), (128, 1, 24), (256, 18, 9)])
+def test_many_heads_of_few_rows(D, nq, heads):
+    """Groups of rows whose heads go to several workgroups: queries alone, values alone, and kinds that meet inside a part."""
+    c = Case(510 + D, [61, 1, 30], [70, 3, 30], 64, heads, D, behind=2)
+    g, end = np.random.default_rng(511), 92
+    x = patterns(g.standard_normal((c.rows, nq + 2 * heads, D)))
+    freq = (10000.0 ** (-np.arange(0, D, 2) / D)).astype(np.float32)
+    gq, gk = (patterns(g.uniform(0.5, 1.5, D)) for _ in range(2))
+    pos = np.array([c.position(r)[1] for r in range(c.rows)])
+    q = torch.full((c.rows, nq * D), NAN16, dtype=torch.int16, device="cuda")
+    c.to_device()
+    kmq.kv_append(c.cache, c.batch, dev(x.reshape(c.rows, -1)), (nq + 2 * heads) * D, q, nq * D, nq, inv_freq=dev(freq), rotary_dim=D,
+                  q_gain=dev(gq), k_gain=dev(gk), eps=1e-6)
+    torch.cuda.synchronize()
+    turned = [okv.round_bf16(okv.turn(x[:, a:b], pos, freq, D, False, True, gain, 1e-6)) for a, b, gain in ((0, nq, gq), (nq, nq + heads, gk))]
+    for r, page_, token in c.places():
+        c.pages.write(page_, token, turned[1][r], x[r, nq + heads:], c.books)
+    c.check_pages()
+    assert np.array_equal(host(q)[:end].reshape(end, nq, D), turned[0][:end]) and (host(q)[end:] == NAN16).all()
+    # written and read by themselves
+    d = Case(510 + D, [61, 1, 30], [70, 3, 30], 64, heads, D, behind=2)
+    check(d, turned[1], x[:, nq + heads:])
