@@ -723,7 +723,9 @@ __device__ __forceinline__ void join_store(const AttentionArgs& a, int64_t pair,
 }
 
 // The parts of a (row, query head) pair joined, a workgroup a pair: a thread a part for the weights, then D / 4 threads a part and
-// several parts at once for the sums, which are added in a fixed order.  Parts without tokens have no sums and are passed over.
+// several parts at once for the sums, which are added in a fixed order.  Parts without tokens (l is zero) have no sums and are passed over;
+// every other one counts whatever its weight, since a NaN in l or in the sums stays one where the weight rounds to zero, or where
+// a part has no maximum but the lowest number because all of its scores are NaN.
 template <int D>
 __global__ void __launch_bounds__(kAttnThreads) attn_join_kernel(AttnArgs A) {
     constexpr int kLanes = D / 4, kAtOnce = kAttnThreads / kLanes;
@@ -747,9 +749,9 @@ __global__ void __launch_bounds__(kAttnThreads) attn_join_kernel(AttnArgs A) {
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kAttnWaves; ++w) most = fmaxf(most, scratch[0][w]);
-    const float mine = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - most);
-    weight[tid] = mine;
-    float all = l * mine;
+    const float mine = __builtin_amdgcn_exp2f(m - most);
+    weight[tid] = l == 0.f ? -1.f : mine;                          // (no weight is negative: nothing to add)
+    float all = l == 0.f ? 0.f : l * mine;
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) all += __shfl_xor(all, d);
     if (lane == 0) scratch[1][wave] = all;
@@ -763,7 +765,7 @@ __global__ void __launch_bounds__(kAttnThreads) attn_join_kernel(AttnArgs A) {
 #pragma unroll 4
     for (int s = part; s < A.splits; s += kAtOnce) {
         const float w = weight[s];
-        if (w == 0.f) continue;
+        if (w < 0.f) continue;
         const f32x4_t o = *reinterpret_cast<const f32x4_t*>(A.part_o + (s * pairs + pair) * D + 4 * d);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] = fmaf(o[e], w, sum[e]);
@@ -811,8 +813,8 @@ __global__ void __launch_bounds__(kAttnThreads) attn_join_few_kernel(AttnArgs A)
     f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < kFewParts; ++s) {
-        const float w = l[s] == 0.f ? 0.f : __builtin_amdgcn_exp2f(m[s] - most);
-        if (s >= A.splits || w == 0.f) continue;
+        if (s >= A.splits || l[s] == 0.f) continue;
+        const float w = __builtin_amdgcn_exp2f(m[s] - most);
         all += l[s] * w;
         const f32x4_t o = *reinterpret_cast<const f32x4_t*>(A.part_o + (s * pairs + pair) * D + 4 * d);
 #pragma unroll
