@@ -104,3 +104,14 @@ def test_a_value_that_is_nan_reaches_rows_whose_other_parts_outweigh_its_own(ker
     q = patterns(np.tile(direction, (rows, 2 * group, 1)))
     value, lse, _, _ = compare(c, q, 70.0 / D, "a NaN far below")               # scores about 140 apart: 2^-200
     assert np.isnan(value[:, :group, D - 64:]).all() and np.isfinite(value[:, group:]).all() and np.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("news,lengths", [([1, 1, 1], [5000, 40, 2999]), ([3, 1, 2], [3100, 2, 1700]), ([2, 0, 1], [4097, 10, 0])])
+@pytest.mark.parametrize("group", (1, 7))
+@pytest.mark.parametrize("window", (0, 1000))
+def test_many_parts_of_wide_heads(news, lengths, group, window):
+    """256 elements a head and more parts than a thread passes over, some of them empty for a sequence."""
+    print(f"wide heads in many parts: news={news} lengths={lengths} group={group} window={window}", flush=True)
+    c = Case(920, news, lengths, 64, 1, 256, behind=2).to_device()
+    assert parts_of(c, group)[0] > 8
+    compare(c, patterns(np.random.default_rng(921).standard_normal((c.rows, group, 256))), 0.07, "wide heads", window=window)
