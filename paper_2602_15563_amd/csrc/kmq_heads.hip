@@ -40,12 +40,13 @@ __device__ __forceinline__ double sum_over(double v) {
     if (LANES >= 64) v += __shfl_xor(v, 32);
     return v;
 }
-// 1 / sqrt(v): the unit's estimate and two Newton steps, each of which doubles its good bits.
+// 1 / sqrt(v): the unit's estimate and two Newton steps, each of which doubles its good bits.  Of an infinity it is zero, which the steps
+// would make a NaN: an infinite head element is one after the norm (infinity times zero), the finite ones beside it are zeros.
 __device__ __forceinline__ double inverse_root(double v) {
     double y = __builtin_amdgcn_rsq(v);
 #pragma unroll
     for (int i = 0; i < 2; ++i) y *= fma(-0.5 * v * y, y, 1.5);
-    return y;
+    return v == __builtin_inf() ? 0.0 : y;
 }
 __device__ __forceinline__ u32x4_t swap_halves(u32x4_t v) {
     return u32x4_t{v[0] >> 16 | v[0] << 16, v[1] >> 16 | v[1] << 16, v[2] >> 16 | v[2] << 16, v[3] >> 16 | v[3] << 16};

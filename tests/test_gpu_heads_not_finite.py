@@ -1,0 +1,94 @@
+"""Head norms and rotation (kmq_qk_norm_rope, kmq_kv_append) of values that are not finite, on the GPU: NaN exactly where the definition has
+it, and the oracle's values everywhere else."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv as okv
+from paper_2602_15563_amd import kmq
+from tests.kv_util import Case, dev, host, patterns
+
+pytestmark = pytest.mark.gpu
+
+INF, MINUS_INF, NAN = 0x7F80, 0xFF80, 0x7FC1
+
+
+def inv_freq(rot):
+    return (10000.0 ** (-np.arange(0, rot, 2) / max(rot, 1))).astype(np.float32)
+
+
+def turned(x, pos, rot, interleaved, norm, gain, eps):
+    with np.errstate(invalid="ignore", over="ignore"):
+        return okv.bf16_value(okv.round_bf16(okv.turn(x, pos, inv_freq(rot), rot, interleaved, norm, gain, eps)))
+
+
+@pytest.mark.parametrize("D,rot", [(64, 64), (80, 80), (128, 128), (128, 32), (256, 256), (512, 0)])
+@pytest.mark.parametrize("interleaved", (False, True))
+@pytest.mark.parametrize("gains", (False, True))
+@pytest.mark.parametrize("rows", (5, 1026))
+def test_a_head_with_an_infinity_under_the_norm(D, rot, interleaved, gains, rows):
+    """The root of the mean square is infinite: finite elements become zero, the infinite one NaN, and its partner in the rotation with it."""
+    print(f"infinity under the norm: D={D} rot={rot} interleaved={interleaved} gains={gains} rows={rows}", flush=True)
+    g = np.random.default_rng(D + rot + rows)
+    nq, nk = 3, 2
+    x = patterns(g.standard_normal((rows, nq + nk, D)))
+    for r in range(rows):
+        for h in range(nq + nk):
+            kind = g.integers(0, 5)                            # none; one; one of each sign; one and a NaN; the last element
+            at = g.choice(D, 2, replace=False)
+            if kind == 1:
+                x[r, h, at[0]] = INF if r % 2 else MINUS_INF
+            elif kind in (2, 3):
+                x[r, h, at[0]], x[r, h, at[1]] = INF, MINUS_INF if kind == 2 else NAN
+            elif kind == 4:
+                x[r, h, D - 1] = MINUS_INF
+    pos = g.integers(0, 100000, rows).astype(np.int32)
+    pos[0] = 0                                                 # sines of zero: an infinity times zero
+    gq, gk = patterns(1 + 0.3 * g.standard_normal(D)), patterns(1 + 0.3 * g.standard_normal(D))
+    gq[1] = 0
+    q, k = (torch.zeros((rows, n * D), dtype=torch.int16, device="cuda") for n in (nq, nk))
+    kmq.qk_norm_rope(dev(x.reshape(rows, -1)), (nq + nk) * D, q, nq * D, k, nk * D, rows, nq, nk, D, positions=dev(pos) if rot else None,
+                     inv_freq=dev(inv_freq(rot)) if rot else None, rotary_dim=rot, interleaved=interleaved, rmsnorm=True,
+                     q_gain=dev(gq) if gains else None, k_gain=dev(gk) if gains else None, eps=1e-5)
+    torch.cuda.synchronize()
+    for first, count, gain, out in ((0, nq, gq, q), (nq, nk, gk, k)):
+        want = turned(x[:, first:first + count], pos, rot, interleaved, True, gain if gains else None, 1e-5)
+        got = okv.bf16_value(host(out)).reshape(rows, count, D)
+        assert np.array_equal(got, want, equal_nan=True), f"{int((~((got == want) | (np.isnan(got) & np.isnan(want)))).sum())} of {got.size} differ"
+        assert np.isnan(want).any() and (want == 0).any()
+
+
+def test_an_infinite_epsilon():
+    x = patterns(np.random.default_rng(1).standard_normal((3, 2, 64)))
+    q = torch.full((3, 128), NAN, dtype=torch.int16, device="cuda")
+    kmq.qk_norm_rope(dev(x.reshape(3, 128)), 128, q, 128, None, 0, 3, 2, 0, 64, rmsnorm=True, eps=float("inf"))
+    torch.cuda.synchronize()
+    assert (okv.bf16_value(host(q)) == 0).all()
+
+
+@pytest.mark.parametrize("news,lengths", [([1, 1, 1], [9, 40, 33]), ([70, 33], [70, 50])])
+def test_a_key_with_an_infinity_on_its_way_into_the_cache(news, lengths):
+    """Blocks without the NaN that it becomes are stored as the zeros that they are; every other key as it was."""
+    c = Case(2, news, lengths, 32, 2, 128)
+    g = np.random.default_rng(3)
+    x = patterns(g.standard_normal((c.rows, 3 + 4, 128)))
+    for r in range(0, c.rows, 3):
+        x[r, 3 + r % 2, 70 + r % 50] = INF                     # (behind the 64 rotated elements: the first block has no NaN)
+    c.to_device()
+    q = torch.zeros((c.rows, 3 * 128), dtype=torch.int16, device="cuda")
+    kmq.kv_append(c.cache, c.batch, dev(x.reshape(c.rows, -1)), 7 * 128, q, 3 * 128, 3, inv_freq=dev(inv_freq(64)), rotary_dim=64, rmsnorm=True, eps=1e-6)
+    back = [torch.zeros((c.rows, 256), dtype=torch.int16, device="cuda") for _ in range(2)]
+    kmq.kv_read(c.cache, c.batch, back[0], 256, back[1], 256)
+    torch.cuda.synchronize()
+    pos = np.array([c.position(r)[1] for r in range(c.rows)])
+    with np.errstate(invalid="ignore"):
+        keys = okv.round_bf16(okv.turn(x[:, 3:5], pos, inv_freq(64), 64, False, True, None, 1e-6))
+        for r, page, token in c.places():
+            c.pages.write(page, token, keys[r], x[r, 5:], c.books)
+        for r, page, token in c.places():
+            want = okv.round_bf16(c.pages.read(page, token, c.books)[0])
+            got = host(back[0])[r].reshape(2, 128)
+            assert np.array_equal(okv.bf16_value(got), okv.bf16_value(want), equal_nan=True)
+            if r % 3 == 0:
+                h = r % 2
+                assert (okv.bf16_value(got[h, :64]) == 0).all() and np.isnan(okv.bf16_value(got[h, 64:])).all()
