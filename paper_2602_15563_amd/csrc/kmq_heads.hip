@@ -120,11 +120,19 @@ __device__ __forceinline__ u32x4_t turn_head(const HeadsArgs& a, const Factors& 
     return out;
 }
 
+// The scale below which 32 bits may not hold what the rounding of boundary * scale takes away.  That is a multiple of 2^-30 of the product (24 and 8
+// bits), so they do from 2^-119 on: with boundaries of 2^-40 and more (or zero) for scales of 2^-60 and more, with a smaller boundary for none.
+__device__ __forceinline__ float small_scale(const float* boundary) {
+    const float edge = fabsf(boundary[threadIdx.x & (kKvCentroids - 1)]);
+    return __ballot(edge != 0.f && edge < 0x1p-40f) ? __builtin_inff() : 0x1p-60f;
+}
+
 // Eight elements of a block of 64 (8 neighbouring lanes) -> their indices in the nibbles of a dword, and the block's scale.
 // `boundary`: the boundaries as a binary tree, node n's children 2 n and 2 n + 1, root 1.  `place`: this wave's thresholds in
 // shared memory, a tree for each of its 8 blocks.  A threshold is b * s rounded down: then x > threshold exactly where x > b * s.
-// An element walks down the tree, and where it arrives is 16 + its index.
-__device__ __forceinline__ uint32_t quantise8(u32x4_t x, const float* boundary, float* place, uint32_t& scale) {
+// An element walks down the tree, and where it arrives is 16 + its index.  Below a scale of `small` (small_scale) the product is made in
+// 64 bits: what its rounding takes away may be too small for 32.
+__device__ __forceinline__ uint32_t quantise8(u32x4_t x, const float* boundary, float small, float* place, uint32_t& scale) {
     typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
     const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), sub = lane & 7;
     const auto size = [](uint32_t v) { return __builtin_bit_cast(u16x2_t, v & 0x7FFF7FFFu); };
@@ -140,7 +148,7 @@ __device__ __forceinline__ uint32_t quantise8(u32x4_t x, const float* boundary, 
         t[k] = edge * s;
         if (fmaf(edge, s, -t[k]) < 0.f) t[k] = __uint_as_float(__float_as_uint(t[k]) + (t[k] > 0.f ? -1 : 1));
     }
-    if (__ballot(s < 0x1p-60f)) {                         // (where what the rounding took away may be too small for 32 bits)
+    if (__ballot(s < small)) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const double exact = static_cast<double>(boundary[2 * sub + k]) * static_cast<double>(s);             // 24 and 8 bits
@@ -275,6 +283,7 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_kernel(HeadsArgs a, KvC
     const int64_t head_bytes = cached ? static_cast<int64_t>(c.page_size / kKvTile) * kv_tile_bytes(D) : 0;
     const double mean = 1.0 / D;
     __syncthreads();
+    const float small_k = cached ? small_scale(boundary[0]) : 0.f, small_v = cached ? small_scale(boundary[1]) : 0.f;
 
     Factors f;
     int factors_of = -1;                                  // the kind that f belongs to
@@ -303,7 +312,7 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_kernel(HeadsArgs a, KvC
             if (live) *reinterpret_cast<u32x4_t*>(out + row * (kind ? a.k_out_stride : a.q_out_stride) + static_cast<int64_t>(h) * D + d0) = own;
         } else {
             uint32_t scale;
-            const uint32_t word = quantise8(own, boundary[0], threshold[wave], scale);
+            const uint32_t word = quantise8(own, boundary[0], small_k, threshold[wave], scale);
             if (live && to.page_tile) store_k(to.page_tile + h * head_bytes, D, to.token + r, d0, word, scale);
         }
         own = coming;
@@ -321,7 +330,7 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_kernel(HeadsArgs a, KvC
                 if (live && (have >> r & 1u)) x[r] = *reinterpret_cast<const u32x4_t*>(a.v + (first + r) * a.v_stride + static_cast<int64_t>(h) * D + d0);
             }
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) bytes[r] = v_bytes(quantise8(x[r], boundary[1], threshold[wave], scale[r]), d0);
+            for (int r = 0; r < ROWS; ++r) bytes[r] = v_bytes(quantise8(x[r], boundary[1], small_v, threshold[wave], scale[r]), d0);
             if (!live || !to.page_tile) continue;
             uint8_t* tile = to.page_tile + h * head_bytes;
             const int v0 = kv_v_byte(D, to.token, v_first(d0)), step = D / 8;
