@@ -221,10 +221,12 @@ __device__ __forceinline__ u32x4_t weigh(const float (&p)[8], const float (&sv)[
     for (int e = 0; e < 8; e += 2) r[e / 2] = kv_pack2(p[e] * sv[e], p[e + 1] * sv[e + 1]);
     return r;
 }
-// A probability of zero stays zero whatever the scale: what a token that is not seen holds may be anything.
-__device__ __forceinline__ void clear_unseen(u32x4_t& w, const float (&p)[8]) {
+// Zeros for the tokens that are not seen, whatever their scales are.  (Not for every probability of zero: that of a token which is seen may
+// round to it, and an infinity or a NaN in its values reaches the row.)
+template <typename F>
+__device__ __forceinline__ void clear_unseen(u32x4_t& w, const F& seen) {
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) w[e / 2] &= (p[e] == 0.f ? 0u : 0x0000FFFFu) | (p[e + 1] == 0.f ? 0u : 0xFFFF0000u);
+    for (int e = 0; e < 8; e += 2) w[e / 2] &= (seen(e) ? 0x0000FFFFu : 0u) | (seen(e + 1) ? 0xFFFF0000u : 0u);
 }
 
 // CT columns' running maxima, sums, and how far a score (base 2, less the maximum) may be up before everything is brought to a new
@@ -409,15 +411,15 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) sv[n][e] = kv_half(now.sc[e / 4][(NB + n) * 2 + e % 4 / 2], e % 2);
         const bool masked = step < steps.whole_from || step >= steps.whole_to || !at.there;
+        const auto seen = [&](int c, int e) __attribute__((always_inline)) {
+            const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
+            return at.there && j >= see_from[c] && j < see_to[c];
+        };
         if (masked) {
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
-                    const bool seen = at.there && j >= see_from[c] && j < see_to[c];
-                    s[c][e] = seen ? s[c][e] : -INFINITY;
-                }
+                for (int e = 0; e < 8; ++e) s[c][e] = seen(c, e) ? s[c][e] : -INFINITY;
         }
         run.template follow<DT>(s, o);
         run.soften(s);
@@ -427,7 +429,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 p[c] = weigh(s[c], sv[n]);
-                if (masked) clear_unseen(p[c], s[c]);
+                if (masked) clear_unseen(p[c], [&](int e) { return seen(c, e); });
             }
 #pragma unroll
             for (int j = 2 * n; j < 2 * n + 2; ++j) {
@@ -617,15 +619,16 @@ __global__ void __launch_bounds__(WAVES * kWave, 2) attn_tile_kernel(AttnArgs A)
             }
         __builtin_amdgcn_s_setprio(0);
         const bool masked = step < own.whole_from || step >= own.whole_to || !there;
+        const auto seen = [&](int c, int e) __attribute__((always_inline)) {
+            const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
+            return there && j >= see_from[c] && j < see_to[c];
+        };
         if (masked) {
             asm volatile("");                                        // (kept a branch: few steps are masked)
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
-                    s[c][e] = there && j >= see_from[c] && j < see_to[c] ? s[c][e] : -INFINITY;
-                }
+                for (int e = 0; e < 8; ++e) s[c][e] = seen(c, e) ? s[c][e] : -INFINITY;
         }
         run.template follow<DT>(s, o);
         run.soften(s);
@@ -644,7 +647,7 @@ __global__ void __launch_bounds__(WAVES * kWave, 2) attn_tile_kernel(AttnArgs A)
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int c = 0; c < CT; ++c) clear_unseen(p[n][c], s[c]);
+                for (int c = 0; c < CT; ++c) clear_unseen(p[n][c], [&](int e) { return seen(c, e); });
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {

@@ -1,0 +1,45 @@
+"""Attention over the 4-bit cache (kmq_kv_attention) on the GPU where something that a row sees is not finite: it reaches the row, and no other."""
+import numpy as np
+import pytest
+
+from oracle import kv as okv
+from paper_2602_15563_amd import kmq
+from tests.kv_util import Case, patterns, run_attention
+from tests.test_gpu_kv_attention_parts import NAN, ONE, TILE, TWO, compare, spoil
+
+pytestmark = pytest.mark.gpu
+
+# kernel, rows, tokens, head size, query heads a key head, table width (pages of 32)
+CASES = [(ONE, 1, 20, 64, 3, None), (ONE, 1, 20, 128, 3, None), (ONE, 1, 20, 256, 3, None), (ONE, 4, 70, 128, 2, None), (TWO, 9, 20, 64, 3, 64),
+         (TWO, 9, 20, 128, 3, 64), (TWO, 40, 75, 128, 1, 64), (TILE, 150, 150, 64, 4, None), (TILE, 150, 150, 128, 4, None), (TILE, 150, 150, 256, 4, None)]
+
+
+def make(seed, kernel, rows, tokens, D, group, width):
+    print(f"not finite: {kernel} rows={rows} tokens={tokens} D={D} group={group} width={width}", flush=True)
+    c = Case(seed, [rows], [tokens], 32, 2, D, width=width).to_device()
+    assert kmq.kernel_name_kv_attention(c.cache, c.batch, 2 * group) == kernel
+    return c
+
+
+@pytest.mark.parametrize("kernel,rows,tokens,D,group,width", CASES)
+@pytest.mark.parametrize("bits", (NAN, 0x7F80))
+def test_a_value_of_a_token_whose_probability_rounds_to_zero(kernel, rows, tokens, D, group, width, bits):
+    """Token 3's score is so far below that of token 0 that its probability is zero in 32 bits; it stands in a step that some of its tokens' columns
+    do not see whole.  A NaN or an infinity among its values is one in every row that sees it."""
+    c = make(940 + D, kernel, rows, tokens, D, group, width)
+    g = np.random.default_rng(941)
+    direction = np.where(g.random(D) < 0.5, -1.0, 1.0)
+    for t in range(tokens):
+        page, place = okv.place(c.table[0], 32, c.num_pages, t)
+        c.pages.write(page, place, patterns(np.tile(direction * (-1 if t == 3 else 1), (2, 1))), patterns(g.standard_normal((2, D))), c.books)
+    spoil(c, 3, 1, block=D // 64 - 1, bits=bits)
+    c.to_device()
+    q = patterns(np.tile(direction, (rows, 2 * group, 1)))
+    if bits == NAN:
+        value, lse, _, _ = compare(c, q, 70.0 / D, "a NaN far below")           # scores about 140 apart: 2^-200
+    else:
+        got, lse = run_attention(c, q, 2 * group, 70.0 / D)
+        value = okv.bf16_value(got)
+    first = max(0, 3 - (tokens - rows))                                          # the first row that sees token 3
+    assert not np.isfinite(value[first:, :group, D - 64:]).any() and np.isfinite(value[:first]).all()
+    assert np.isfinite(value[:, group:]).all() and np.isfinite(value[:, :, :D - 64]).all() and np.isfinite(lse).all()
