@@ -405,39 +405,46 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[c][4 * t + e] = fmaf(sum[c][e], scale, -run.m[c]);
         }
-        float sv[NB][8];
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sv[n][e] = kv_half(now.sc[e / 4][(NB + n) * 2 + e % 4 / 2], e % 2);
         const bool masked = step < steps.whole_from || step >= steps.whole_to || !at.there;
-        const auto seen = [&](int c, int e) __attribute__((always_inline)) {
-            const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
+        const auto seen = [&](int first, int c, int e) __attribute__((always_inline)) {
+            const int j = first + e / 4 * kKvTile + e % 4;
             return at.there && j >= see_from[c] && j < see_to[c];
         };
         if (masked) {
+            const int first = step * kKvStep + quarter * 4;
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[c][e] = seen(c, e) ? s[c][e] : -INFINITY;
+                for (int e = 0; e < 8; ++e) s[c][e] = seen(first, c, e) ? s[c][e] : -INFINITY;
         }
         run.template follow<DT>(s, o);
         run.soften(s);
+        u32x4_t p[NB][CT];
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-            u32x4_t p[CT];
+            float sv[8];
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                p[c] = weigh(s[c], sv[n]);
-                if (masked) clear_unseen(p[c], [&](int e) { return seen(c, e); });
-            }
+            for (int e = 0; e < 8; ++e) sv[e] = kv_half(now.sc[e / 4][(NB + n) * 2 + e % 4 / 2], e % 2);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) p[n][c] = weigh(s[c], sv);
+        }
+        if (masked) {
+            int first = step * kKvStep + quarter * 4;
+            asm volatile("" : "+v"(first));                          // (worked out again: what the mask found would be held through every step)
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) clear_unseen(p[n][c], [&](int e) { return seen(first, c, e); });
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
 #pragma unroll
             for (int j = 2 * n; j < 2 * n + 2; ++j) {
                 const u32x4_t x = decode8_table_of_v(table[1], vw[0][j]), y = decode8(cv, vw[1][j]);
 #pragma unroll
                 for (int c = 0; c < CT; ++c) {
-                    o[c][2 * j] = mfma(u32x4_t{x[0], x[1], y[0], y[1]}, p[c], o[c][2 * j]);
-                    o[c][2 * j + 1] = mfma(u32x4_t{x[2], x[3], y[2], y[3]}, p[c], o[c][2 * j + 1]);
+                    o[c][2 * j] = mfma(u32x4_t{x[0], x[1], y[0], y[1]}, p[n][c], o[c][2 * j]);
+                    o[c][2 * j + 1] = mfma(u32x4_t{x[2], x[3], y[2], y[3]}, p[n][c], o[c][2 * j + 1]);
                 }
             }
         }
@@ -619,16 +626,17 @@ __global__ void __launch_bounds__(WAVES * kWave, 2) attn_tile_kernel(AttnArgs A)
             }
         __builtin_amdgcn_s_setprio(0);
         const bool masked = step < own.whole_from || step >= own.whole_to || !there;
-        const auto seen = [&](int c, int e) __attribute__((always_inline)) {
-            const int j = step * kKvStep + e / 4 * kKvTile + quarter * 4 + e % 4;
+        const auto seen = [&](int first, int c, int e) __attribute__((always_inline)) {
+            const int j = first + e / 4 * kKvTile + e % 4;
             return there && j >= see_from[c] && j < see_to[c];
         };
         if (masked) {
+            const int first = step * kKvStep + quarter * 4;
             asm volatile("");                                        // (kept a branch: few steps are masked)
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[c][e] = seen(c, e) ? s[c][e] : -INFINITY;
+                for (int e = 0; e < 8; ++e) s[c][e] = seen(first, c, e) ? s[c][e] : -INFINITY;
         }
         run.template follow<DT>(s, o);
         run.soften(s);
@@ -643,11 +651,12 @@ __global__ void __launch_bounds__(WAVES * kWave, 2) attn_tile_kernel(AttnArgs A)
             for (int c = 0; c < CT; ++c) p[n][c] = weigh(s[c], sv);
         }
         if (masked) {
-            asm volatile("");
+            int first = step * kKvStep + quarter * 4;
+            asm volatile("" : "+v"(first));
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int c = 0; c < CT; ++c) clear_unseen(p[n][c], [&](int e) { return seen(c, e); });
+                for (int c = 0; c < CT; ++c) clear_unseen(p[n][c], [&](int e) { return seen(first, c, e); });
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
