@@ -43,3 +43,25 @@ def test_a_value_of_a_token_whose_probability_rounds_to_zero(kernel, rows, token
     first = max(0, 3 - (tokens - rows))                                          # the first row that sees token 3
     assert not np.isfinite(value[first:, :group, D - 64:]).any() and np.isfinite(value[:first]).all()
     assert np.isfinite(value[:, group:]).all() and np.isfinite(value[:, :, :D - 64]).all() and np.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("kernel,rows,tokens,D,group,width", CASES + [(ONE, 1, 1, 128, 2, None), (ONE, 1, 2, 64, 1, None), (ONE, 1, 700, 128, 2, None), (ONE, 1, 3000, 256, 2, None),
+                                                                      (TWO, 20, 5, 128, 2, 64), (TILE, 250, 700, 128, 3, None)])
+@pytest.mark.parametrize("bits", (0x7F80, 0xFF80))
+def test_an_infinite_query_is_nan_in_its_head_and_row(kernel, rows, tokens, D, group, width, bits):
+    """Its scores are infinite, all of one sign where its keys are few: exp(S) / sum exp(S) has no number for them.  A row that sees nothing stays zero."""
+    c = make(950 + D, kernel, rows, tokens, D, group, width)
+    g = np.random.default_rng(951)
+    q = patterns(g.standard_normal((rows, 2 * group, D)))
+    want, lse = run_attention(c, q, 2 * group, D ** -0.5)
+    places = {(int(g.integers(0, rows)), int(h)) for h in g.permutation(2 * group)[:3]} | {(0, 0)}
+    for r, h in places:
+        q[r, h, g.integers(0, D)] = bits
+    got, lse2 = run_attention(c, q, 2 * group, D ** -0.5)
+    for r, h in places:
+        if r >= rows - tokens:
+            assert np.isnan(okv.bf16_value(got[r, h])).all() and np.isnan(lse2[r, h])
+        else:
+            assert (got[r, h] == 0).all() and np.isneginf(lse2[r, h])
+        got[r, h], lse2[r, h] = want[r, h], lse[r, h]
+    assert np.array_equal(got, want) and np.array_equal(lse2, lse)
