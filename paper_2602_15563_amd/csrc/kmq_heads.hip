@@ -86,7 +86,7 @@ __device__ __forceinline__ Factors make_factors(const HeadsArgs& a, const uint16
     for (int e = 0; e < 8; ++e) {
         const double2 t = angles[!turned ? half : a.interleaved ? d0 / 2 + e / 2 : (left ? d0 : d0 - half) + e];
         f.own[e] = static_cast<double>(kv_half(g[e / 2], e % 2)) * t.x;
-        f.far[e] = static_cast<double>(kv_half(go[e / 2], e % 2)) * t.y;
+        f.far[e] = turned ? static_cast<double>(kv_half(go[e / 2], e % 2)) * t.y : -0.0;      // (partners of zero are added: less zero, so that -0 stays -0)
     }
     return f;
 }

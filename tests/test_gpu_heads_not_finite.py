@@ -92,3 +92,28 @@ def test_a_key_with_an_infinity_on_its_way_into_the_cache(news, lengths):
             if r % 3 == 0:
                 h = r % 2
                 assert (okv.bf16_value(got[h, :64]) == 0).all() and np.isnan(okv.bf16_value(got[h, 64:])).all()
+
+
+@pytest.mark.parametrize("D,rot", [(64, 0), (64, 32), (80, 16), (128, 96), (128, 128), (512, 256)])
+@pytest.mark.parametrize("interleaved", (False, True))
+@pytest.mark.parametrize("norm,gains", [(False, False), (True, False), (True, True)])
+@pytest.mark.parametrize("rows", (3, 1025))
+def test_zeros_keep_their_signs(D, rot, interleaved, norm, gains, rows):
+    """Zeros of both signs among the elements, turned and not: bit for bit the definition's."""
+    if not (rot or norm):
+        return                                                 # (nothing turns the heads: a call without norm and rotation copies them)
+    print(f"zeros: D={D} rot={rot} interleaved={interleaved} norm={norm} gains={gains} rows={rows}", flush=True)
+    g = np.random.default_rng(D + rot)
+    x = patterns(g.standard_normal((rows, 3, D)))
+    kind = g.integers(0, 4, x.shape)
+    x[kind == 0], x[kind == 1] = 0, 0x8000
+    pos = g.integers(0, 1000, rows).astype(np.int32)
+    gain = patterns(g.standard_normal(D))
+    q = torch.full((rows, 3 * D), NAN, dtype=torch.int16, device="cuda")
+    kmq.qk_norm_rope(dev(x.reshape(rows, -1)), 3 * D, q, 3 * D, None, 0, rows, 3, 0, D, positions=dev(pos) if rot else None,
+                     inv_freq=dev(inv_freq(rot)) if rot else None, rotary_dim=rot, interleaved=interleaved, rmsnorm=norm, q_gain=dev(gain) if gains else None, eps=1e-5)
+    torch.cuda.synchronize()
+    want = okv.round_bf16(okv.turn(x, pos, inv_freq(rot), rot, interleaved, norm, gain if gains else None, 1e-5))
+    got = host(q).reshape(rows, 3, D)
+    assert (want == 0x8000).any()
+    assert np.array_equal(got, want), f"{int((got != want).sum())} of {got.size} differ"
