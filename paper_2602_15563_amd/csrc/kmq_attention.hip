@@ -918,6 +918,7 @@ AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_h
         if (b.sequences > 1 && steps >= 96 * splits) splits *= 2;
         if (splits > most) splits = most;
     }
+    if (b.rows * q_heads * (c.head_dim / 4) > (int64_t(1) << 32) - kAttnThreads) splits = 1;     // (the joining launch's threads are counted in 32 bits)
     if (splits > 1) {
         p.splits = static_cast<int>(splits);
         p.workspace_bytes = static_cast<size_t>(splits) * b.rows * q_heads * (c.head_dim + 2) * sizeof(float);
