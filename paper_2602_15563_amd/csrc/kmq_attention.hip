@@ -88,6 +88,16 @@ struct KWords {
             load_words<D / 16>(sc[t], base + t * 17 * D + 16 * D + quarter * (D / 4));
         }
     }
+    // Whether a scale of K, of any of the step's tokens, is an infinity or a NaN (or has a sign, which none has that is written here).
+    __device__ __forceinline__ bool not_finite() const {
+        typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
+        u16x2_t most = {0, 0};
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, sc[t][i]));
+        return __ballot(most[0] > 0x7F7F || most[1] > 0x7F7F) != 0;
+    }
 };
 __device__ __forceinline__ f32x4_t mfma(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
@@ -394,6 +404,8 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
         const Place next = walk.place(step + kAttnWaves < steps.to);
         if (step + kAttnWaves < steps.to) kw.load(next.base, lane, quarter);
 
+        // a key whose scale is an infinity scores NaN: its product with the sum over the block would be one of either sign, and minus infinity no score
+        const bool odd = now.not_finite();
         float s[CT][8];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -417,13 +429,28 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[c][4 * t + e] = fmaf(sum[c][e], scale, -run.m[c]);
         }
-        const bool masked = step < steps.whole_from || step >= steps.whole_to || !at.there;
+        const bool masked = step < steps.whole_from || step >= steps.whole_to || !at.there || odd;
         const auto seen = [&](int first, int c, int e) __attribute__((always_inline)) {
             const int j = first + e / 4 * kKvTile + e % 4;
             return at.there && j >= see_from[c] && j < see_to[c];
         };
         if (masked) {
             const int first = step * kKvStep + quarter * 4;
+            if (odd) {                                               // (read again: held until here, the scales would take registers in every step)
+                const uint8_t* scales = at.base + 16 * D + quarter * (D / 4);
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        uint32_t w = *reinterpret_cast<const uint32_t*>(scales + e / 4 * kTile + n * 8 + e % 4 * 2);
+                        asm volatile("" : "+v"(w));
+#pragma unroll
+                        for (int c = 0; c < CT; ++c) {
+                            s[c][e] += kv_half(w, 0) * 0.f;
+                            s[c][e + 1] += kv_half(w, 1) * 0.f;
+                        }
+                    }
+            }
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
@@ -587,7 +614,8 @@ __global__ void __launch_bounds__(WAVES * kWave, 2) attn_tile_kernel(AttnArgs A)
     // this wave's share of a step
     const int kt = wave / kShares, k0 = wave % kShares * KD;
     const int v0 = kHalves ? wave >> 1 : wave, v_shift = (wave & 1) * 4;
-    const float sf = tid / (2 * NB) & 1 ? 1.f : a.scale * kLog2e;     // (dword tid of a step's scales: a quarter's K, then its V)
+    const bool of_k = !(tid / (2 * NB) & 1);                         // (dword tid of a step's scales: a quarter's K, then its V)
+    const float sf = a.scale * kLog2e;
     uint32_t kw[KD], vw[2], sw = 0;
     const auto load = [&](const uint8_t* base) __attribute__((always_inline)) {
         const uint8_t* k = base + kt * kTile + lane * (D / 8) + 4 * k0;
@@ -614,8 +642,11 @@ __global__ void __launch_bounds__(WAVES * kWave, 2) attn_tile_kernel(AttnArgs A)
             vf[buffer][wave][lane] = u32x4_t{r[0], r[1], r[2], r[3]};
         }
         if (tid < D / 2) {
-            scales[buffer][2 * tid] = kv_half(sw, 0) * sf;
-            scales[buffer][2 * tid + 1] = kv_half(sw, 1) * sf;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float x = kv_half(sw, i);
+                scales[buffer][2 * tid + i] = of_k ? fmaf(x, 0.f, x * sf) : x;     // (of K an infinity becomes a NaN)
+            }
         }
     };
     const auto multiply = [&](int step, int buffer, bool there) __attribute__((always_inline)) {

@@ -65,3 +65,32 @@ def test_an_infinite_query_is_nan_in_its_head_and_row(kernel, rows, tokens, D, g
             assert (got[r, h] == 0).all() and np.isneginf(lse2[r, h])
         got[r, h], lse2[r, h] = want[r, h], lse[r, h]
     assert np.array_equal(got, want) and np.array_equal(lse2, lse)
+
+
+@pytest.mark.parametrize("kernel,rows,tokens,D,group,width", CASES + [(ONE, 1, 1, 128, 2, None), (ONE, 1, 700, 64, 2, None), (ONE, 2, 3000, 256, 2, None), (TWO, 20, 300, 128, 2, 64),
+                                                                      (TWO, 20, 2500, 64, 2, None), (TILE, 250, 700, 64, 3, None), (TILE, 250, 700, 256, 3, None)])
+@pytest.mark.parametrize("bits", (0x7F80, NAN))
+def test_a_key_that_is_not_finite_is_nan_in_every_row_that_sees_it(kernel, rows, tokens, D, group, width, bits):
+    """One block's scale of one key, in tokens that all rows see, some do, or the last alone, in whole steps and at their ends, for every place in a
+    tile; and in a token that lies behind the sequence or before every window, which changes nothing."""
+    c = make(960 + D, kernel, rows, tokens, D, group, width)
+    g = np.random.default_rng(961)
+    q = patterns(g.standard_normal((rows, 2 * group, D)))
+    clean = c.pages.bytes.copy()
+    want, lse = run_attention(c, q, 2 * group, D ** -0.5)
+    places = sorted({0, tokens - 1, max(0, tokens - rows), tokens // 2} | {int(t) for t in g.integers(0, tokens, 6)})
+    for t in places:
+        c.pages.bytes[:] = clean
+        spoil(c, t, 0, head=1, block=int(g.integers(0, D // 64)), bits=bits)
+        got, lse2 = run_attention(c.to_device(), q, 2 * group, D ** -0.5)
+        first = max(0, t - (tokens - rows))
+        assert np.isnan(okv.bf16_value(got[first:, group:])).all() and np.isnan(lse2[first:, group:]).all(), f"token {t}"
+        assert np.array_equal(got[:, :group], want[:, :group]) and np.array_equal(lse2[:, :group], lse[:, :group]), f"token {t}: the other head"
+        assert np.array_equal(got[:first], want[:first]) and np.array_equal(lse2[:first], lse[:first]), f"token {t}: rows before it"
+    if tokens > rows + 20:
+        c.pages.bytes[:] = clean
+        want, lse = run_attention(c.to_device(), q, 2 * group, D ** -0.5, window=20)
+        for t in range(0, tokens - rows - 20):
+            spoil(c, t, 0, bits=bits)
+        got, lse2 = run_attention(c.to_device(), q, 2 * group, D ** -0.5, window=20)
+        assert np.array_equal(got, want) and np.array_equal(lse, lse2)
