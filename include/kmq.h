@@ -344,7 +344,8 @@ kmq_status kmq_quantize_blockscaled(const uint16_t* Wdense, int64_t N, int64_t K
  *     a_i = position * inv_freq[i],  i = 0 .. rotary_dim/2 - 1
  *     left  = n_l cos a_i - n_r sin a_i,   right = n_r cos a_i + n_l sin a_i
  *     (l, r) = (i, i + rotary_dim/2), or (2i, 2i + 1) where `interleaved` is 1
- * Computed in 64 bits, rounded to 32 and then to bf16 (nearest even).  rotary_dim is a multiple of 16, at
+ * Computed in 64 bits, rounded to 32 and then to bf16 (nearest even); infinities and NaN as the formulas have them (under the norm a head with an
+ * infinity is zeros but for that element and its partner, which are NaN).  rotary_dim is a multiple of 16, at
  * most the head's size; 0: no rotation, and positions and inv_freq are not looked at.  A host structure, read
  * during the call; what it points to is device memory. */
 typedef struct kmq_head_turn {
@@ -381,7 +382,7 @@ typedef struct kmq_kv_cache {
     int64_t num_pages;
     int32_t page_size;          /* tokens: a multiple of 32 (a cache without pages: one page a sequence) */
     int32_t kv_heads;
-    int32_t head_dim;           /* 64, 128 or 256 */
+    int32_t head_dim;           /* 64, 128 or 256: whole blocks, as many as fill the matrix cores' operands */
 } kmq_kv_cache;
 
 /* Which rows belong to which sequence, and where its tokens are.  Row row_starts[b] + i of sequence b, i < n = row_starts[b+1] -
@@ -418,12 +419,18 @@ kmq_status kmq_kv_append(const kmq_kv_cache* cache, const kmq_kv_batch* batch, c
 /* Attention of the batch's rows over the cache.  Query head h reads key head h / (q_heads / kv_heads).
  *     S_j = scale * q . K_j,    out = sum_j exp(S_j) V_j / sum_j exp(S_j)
  * over the positions j of the row's sequence that are in the cache, below lengths, with j <= p (causal = 1) and j > p - window
- * (window > 0), p the row's position.  A row that sees none is zero.  Sums in fp32, one rounding to bf16.
+ * (window > 0), p the row's position.  A row that sees none is zero.
+ * Scores, maxima and sums in fp32.  exp(S_j) times the scale of V's block is rounded to bf16 before it multiplies the centroids (2^-8 of itself at
+ * most; the sum that divides is of exp(S_j) as it is), and the output once more.  The sums are divided at the end: values beyond
+ * 2^119 / tokens may overflow them.
  *   lse        rows x q_heads fp32, log sum_j exp(S_j) (minus infinity where none is seen), or NULL
  *   workspace  kmq_kv_attention_workspace_bytes() bytes, 16-byte aligned, not initialised: where the rows are too few to fill the
  *              compute units, the tokens are split over workgroups, and a second kernel joins the parts in their order
- * The size depends on the structures' numbers alone, not on lengths, so a captured call may be replayed with others; 0 on bad
- * arguments.  Tokens that no row sees, and what lies behind a sequence, may hold anything, NaN and infinities too.
+ * The size, the number of parts and the kernel depend on the structures' numbers alone, not on lengths, so a captured call may be replayed with
+ * others; 0 on bad arguments.  A table much wider than its sequences therefore costs parts that find nothing, and a batch of very unequal
+ * sequences runs one kernel, chosen by its rows on average.
+ * Tokens that a row does not see, and what lies behind a sequence, may hold anything, NaN and infinities too.  In what it sees, a NaN or an
+ * infinity in its query or in a key's scales makes the row and its lse NaN, and one in a value's scale makes that block's outputs not finite.
  * KMQ_ERR_SHAPE: q_heads no multiple of kv_heads, rows * q_heads > 2^30, more than 2^22 workgroups (sequences, or 16 (row, query head)
  * pairs of a sequence and a key head, times kv_heads), scale not finite, window < 0. */
 size_t kmq_kv_attention_workspace_bytes(const kmq_kv_cache* cache, const kmq_kv_batch* batch, int q_heads);

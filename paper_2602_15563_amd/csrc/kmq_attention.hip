@@ -306,10 +306,10 @@ struct Running {
 
 // Few columns a sequence (single tokens, drafts): a workgroup takes 16 x CT columns, and its waves take the steps in turn.  A wave reads
 // and decodes for itself, K and half of V by tables of index pairs in shared memory, the other half of V by byte permutes from
-// registers: any more of one alone keeps its unit busier than the memory (16 contexts of 32768 tokens: 112 us so, 121 with K alone by
-// the table, 118 with all of V too; nothing by it 151, when K alone took 134).  16 x 32768 tokens take 105 us now, 4.3 TB/s of cache (a copy
-// takes 91): vector issue is busy for 75 % of that and the tables for 67 % (46 % lanes that want the same bank).
-// Two column tiles take 221 registers at 128 elements (two waves a unit, not three) and decode half as often.
+// registers: any more of one alone keeps its unit busier than the memory (16 contexts of 17408 to 32768 tokens, when each was tried: 112 us so,
+// 121 with K alone by the table, 118 with all of V too; nothing by it 151, when K alone took 134).  They take 102 us now, 4.3 TB/s of cache (a
+// copy takes 91): vector issue is busy for 73 % of that and the tables for 69 % (48 % lanes that want the same bank).
+// Two column tiles take 228 registers at 128 elements (two waves a unit, not three) and decode half as often.
 template <int D, int CT>
 __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
     constexpr int NB = D / KMQ_BLOCK, DT = D / 16;
@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attn_kernel(AttnArgs A) {
 // Many columns a sequence (prompts, long drafts): a workgroup takes 16 x CT columns a wave, and its waves decode every step
 // together, an equal share of it each, into shared memory in the order of the first product's and the second product's first operand.
 // Two such buffers: the next step is decoded into one while the products read the other.  A prompt of 4096 tokens (32 query heads of
-// 128 elements) takes 211 us, 650 TFLOP/s: vector issue (exponentials, scales, roundings, decode) is busy for 57 % of it and the
+// 128 elements) takes 210 us, 653 TFLOP/s: vector issue (exponentials, scales, roundings, decode) is busy for 57 % of it and the
 // matrix cores for 28 %, and two waves a unit, which is what the registers allow, seldom overlap them.
 template <int D, int CT, int WAVES>
 __global__ void __launch_bounds__(WAVES * kWave, 2) attn_tile_kernel(AttnArgs A) {
@@ -890,7 +890,11 @@ template <int D> constexpr int kColumnTiles = D == 256 ? 1 : 2;        // of 16 
 template <int D> constexpr int kTileColumns = kTileWaves<D> * 16 * kColumnTiles<D>;
 static int tile_columns(int D) { return D == 64 ? kTileColumns<64> : D == 128 ? kTileColumns<128> : kTileColumns<256>; }
 
-// Which kernel, and into how many parts the tokens go.  Turns of waves with two column tiles decode half as often, but leave half as many
+// Which kernel, and into how many parts the tokens go.  Both go by the structures' numbers alone, so that a captured call can be replayed with other
+// lengths: columns a sequence are an average, and the table's width stands for the tokens.  What that costs, us (8 key heads, 32 query heads of
+// 128 elements): one token after 200 in a table of 256 tokens 7.0, of 4096 10.5, of 131072 11.0 (96 parts, 95 of them empty); 16 tokens of 2000 in a
+// table of 2048 17.9, of 131072 18.6; a piece of 2048 rows beside 15 single tokens, 8000 tokens each, 470, and one after the other 354 + 37.
+// Turns of waves with two column tiles decode half as often, but leave half as many
 // workgroups and fewer waves a unit: from 2048 tokens on, where there are more columns than one tile, at up to 128 elements.  The tiles
 // decode a step once for all of their columns and are worth it where they are full and few.  Measured, us, one column tile / two / the
 // tiles (8 key heads, 128 elements, 8000 tokens; of several sequences the first, the others down to half of its columns and tokens):
@@ -898,11 +902,15 @@ static int tile_columns(int D) { return D == 64 ? kTileColumns<64> : D == 128 ? 
 //     two: 160 columns 45 / 43 / 51, 256 columns 58 / 49 / 55, 320 columns 67 / 57 / 63, 2048 columns 291 / 211 / 195
 //     four, 320 columns 102 / 85 / 106; eight: 192 columns 112 / 93 / 176, 256 columns 138 / 111 / 160, 384 columns 195 / 157 / 193,
 //     512 columns 252 / 193 / 251, 640 columns - / 241 / 264
+//     beyond the line: four, 1024 columns - / 195 / 191; eight, 1024 columns - / 347 / 353, 2048 columns - / 642 / 607
 //     eight drafts of 8 tokens (32 columns) on 4000 tokens 28 / 25 / -; of 1000 tokens: four, 256 columns 26 / 27 / 28, eight, 64 elements, 256 columns 16 / 24 / 26
-//     256 elements: two, 200 columns 96 / - / 68, four, 120 columns 103 / - / 98, eight, 256 columns 278 / - / 323
+//     256 elements: one, 100 columns 48 / - / 33; two, 200 columns 94 / - / 70; four, 120 columns 102 / - / 97; eight, 256 columns 272 / - / 281,
+//     512 columns 501 / - / 408
+// The lines below were drawn at 128 elements and serve 256 too, where they are not the best: the first three of its points go to the turns of waves,
+// though the tiles are faster there.
 // Parts of the waves' turns: as many workgroups as the compute units hold at once (three a unit, two where the head or the tile is wide); more would
 // begin when the first end (131071 tokens, 8 key heads: 96 parts 42, 192 parts 50).  But sequences of
-// different lengths end at different times: where their parts are long, twice as many (16 x 32768 tokens: 6 parts 115, 12 parts 107).
+// different lengths end at different times: where their parts are long, twice as many (16 x 32768 tokens, when it was tried: 6 parts 115, 12 parts 107).
 // Parts of the tiles: a unit holds one workgroup (three at 64 elements), and what counts is how many turns of them there are and how long
 // each is: turns * (steps of a part + 4 to begin with), and a step for a million elements of the parts' results, written and read.  One
 // more workgroup than the units hold makes it two turns.  us at 8000 tokens and 8 key heads: one sequence of 1600 columns, 4 parts (224

@@ -13,7 +13,7 @@
 // and A and B are the same for all query heads of a row, and for all its key heads: three operations an element.
 //
 // 4001 rows of 64 query and 8 key heads take 39 us, 3.8 TB/s read and written (a copy of them 31).  A write of keys and values alone is
-// bound by vector issue: 10004 rows of 8 + 8 heads 23.5 us, 75 % of it issuing the 17 operations that an element takes.
+// bound by vector issue: 10004 rows of 8 + 8 heads 23.5 us, 74 % of it issuing the 17 operations that an element takes.
 #include <type_traits>
 
 #include "kmq_kv.h"
