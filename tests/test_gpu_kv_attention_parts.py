@@ -55,6 +55,7 @@ CASES = [
     (ONE, 1, 257, 128, 3, None, False), (ONE, 1, 257, 64, 3, None, False), (ONE, 1, 257, 256, 3, None, False), (ONE, 3, 1500, 256, 2, None, False),
     (ONE, 1, 3000, 64, 2, None, True), (ONE, 1, 3000, 128, 4, None, True), (ONE, 1, 3000, 256, 3, None, True), (ONE, 2, 5000, 256, 5, None, True),
     (TWO, 9, 1900, 128, 3, 64, False), (TWO, 9, 1900, 64, 3, 64, False), (TWO, 20, 2500, 128, 1, None, True), (TWO, 20, 2500, 64, 1, None, True),
+    (TILE, 300, 5000, 64, 1, None, True), (TILE, 300, 4000, 128, 1, None, True), (TILE, 150, 3000, 256, 1, None, True),
     (TILE, 250, 1500, 64, 3, None, False), (TILE, 250, 1500, 128, 3, None, False), (TILE, 250, 1500, 256, 3, None, False),
 ]
 
