@@ -440,6 +440,94 @@ kmq_status kmq_kv_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch
 /* As kmq_kernel_name, for the attention. */
 const char* kmq_kernel_name_kv_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch, int q_heads);
 
+/* ---- Norms around a block, and a mixture of experts for a few tokens -------------------
+ * What follows the attention in a decoder layer whose MLP is a mixture of experts: its output goes into the residual stream, the
+ * stream is normalised, a router chooses experts for every token, these are run, and their output goes into the stream again.
+ * Rows are bf16; strides are multiples of 8 elements, at least as long as the row (KMQ_ERR_SHAPE), and rows start 16-byte aligned.  A
+ * call with 0 rows does nothing and succeeds.  Outputs overlap no input, but where a call says so. */
+
+/* How a block's output joins the residual stream.  A host structure, read during the call; what it points to is device memory.
+ *     n = x * post_gain / sqrt( (1/H) sum_j x_j^2 + eps )      (post_norm = 1; else n = x)
+ *     s = residual_scale * residual + scale * g * n            g = gate, or 1 / (1 + exp(-gate)) where gate_sigmoid is 1, or 1
+ *     out = s,   normed = s * pre_gain / sqrt( (1/H) sum_j s_j^2 + eps )
+ * Computed in 64 bits (s goes into the second norm unrounded), rounded to 32 and then to bf16 (nearest even); infinities and NaN as the
+ * formulas have them. */
+typedef struct kmq_block_join {
+    const uint16_t* residual;   /* rows of H bf16, or NULL: none (zeros) */
+    const uint16_t* gate;       /* rows of H bf16, or NULL */
+    const uint16_t* post_gain;  /* H bf16, 16-byte aligned, or NULL: unit gains */
+    const uint16_t* pre_gain;
+    int64_t residual_stride;
+    int64_t gate_stride;        /* 0: one row of gates for all rows */
+    float scale, residual_scale;
+    float eps;                  /* >= 0 */
+    int32_t post_norm, gate_sigmoid;
+} kmq_block_join;
+
+/* The block's output x (rows of H = width elements, a multiple of 8 up to 32768) joined, in one launch.  out or normed may be NULL, not both.
+ * out may be x's or the residual's own place, normed x's (same strides). */
+kmq_status kmq_block_norm(const uint16_t* x, int64_t x_stride, int64_t rows, int64_t width, const kmq_block_join* join,
+                          uint16_t* out, int64_t out_stride, uint16_t* normed, int64_t normed_stride, void* hip_stream);
+
+#define KMQ_MOE_MAX_EXPERTS 1024
+#define KMQ_MOE_MAX_TOP_K 16
+#define KMQ_MOE_MAX_ROWS 128    /* of kmq_moe_experts */
+
+/* How experts are chosen.  A host structure, read during the call; what it points to is device memory.
+ *     l_e = sum_k X_k W_ek,   s = softmax(l), or 1 / (1 + exp(-l)) where `sigmoid` is 1,   c = s + bias
+ *     groups > 1: the experts are that many groups of neighbours; the top_groups of them whose two largest c have the largest sum stay
+ *     the top_k experts with the largest c, in descending order; weight = s_e, divided by the sum of the chosen (normalise = 1; a sum of
+ *     zero: weights of zero), times scale
+ * Equal values go to the lower index.  A NaN counts as minus infinity for its group, and is chosen behind everything else.
+ * Computed in 64 bits, weights rounded to fp32. */
+typedef struct kmq_moe_router {
+    const uint16_t* weights;    /* experts x width bf16, 16-byte aligned */
+    const float* bias;          /* one an expert, or NULL */
+    int64_t width;              /* a multiple of 8, at most 65536 */
+    int32_t experts;            /* 1 .. KMQ_MOE_MAX_EXPERTS */
+    int32_t top_k;              /* 1 .. KMQ_MOE_MAX_TOP_K, at most the experts of top_groups groups */
+    int32_t groups, top_groups; /* groups: at most 64, divides experts; 1, 1: no groups */
+    int32_t sigmoid, normalise;
+    float scale;
+} kmq_moe_router;
+
+/* Choice of experts for `rows` rows of x (any number up to 2^20, rows * experts <= 2^28): ids and gates, rows x top_k.
+ *   workspace  kmq_moe_route_workspace_bytes() bytes, 16-byte aligned, not initialised (0 on bad arguments) */
+size_t kmq_moe_route_workspace_bytes(int64_t rows, int experts, int64_t width);
+kmq_status kmq_moe_route(const uint16_t* x, int64_t x_stride, int64_t rows, const kmq_moe_router* router, int32_t* ids, float* gates,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The experts' matrices in the block-scaled format, KMQ_LAYOUT_TILED, one after the other: expert e of a matrix of N rows and K columns has
+ * its words at e * kmq_tiled_words(N, K, bits, KMQ_LAYOUT_TILED), its codebook at e * 2^bits, its scales at e * N * K / 64.
+ * Host structures, read during the call. */
+typedef struct kmq_moe_matrix {
+    const uint32_t* words;      /* device, 16-byte aligned */
+    const uint16_t* codebooks;  /* device, 2^bits bf16 an expert; 4-byte aligned */
+    const uint16_t* scales;     /* device, N x K / 64 bf16 an expert; 16-byte aligned */
+} kmq_moe_matrix;
+typedef struct kmq_moe_weights {
+    kmq_moe_matrix gate, up;    /* width rows of hidden columns */
+    kmq_moe_matrix down;        /* hidden rows of width columns */
+    int64_t hidden, width;      /* whole super-blocks: multiples of 512, 256, 128, 128 for bits = 1..4 (KMQ_ERR_LAYOUT); at most 65536.  A narrower
+                                   expert is padded with rows and columns whose scales are zero. */
+    int32_t experts, bits;      /* experts: 1 .. KMQ_MOE_MAX_EXPERTS; bits: 1..4 */
+} kmq_moe_weights;
+
+/* The chosen experts' SwiGLU for a few tokens, in two launches (each active expert's matrices are read once for up to 64 of its tokens):
+ *     h = bf16( silu(G_e x) * (U_e x) ),   y = residual + sum_j gates[j] * D_e h           e = ids[j], j = 0 .. top_k - 1
+ * silu(t) = t / (1 + exp(-t)); all sums in fp32, h rounded to bf16 as kmq_gemv_swiglu leaves it (2^-8 of itself at most), y once more.
+ *   x, residual, y   rows of `hidden` elements, x_stride at most 2^22; residual may be NULL, and y's own place
+ *   ids, gates       rows x top_k, from kmq_moe_route or anybody else.  An id outside 0 .. experts - 1 counts for nothing (an expert
+ *                    that is held elsewhere, a token that is none); an expert that a token has twice counts with the sum of both gates
+ *   workspace        kmq_moe_experts_workspace_bytes() bytes, 16-byte aligned, not initialised (0 on bad arguments)
+ * rows: 0 .. KMQ_MOE_MAX_ROWS (KMQ_ERR_SHAPE); more are cut into several calls, and prompts are better served by kmq_dequant_blockscaled
+ * and dense products.  Launches and workspace do not depend on the choices, so a captured call may be replayed with others.  A token's
+ * output depends on no other token's elements; experts that are not chosen are not read. */
+size_t kmq_moe_experts_workspace_bytes(const kmq_moe_weights* weights, int64_t rows, int top_k);
+kmq_status kmq_moe_experts(const kmq_moe_weights* weights, const uint16_t* x, int64_t x_stride, int64_t rows, const int32_t* ids,
+                           const float* gates, int top_k, const uint16_t* residual, int64_t residual_stride, uint16_t* y, int64_t y_stride,
+                           void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Name of the kernel variant the launch heuristic picks for this problem
  * (static string, never NULL; "invalid" on bad arguments).  For reports. */
 const char* kmq_kernel_name(int64_t N, int64_t K, int bits, int M, int layout);

@@ -17,7 +17,7 @@ OUT = os.path.join(HERE, "libkmq.so")
 PROBE_OUT = os.path.join(HERE, "probe", "libkmq_probe.so")
 OBJ_DIR = os.path.join(ROOT, "_build")
 
-SOURCES = ["kmq_host.cpp", "kmq_generic.hip", "kmq_lut.hip", "kmq_lut_columns.hip", "kmq_lut_loop.hip", "kmq_rowlane.hip", "kmq_mfma.hip", "kmq_mfma_kslice.hip", "kmq_mfma_any_b1.hip", "kmq_mfma_any_b2.hip", "kmq_mfma_any_b3.hip", "kmq_mfma_any_b4.hip", "kmq_mfma_b8.hip", "kmq_blockscaled.hip", "kmq_dense.hip", "kmq_quantize.hip", "kmq_fused.hip", "kmq_heads.hip", "kmq_attention.hip", "kmq_api.hip"]
+SOURCES = ["kmq_host.cpp", "kmq_generic.hip", "kmq_lut.hip", "kmq_lut_columns.hip", "kmq_lut_loop.hip", "kmq_rowlane.hip", "kmq_mfma.hip", "kmq_mfma_kslice.hip", "kmq_mfma_any_b1.hip", "kmq_mfma_any_b2.hip", "kmq_mfma_any_b3.hip", "kmq_mfma_any_b4.hip", "kmq_mfma_b8.hip", "kmq_blockscaled.hip", "kmq_dense.hip", "kmq_quantize.hip", "kmq_fused.hip", "kmq_heads.hip", "kmq_attention.hip", "kmq_norm.hip", "kmq_route.hip", "kmq_moe.hip", "kmq_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # packed-fp32 code generation is switched off on purpose: some packed forms have given
          # wrong results on this hardware; ordinary float code loses nothing measurable here

@@ -260,6 +260,34 @@ static void set_turn(HeadsArgs& a, const kmq_head_turn* t) {
     a.inv_freq = t->inv_freq;
 }
 
+// ---- norms around a block, mixture of experts ----
+static bool row_of(int64_t stride, int64_t width, int64_t most) { return stride % 8 == 0 && stride >= width && stride <= most; }
+constexpr int64_t kMaxStride = int64_t(1) << 31, kMaxMoeStride = int64_t(1) << 22, kMaxMoeDim = 65536, kMaxNormWidth = 32768;
+
+static kmq_status check_router(const kmq_moe_router* r) {
+    if (!r || !r->weights) return KMQ_ERR_NULL;
+    if (r->width < 8 || r->width % 8 || r->width > kMaxMoeDim || r->experts < 1 || r->experts > KMQ_MOE_MAX_EXPERTS) return KMQ_ERR_SHAPE;
+    if (r->groups < 1 || r->groups > 64 || r->experts % r->groups || r->top_groups < 1 || r->top_groups > r->groups) return KMQ_ERR_SHAPE;
+    if (r->top_k < 1 || r->top_k > KMQ_MOE_MAX_TOP_K || r->top_k > r->experts / r->groups * r->top_groups) return KMQ_ERR_SHAPE;
+    if ((r->sigmoid != 0 && r->sigmoid != 1) || (r->normalise != 0 && r->normalise != 1) || !(r->scale - r->scale == 0.f)) return KMQ_ERR_SHAPE;
+    if (!aligned(r->weights, 16) || !aligned(r->bias, 4)) return KMQ_ERR_ALIGN;
+    return KMQ_OK;
+}
+static bool route_rows_valid(int64_t rows, int64_t experts) { return rows >= 0 && rows <= (int64_t(1) << 20) && rows * experts <= (int64_t(1) << 28); }
+
+static kmq_status check_matrix(const kmq_moe_matrix& m) {
+    if (!m.words || !m.codebooks || !m.scales) return KMQ_ERR_NULL;
+    return aligned(m.words, 16) && aligned(m.codebooks, 4) && aligned(m.scales, 16) ? KMQ_OK : KMQ_ERR_ALIGN;
+}
+// Sizes only: enough for the workspace.
+static kmq_status check_moe_shape(const kmq_moe_weights* w, int64_t rows, int top_k) {
+    if (!w) return KMQ_ERR_NULL;
+    if (w->bits < 1 || w->bits > 4) return KMQ_ERR_BITS;
+    if (w->hidden < 1 || w->width < 1 || w->hidden > kMaxMoeDim || w->width > kMaxMoeDim || w->experts < 1 || w->experts > KMQ_MOE_MAX_EXPERTS ||
+        rows < 0 || rows > KMQ_MOE_MAX_ROWS || top_k < 1 || top_k > KMQ_MOE_MAX_TOP_K) return KMQ_ERR_SHAPE;
+    return tiled_valid(w->bits, w->hidden) && tiled_valid(w->bits, w->width) ? KMQ_OK : KMQ_ERR_LAYOUT;
+}
+
 }  // namespace kmq
 
 extern "C" {
@@ -579,6 +607,70 @@ kmq_status kmq_kv_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch
     if (need > 0 && (!workspace || workspace_bytes < need)) return KMQ_ERR_WORKSPACE;
     if (need > 0 && !kmq::aligned(workspace, 16)) return KMQ_ERR_ALIGN;
     return kmq::hip_status(kmq::launch_attention(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+kmq_status kmq_block_norm(const uint16_t* x, int64_t x_stride, int64_t rows, int64_t width, const kmq_block_join* join,
+                          uint16_t* out, int64_t out_stride, uint16_t* normed, int64_t normed_stride, void* hip_stream) {
+    if (!x || !join || (!out && !normed)) return KMQ_ERR_NULL;
+    if (rows < 0 || rows > kmq::kMaxDim || width < 8 || width % 8 || width > kmq::kMaxNormWidth) return KMQ_ERR_SHAPE;
+    if ((join->post_norm != 0 && join->post_norm != 1) || (join->gate_sigmoid != 0 && join->gate_sigmoid != 1) || !(join->eps >= 0.f) ||
+        !(join->scale - join->scale == 0.f) || !(join->residual_scale - join->residual_scale == 0.f)) return KMQ_ERR_SHAPE;
+    if (!kmq::row_of(x_stride, width, kmq::kMaxStride) || (join->residual && !kmq::row_of(join->residual_stride, width, kmq::kMaxStride)) ||
+        (join->gate && join->gate_stride && !kmq::row_of(join->gate_stride, width, kmq::kMaxStride)) ||
+        (out && !kmq::row_of(out_stride, width, kmq::kMaxStride)) || (normed && !kmq::row_of(normed_stride, width, kmq::kMaxStride))) return KMQ_ERR_SHAPE;
+    if (!kmq::aligned(x, 16) || !kmq::aligned(join->residual, 16) || !kmq::aligned(join->gate, 16) || !kmq::aligned(join->post_gain, 16) ||
+        !kmq::aligned(join->pre_gain, 16) || !kmq::aligned(out, 16) || !kmq::aligned(normed, 16)) return KMQ_ERR_ALIGN;
+    const kmq::BlockNormArgs a{x, join->residual, join->gate, join->post_gain, join->pre_gain, x_stride, join->residual_stride, join->gate_stride,
+                               rows, width, join->scale, join->residual_scale, join->eps, join->post_norm != 0, join->gate && join->gate_sigmoid,
+                               out, normed, out_stride, normed_stride};
+    return kmq::hip_status(kmq::launch_block_norm(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t kmq_moe_route_workspace_bytes(int64_t rows, int experts, int64_t width) {
+    if (experts < 1 || experts > KMQ_MOE_MAX_EXPERTS || width < 8 || width % 8 || width > kmq::kMaxMoeDim || !kmq::route_rows_valid(rows, experts)) return 0;
+    return static_cast<size_t>(rows) * experts * (rows ? kmq::route_slices(rows, experts, width) : 0) * sizeof(double);
+}
+
+kmq_status kmq_moe_route(const uint16_t* x, int64_t x_stride, int64_t rows, const kmq_moe_router* router, int32_t* ids, float* gates,
+                         void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!x || !ids || !gates) return KMQ_ERR_NULL;
+    const kmq_status c = kmq::check_router(router);
+    if (c != KMQ_OK) return c;
+    if (!kmq::route_rows_valid(rows, router->experts) || !kmq::row_of(x_stride, router->width, kmq::kMaxStride)) return KMQ_ERR_SHAPE;
+    if (!kmq::aligned(x, 16) || !kmq::aligned(ids, 4) || !kmq::aligned(gates, 4)) return KMQ_ERR_ALIGN;
+    const size_t need = kmq_moe_route_workspace_bytes(rows, router->experts, router->width);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return KMQ_ERR_WORKSPACE;
+    if (need > 0 && !kmq::aligned(workspace, 16)) return KMQ_ERR_ALIGN;
+    const kmq::RouteArgs a{x, router->weights, router->bias, x_stride, router->width, static_cast<int>(rows), router->experts, router->top_k,
+                           router->groups, router->top_groups, router->sigmoid != 0, router->normalise != 0, router->scale, ids, gates, workspace};
+    return kmq::hip_status(kmq::launch_route(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t kmq_moe_experts_workspace_bytes(const kmq_moe_weights* weights, int64_t rows, int top_k) {
+    return kmq::check_moe_shape(weights, rows, top_k) == KMQ_OK ? kmq::moe_workspace_bytes(rows, top_k, weights->width) : 0;
+}
+
+kmq_status kmq_moe_experts(const kmq_moe_weights* weights, const uint16_t* x, int64_t x_stride, int64_t rows, const int32_t* ids,
+                           const float* gates, int top_k, const uint16_t* residual, int64_t residual_stride, uint16_t* y, int64_t y_stride,
+                           void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!x || !ids || !gates || !y) return KMQ_ERR_NULL;
+    const kmq_status c = kmq::check_moe_shape(weights, rows, top_k);
+    if (c != KMQ_OK) return c;
+    for (const kmq_moe_matrix* m : {&weights->gate, &weights->up, &weights->down}) {
+        const kmq_status s = kmq::check_matrix(*m);
+        if (s != KMQ_OK) return s;
+    }
+    const int64_t hidden = weights->hidden, width = weights->width;
+    if (!kmq::row_of(x_stride, hidden, kmq::kMaxMoeStride) || (residual && !kmq::row_of(residual_stride, hidden, kmq::kMaxStride)) ||
+        !kmq::row_of(y_stride, hidden, kmq::kMaxStride)) return KMQ_ERR_SHAPE;
+    if (!kmq::aligned(x, 16) || !kmq::aligned(residual, 16) || !kmq::aligned(y, 16) || !kmq::aligned(ids, 4) || !kmq::aligned(gates, 4)) return KMQ_ERR_ALIGN;
+    const size_t need = kmq::moe_workspace_bytes(rows, top_k, width);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return KMQ_ERR_WORKSPACE;
+    if (need > 0 && !kmq::aligned(workspace, 16)) return KMQ_ERR_ALIGN;
+    const auto matrix = [](const kmq_moe_matrix& m, int64_t n) { return kmq::MoeMatrix{m.words, m.codebooks, m.scales, n}; };
+    const kmq::MoeArgs a{matrix(weights->gate, width), matrix(weights->up, width), matrix(weights->down, hidden), hidden, width, weights->experts, weights->bits,
+                         x, residual, x_stride, residual_stride, y_stride, static_cast<int>(rows), top_k, ids, gates, y, workspace};
+    return kmq::hip_status(kmq::launch_moe(a, static_cast<hipStream_t>(hip_stream)));
 }
 
 const char* kmq_last_hip_error(void) { return kmq::g_last_hip_error; }

@@ -62,6 +62,33 @@ __device__ __forceinline__ float group_sum_scaled(float v, float scale) {
     return group_sum_of_pairs<LANES>(fmaf(v, scale, dpp_move<0xB1>(v * scale)));
 }
 
+template <int CTRL>
+__device__ __forceinline__ double dpp_move64(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, 0xF, 0xF, true));
+    const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, 0xF, 0xF, true));
+    return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+// The sum over groups of LANES lanes, in all of them.
+template <int LANES>
+__device__ __forceinline__ double sum_over(double v) {
+    v += dpp_move64<0xB1>(v);                             // quad_perm [1,0,3,2]
+    v += dpp_move64<0x4E>(v);                             // quad_perm [2,3,0,1]
+    v += dpp_move64<0x141>(v);                            // row_half_mirror
+    if (LANES >= 16) v += dpp_move64<0x140>(v);           // row_mirror
+    if (LANES >= 32) v += __shfl_xor(v, 16);
+    if (LANES >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+// 1 / sqrt(v): the unit's estimate and two Newton steps, each of which doubles its good bits.  Of an infinity it is zero, which the steps
+// would make a NaN: an infinite element is one after a norm (infinity times zero), the finite ones beside it are zeros.
+__device__ __forceinline__ double inverse_root(double v) {
+    double y = __builtin_amdgcn_rsq(v);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) y *= fma(-0.5 * v * y, y, 1.5);
+    return v == __builtin_inf() ? 0.0 : y;
+}
+
 // Index of element k of row n read from the tiled stream (slow path: used by the
 // shape-agnostic kernels only).
 __device__ __forceinline__ uint32_t tiled_fetch_index(const uint32_t* W, int bits, int64_t K, int64_t n, int64_t k) {

@@ -167,6 +167,52 @@ constexpr int64_t kMaxAttentionWorkgroups = int64_t(1) << 22;    // (threads of 
 AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads);
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t s);
 
+// ---- Norms around a block, and a mixture of experts ----
+struct BlockNormArgs {
+    const uint16_t *x, *residual, *gate, *post_gain, *pre_gain;   // all but x: or nullptr
+    int64_t x_stride, residual_stride, gate_stride;               // elements from row to row
+    int64_t rows, width;
+    float scale, residual_scale, eps;
+    bool post_norm, sigmoid;
+    uint16_t *out, *normed;                                       // one of them may be nullptr
+    int64_t out_stride, normed_stride;
+};
+hipError_t launch_block_norm(const BlockNormArgs& a, hipStream_t s);
+
+struct RouteArgs {
+    const uint16_t *x, *router;
+    const float* bias;                   // or nullptr
+    int64_t x_stride, width;
+    int rows, experts, top_k, groups, top_groups;
+    bool sigmoid, normalise;
+    float scale;
+    int32_t* ids;
+    float* gates;
+    void* workspace;                     // route_slices() x rows x experts doubles
+};
+int route_slices(int64_t rows, int64_t experts, int64_t width);
+hipError_t launch_route(const RouteArgs& a, hipStream_t s);
+
+struct MoeMatrix {
+    const uint32_t* words;
+    const uint16_t *books, *scales;
+    int64_t rows;                        // of one expert
+};
+struct MoeArgs {
+    MoeMatrix gate, up, down;
+    int64_t hidden, width;
+    int experts, bits;
+    const uint16_t *x, *residual;        // residual: or nullptr
+    int64_t x_stride, residual_stride, y_stride;
+    int rows, top_k;
+    const int32_t* ids;
+    const float* gates;
+    uint16_t* y;
+    void* workspace;
+};
+size_t moe_workspace_bytes(int64_t rows, int64_t top_k, int64_t width);
+hipError_t launch_moe(const MoeArgs& a, hipStream_t s);
+
 }  // namespace kmq
 
 #endif

@@ -104,6 +104,16 @@ _lib.kmq_kv_attention.restype = ctypes.c_int32
 _lib.kmq_kv_attention.argtypes = [_vp, _vp, _vp, _i64, _int, ctypes.c_float, _int, _int, _vp, _i64, _vp, _vp, _sz, _vp]
 _lib.kmq_kernel_name_kv_attention.restype = ctypes.c_char_p
 _lib.kmq_kernel_name_kv_attention.argtypes = [_vp, _vp, _int]
+_lib.kmq_block_norm.restype = ctypes.c_int32
+_lib.kmq_block_norm.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp]
+_lib.kmq_moe_route_workspace_bytes.restype = _sz
+_lib.kmq_moe_route_workspace_bytes.argtypes = [_i64, _int, _i64]
+_lib.kmq_moe_route.restype = ctypes.c_int32
+_lib.kmq_moe_route.argtypes = [_vp, _i64, _i64, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.kmq_moe_experts_workspace_bytes.restype = _sz
+_lib.kmq_moe_experts_workspace_bytes.argtypes = [_vp, _i64, _int]
+_lib.kmq_moe_experts.restype = ctypes.c_int32
+_lib.kmq_moe_experts.argtypes = [_vp, _vp, _i64, _i64, _vp, _vp, _int, _vp, _i64, _vp, _i64, _vp, _sz, _vp]
 _lib.kmq_last_hip_error.restype = ctypes.c_char_p
 _lib.kmq_last_hip_error.argtypes = []
 _lib.kmq_status_string.restype = ctypes.c_char_p
@@ -430,3 +440,90 @@ def kv_attention(cache: KvCache, batch: KvBatch, q, q_stride: int, out, out_stri
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(_lib.kmq_kv_attention(cache._at, batch._at, _ptr(q), q_stride, q_heads, scale, 1 if causal else 0, window, _ptr(out), out_stride,
                                  _ptr(lse), _ptr(workspace), ws_bytes, _stream()))
+
+
+# ---- norms around a block, mixture of experts ---------------------------------------------------------------------------
+
+MOE_MAX_ROWS, MOE_MAX_TOP_K, MOE_MAX_EXPERTS = 128, 16, 1024
+
+
+class _JoinStruct(ctypes.Structure):
+    _fields_ = [("residual", _vp), ("gate", _vp), ("post_gain", _vp), ("pre_gain", _vp), ("residual_stride", _i64), ("gate_stride", _i64),
+                ("scale", ctypes.c_float), ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float), ("post_norm", ctypes.c_int32),
+                ("gate_sigmoid", ctypes.c_int32)]
+
+
+class _RouterStruct(ctypes.Structure):
+    _fields_ = [("weights", _vp), ("bias", _vp), ("width", _i64), ("experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("top_groups", ctypes.c_int32), ("sigmoid", ctypes.c_int32), ("normalise", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class _MatrixStruct(ctypes.Structure):
+    _fields_ = [("words", _vp), ("codebooks", _vp), ("scales", _vp)]
+
+
+class _WeightsStruct(ctypes.Structure):
+    _fields_ = [("gate", _MatrixStruct), ("up", _MatrixStruct), ("down", _MatrixStruct), ("hidden", _i64), ("width", _i64), ("experts", ctypes.c_int32),
+                ("bits", ctypes.c_int32)]
+
+
+def block_norm(x, x_stride: int, rows: int, width: int, out=None, out_stride: int = 0, normed=None, normed_stride: int = 0, residual=None,
+               residual_stride: int = 0, residual_scale: float = 1.0, gate=None, gate_stride: int = 0, gate_sigmoid: bool = False, post_norm=None,
+               post_gain=None, pre_gain=None, eps: float = 0.0, scale: float = 1.0):
+    """A block's output x joined with the residual stream, and the stream normalised for the next block, in one launch on torch's current
+    stream: out = residual_scale * residual + scale * gate * rmsnorm(x; post_gain), normed = rmsnorm(out; pre_gain).
+    post_norm defaults to "post_gain was given"; gate_stride 0: one row of gates for all rows."""
+    if post_norm is None:
+        post_norm = post_gain is not None
+    join = _JoinStruct(_ptr(residual), _ptr(gate), _ptr(post_gain), _ptr(pre_gain), residual_stride, gate_stride, scale, residual_scale, eps,
+                       1 if post_norm else 0, 1 if gate_sigmoid else 0)
+    _check(_lib.kmq_block_norm(_ptr(x), x_stride, rows, width, ctypes.addressof(join), _ptr(out), out_stride, _ptr(normed), normed_stride, _stream()))
+
+
+def moe_route_workspace_bytes(rows: int, experts: int, width: int) -> int:
+    return int(_lib.kmq_moe_route_workspace_bytes(rows, experts, width))
+
+
+def moe_route(x, x_stride: int, rows: int, router, experts: int, width: int, ids, gates, top_k: int, sigmoid: bool = False, bias=None, groups: int = 1,
+              top_groups: int = 1, normalise: bool = True, scale: float = 1.0, workspace=None):
+    """Experts of every row of x (ids int32, gates fp32; rows x top_k) by a router of experts x width bf16, on torch's current stream.
+    workspace: moe_route_workspace_bytes() device bytes."""
+    r = _RouterStruct(_ptr(router), _ptr(bias), width, experts, top_k, groups, top_groups, 1 if sigmoid else 0, 1 if normalise else 0, scale)
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_lib.kmq_moe_route(_ptr(x), x_stride, rows, ctypes.addressof(r), _ptr(ids), _ptr(gates), _ptr(workspace), ws_bytes, _stream()))
+
+
+class MoeWeights:
+    """The experts' matrices in the block-scaled format, tiled layout (include/kmq.h): packed words, codebooks (2^bits bf16 an expert) and
+    scales of gate, up (width x hidden) and down (hidden x width).  Keeps them alive; made once, handed to every call."""
+
+    def __init__(self, gate, up, down, gate_codebooks, up_codebooks, down_codebooks, gate_scales, up_scales, down_scales, experts: int, hidden: int,
+                 width: int, bits: int):
+        size = lambda t: t.numel() * t.element_size()  # noqa: E731
+        for words, books, scales, n, k in ((gate, gate_codebooks, gate_scales, width, hidden), (up, up_codebooks, up_scales, width, hidden),
+                                           (down, down_codebooks, down_scales, hidden, width)):
+            each = tiled_words(n, k, bits, LAYOUT_TILED)
+            if each < 0:
+                raise KmqError(2 if not 1 <= bits <= 4 else 7)
+            if experts < 1 or size(words) < experts * each * 4 or size(books) < experts * 2 * 2 ** bits or size(scales) < experts * n * (k // 64) * 2:
+                raise KmqError(3)
+            if not (words.is_contiguous() and books.is_contiguous() and scales.is_contiguous()):
+                raise KmqError(3)
+        self.tensors = (gate, up, down, gate_codebooks, up_codebooks, down_codebooks, gate_scales, up_scales, down_scales)
+        self.experts, self.hidden, self.width, self.bits = experts, hidden, width, bits
+        self._struct = _WeightsStruct(_MatrixStruct(_ptr(gate), _ptr(gate_codebooks), _ptr(gate_scales)), _MatrixStruct(_ptr(up), _ptr(up_codebooks), _ptr(up_scales)),
+                                      _MatrixStruct(_ptr(down), _ptr(down_codebooks), _ptr(down_scales)), hidden, width, experts, bits)
+        self._at = ctypes.addressof(self._struct)
+
+
+def moe_experts_workspace_bytes(weights: MoeWeights, rows: int, top_k: int) -> int:
+    return int(_lib.kmq_moe_experts_workspace_bytes(weights._at, rows, top_k))
+
+
+def moe_experts(weights: MoeWeights, x, x_stride: int, rows: int, ids, gates, top_k: int, y, y_stride: int, residual=None, residual_stride: int = 0,
+                workspace=None):
+    """y = residual + sum over a row's top_k experts of gate * down(silu(gate x) * up x), for up to MOE_MAX_ROWS rows, on torch's current
+    stream.  workspace: moe_experts_workspace_bytes() device bytes."""
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_lib.kmq_moe_experts(weights._at, _ptr(x), x_stride, rows, _ptr(ids), _ptr(gates), top_k, _ptr(residual), residual_stride, _ptr(y), y_stride,
+                                _ptr(workspace), ws_bytes, _stream()))

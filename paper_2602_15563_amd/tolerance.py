@@ -62,3 +62,22 @@ def attention_bound(out, spread, size, tokens, head_dim):
     d = attention_lse_bound(size, tokens, head_dim)[..., None]
     inner = (2 * d * (1 + d) + 2 * 2.0 ** -8 + (tokens + 8) * 2.0 ** -23) * spread
     return inner + 2.0 ** -8 * (np.abs(out) + inner)
+
+
+def moe_bound(y, pairs, matrices, hidden, width, residual_size):
+    """Output of the experts in bf16.  y: the fp64 result; pairs: what the oracle says of every (token, expert); matrices[e]: the expert's
+    three matrices; residual_size: |residual| or zeros.  A product of K columns in the block-scaled format is good to (K + 16) * 2^-23 of
+    its absolute sum: K products, a rounding per block's scale, the sums of the waves.  silu(g) * u moves as in swiglu_bound, and
+    its own arithmetic takes 8 roundings, of which exp(-g) has 2 |g| 2^-24 more (its argument is rounded).  h is then rounded to
+    bf16 (2^-8 of itself).  The second product carries h's error through |D|; gates, waves and residual are a sum of the pairs' terms, each
+    of which may be rounded once a pair and once a wave; the result is rounded to bf16."""
+    bound = (len(pairs) + 24) * 2.0 ** -23 * residual_size
+    for p in pairs:
+        dg, du = (hidden + 16) * 2.0 ** -23 * p["g_size"], (hidden + 16) * 2.0 ** -23 * p["u_size"]
+        silu = np.abs(p["g"]) / (1 + np.exp(-p["g"]))
+        dh = 1.1 * np.abs(p["u"]) * dg + silu * du + 1.1 * dg * du + (8 + np.abs(p["g"])) * 2.0 ** -23 * np.abs(p["h"])
+        dh = dh + 2.0 ** -8 * (np.abs(p["h"]) + dh)
+        D = np.abs(matrices[p["expert"]][2])
+        size = D @ (np.abs(p["h"]) + dh)
+        bound[p["token"]] += abs(p["weight"]) * (D @ dh + (width + 16 + len(pairs) + 24) * 2.0 ** -23 * size)
+    return bound + 2.0 ** -8 * (np.abs(y) + bound)
