@@ -647,7 +647,7 @@ kmq_status kmq_moe_route(const uint16_t* x, int64_t x_stride, int64_t rows, cons
 }
 
 size_t kmq_moe_experts_workspace_bytes(const kmq_moe_weights* weights, int64_t rows, int top_k) {
-    return kmq::check_moe_shape(weights, rows, top_k) == KMQ_OK ? kmq::moe_workspace_bytes(rows, top_k, weights->width) : 0;
+    return kmq::check_moe_shape(weights, rows, top_k) == KMQ_OK ? kmq::moe_workspace_bytes(rows, top_k, weights->width, weights->hidden) : 0;
 }
 
 kmq_status kmq_moe_experts(const kmq_moe_weights* weights, const uint16_t* x, int64_t x_stride, int64_t rows, const int32_t* ids,
@@ -664,7 +664,7 @@ kmq_status kmq_moe_experts(const kmq_moe_weights* weights, const uint16_t* x, in
     if (!kmq::row_of(x_stride, hidden, kmq::kMaxMoeStride) || (residual && !kmq::row_of(residual_stride, hidden, kmq::kMaxStride)) ||
         !kmq::row_of(y_stride, hidden, kmq::kMaxStride)) return KMQ_ERR_SHAPE;
     if (!kmq::aligned(x, 16) || !kmq::aligned(residual, 16) || !kmq::aligned(y, 16) || !kmq::aligned(ids, 4) || !kmq::aligned(gates, 4)) return KMQ_ERR_ALIGN;
-    const size_t need = kmq::moe_workspace_bytes(rows, top_k, width);
+    const size_t need = kmq::moe_workspace_bytes(rows, top_k, width, hidden);
     if (need > 0 && (!workspace || workspace_bytes < need)) return KMQ_ERR_WORKSPACE;
     if (need > 0 && !kmq::aligned(workspace, 16)) return KMQ_ERR_ALIGN;
     const auto matrix = [](const kmq_moe_matrix& m, int64_t n) { return kmq::MoeMatrix{m.words, m.codebooks, m.scales, n}; };

@@ -210,7 +210,7 @@ struct MoeArgs {
     uint16_t* y;
     void* workspace;
 };
-size_t moe_workspace_bytes(int64_t rows, int64_t top_k, int64_t width);
+size_t moe_workspace_bytes(int64_t rows, int64_t top_k, int64_t width, int64_t hidden);
 hipError_t launch_moe(const MoeArgs& a, hipStream_t s);
 
 }  // namespace kmq

@@ -2,15 +2,23 @@
 //
 //     h_p = silu(G_e x) * (U_e x),   y = residual + sum_j gate_j * D_e h_p            pair p = (token, j), e = its expert
 //
-// Every expert that some token chose is read once.  Both kernels build the list of these experts from the choices themselves (so the
+// Every expert that some token chose is read once.  The kernels build the list of these experts from the choices themselves (so the
 // launches do not depend on them, and a captured call may be replayed with others) and gather the tokens of an expert as the
 // columns of matrix steps: v_mfma_f32_16x16x32_bf16 with the tokens first, so that what belongs to a row of the
 // matrix (its scales) is needed by the lane that holds it.  Columns do not mix: what one token holds reaches no other.
-//   gate_up   a workgroup takes 16 rows of both matrices of an expert at a time; its waves split the row, their sums are added in
-//             shared memory, and SwiGLU of the two goes to the workspace, a row a pair, rounded to bf16;
-//   down      a workgroup owns 16 rows of the output for all experts; its waves share the experts' super-blocks evenly, each
-//             adds what it has of an expert, times the pair's weight, to its own sums in shared memory; these are added in the waves' order.
+//
+// Three launches: the rows of G and U (SwiGLU of both goes to the workspace, a row a pair, rounded to bf16), the rows of D (a row a pair
+// again, in fp32), and the sum of a token's pairs.  The first two are one kernel: a wave multiplies 16 rows of two matrices with the same
+// tokens, the gate's and the up projection's, or two blocks of the down projection.  NW waves (a team) split the rows' length, their
+// sums are added in shared memory; the teams of a workgroup share the table of the expert's centroids.  A workgroup takes neighbouring
+// rows of the list of all experts' rows, as many as any other; the first super-blocks of what comes next are asked for before the
+// sums are joined.
 // Block scales: two matrix steps are a block of 64 columns; their sum from zero is multiplied by the block's scale.
+//
+// Decode: tables in shared memory whose entries are ready operand registers, a column a lane modulo 32, so that look-ups never collide
+// whatever the indices are.  2 to 4 bits: a pair of indices (4, 6, 8 bits of a byte of the granule) is an entry of two centroids; at 2 and 3
+// bits it is elements k and k + 4 of a step, and the tokens' elements are brought into that order.  1 bit: four indices, eight bytes.  The
+// index goes into byte 1 of the address by one instruction.
 #include <type_traits>
 
 #include "kmq_kv.h"
@@ -22,12 +30,11 @@ namespace {
 
 // Bundles a wave has asked for, by their registers.
 #ifndef KMQ_RING
-#define KMQ_RING 60
+#define KMQ_RING 30
 #endif
 constexpr int depth(int words) { return words * 4 <= KMQ_RING ? 4 : words * 3 <= KMQ_RING ? 3 : 2; }
 // Waves a SIMD that the registers have to leave room for: as many as an instance needs no spilling for.
-constexpr int gate_up_waves(int bits, int t) { return t > 16 ? 2 : t == 16 && bits <= 2 ? 3 : t == 8 && bits == 1 ? 3 : 4; }
-constexpr int down_waves(int bits, int t) { return t > 16 ? bits == 2 ? 2 : 3 : 4; }
+constexpr int waves_for(int bits, int t) { return bits == 1 || t > 16 || (bits == 2 && t >= 8) || (bits == 3 && t == 16) ? 3 : 4; }
 
 typedef __amdgpu_buffer_rsrc_t Rows;
 // Rows read by byte offset; kNoRow gives zeros.
@@ -41,23 +48,22 @@ template <int BITS> struct Granule {
     static constexpr int STEPS = BITS == 1 ? 16 : BITS == 2 ? 8 : 4;      // matrix steps of 32 columns
     static constexpr int WORDS = STEPS * BITS / 4, COLUMNS = 32 * STEPS, BLOCKS = STEPS / 2;
     uint32_t w[WORDS];
-    uint32_t scale[BLOCKS / 2];                           // of the lane's row, two a word
 };
 
-// 16 rows of one expert's matrix from some unit (super-block) on, as a lane sees them: granules, and the scales of its row.
+// 16 rows of one expert's matrix: granules, and the scales, two blocks a word.  The same in all lanes.
 // (Rows come in whole blocks: their number is a multiple of 128.)
 struct Matrix {
-    const uint32_t* words;                                // the same in all lanes
-    const uint16_t* scales;
+    const uint32_t* words;
+    const uint32_t* scales;
 };
 template <int BITS>
-__device__ __forceinline__ Matrix matrix_of(const MoeMatrix& m, int expert, int block, int units, int unit) {
+__device__ __forceinline__ Matrix matrix_of(const MoeMatrix& m, int expert, int block, int units) {
     using G = Granule<BITS>;
-    const int64_t at = expert * (m.rows >> 4) + block;
-    return {m.words + (at * units + unit) * (64 * G::WORDS), m.scales + (at * 16 * units + unit) * G::BLOCKS};
+    const int64_t at = (expert * (m.rows >> 4) + block) * units;
+    return {m.words + at * (64 * G::WORDS), reinterpret_cast<const uint32_t*>(m.scales) + at * (16 * G::BLOCKS / 2)};
 }
 template <int BITS>
-__device__ __forceinline__ void load_granule(const Matrix& m, int units, int unit, int lane, Granule<BITS>& g) {
+__device__ __forceinline__ void load_granule(const Matrix& m, int unit, int lane, Granule<BITS>& g) {
     using G = Granule<BITS>;
     const uint32_t* p = m.words + unit * (64 * G::WORDS) + lane * G::WORDS;
     if constexpr (G::WORDS == 3) {
@@ -68,115 +74,132 @@ __device__ __forceinline__ void load_granule(const Matrix& m, int units, int uni
         const u32x4_t t = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
         g.w[0] = t[0]; g.w[1] = t[1]; g.w[2] = t[2]; g.w[3] = t[3];
     }
-    const uint16_t* s = m.scales + unit * G::BLOCKS + (lane & 15) * (units * G::BLOCKS);
-    if constexpr (BITS >= 3) {
-        g.scale[0] = *reinterpret_cast<const uint32_t*>(s);
-    } else if constexpr (BITS == 2) {
-        const u32x2_t t = *reinterpret_cast<const u32x2_t*>(s);
-        g.scale[0] = t[0]; g.scale[1] = t[1];
-    } else {
-        const u32x4_t t = *reinterpret_cast<const u32x4_t*>(s);
-        g.scale[0] = t[0]; g.scale[1] = t[1]; g.scale[2] = t[2]; g.scale[3] = t[3];
-    }
 }
 
-// An expert's centroids, ready to be looked up: 1 bit both in registers, 2 and 3 bits their bytes as v_perm_b32 pools, 4 bits a table
-// [centroid][lane] in shared memory (a lane reads its own bank), the centroid in both halves.
-template <int BITS> struct Centroids {
-    uint32_t a, b, c, d;
-};
-typedef uint32_t Table[16][64];
-template <int BITS>
-__device__ __forceinline__ Centroids<BITS> centroids_of(const uint16_t* book) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(book);
-    Centroids<BITS> c = {0, 0, 0, 0};
-    if constexpr (BITS == 1) {
-        c.a = __builtin_amdgcn_perm(w[0], w[0], 0x01000100u);
-        c.b = __builtin_amdgcn_perm(w[0], w[0], 0x03020302u);
-    } else if constexpr (BITS <= 3) {
-        c.a = __builtin_amdgcn_perm(w[1], w[0], 0x06040200u);
-        c.c = __builtin_amdgcn_perm(w[1], w[0], 0x07050301u);
-        c.b = c.a;
-        c.d = c.c;
-        if constexpr (BITS == 3) {
-            c.b = __builtin_amdgcn_perm(w[3], w[2], 0x06040200u);
-            c.d = __builtin_amdgcn_perm(w[3], w[2], 0x07050301u);
-        }
-    }
-    return c;
-}
-// Pairs of entries first, first + step, .. of a 4-bit table.
-__device__ __forceinline__ void fill_table(Table& table, const uint16_t* book, int first, int step, int lane) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(book);
-    for (int e = first; e < 8; e += step) {
-        const uint32_t two = w[e];
-        table[2 * e][lane] = __builtin_amdgcn_perm(two, two, 0x01000100u);
-        table[2 * e + 1][lane] = __builtin_amdgcn_perm(two, two, 0x03020302u);
-    }
-}
-
-// Eight weights of step j.  4 bits: `at` are look-up addresses, byte 0 = lane * 4; byte 1 is the index, with `which` above it (the number of
-// the table behind the one at `table`, in all bytes' upper halves).
-struct LookUp {
-    uint32_t at[8];
-    uint32_t which;
-};
-template <int BITS>
-__device__ __forceinline__ u32x4_t decode(const Granule<BITS>& g, const Centroids<BITS>& c, LookUp& l, uint32_t table, const u32x2_t* masks, int j) {
-    if constexpr (BITS == 1) {
-        const uint32_t b = g.w[j >> 2] >> (8 * (j & 3));
-        const u32x2_t lo = masks[b & 15u], hi = masks[(b >> 4) & 15u];
-        const auto choose = [&](uint32_t m) { return (m & c.b) | (~m & c.a); };
-        return u32x4_t{choose(lo[0]), choose(lo[1]), choose(hi[0]), choose(hi[1])};
-    } else if constexpr (BITS <= 3) {
-        u32x4_t a;
+// A row's length goes by pieces of kPiece columns, whose scales a team keeps in shared memory, [matrix][row][word], rows an odd number of
+// words apart.  They are asked for as they lie, row after row: granule by granule, 4 to 16 bytes of each of 16 rows an instruction, the same
+// lines are asked for from the L2 again and again (16 tokens of 128 experts, 4096 x 1536, 4 bits: SCALES_BEFORE us, and SCALES_NOW).
+constexpr int kPiece = 4096, kPieceWords = kPiece / 128;
+typedef uint32_t PieceScales[2][16 * (kPieceWords + 1)];
+template <int LANES>
+struct Scales {
+    static constexpr int EACH = 16 * kPieceWords / LANES;
+    uint32_t raw[2][EACH];
+    // Words first .. first + words - 1 of 16 rows of `row_words`; `lane` of the team's.
+    __device__ __forceinline__ void load(const Matrix (&m)[2], int row_words, int first, int words, int lane) {
+        const uint32_t inverse = 65536u / words + 1;      // (exact below 512 = 16 rows of 32 words)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint32_t sel;
-            if constexpr (BITS == 2) {
-                const int i = 2 * j + h;
-                sel = (g.w[i >> 2] >> (2 * (i & 3))) & 0x03030303u;
-            } else {
-                if (j < 3) sel = (h == 0 ? g.w[j] : g.w[j] >> 3) & 0x07070707u;
-                else if (h == 0) sel = ((g.w[0] >> 6) & 0x03030303u) | ((g.w[1] >> 4) & 0x04040404u);
-                else sel = ((g.w[1] >> 7) & 0x01010101u) | ((g.w[2] >> 5) & 0x06060606u);
-            }
-            const uint32_t lo = __builtin_amdgcn_perm(c.b, c.a, sel), hi = __builtin_amdgcn_perm(c.d, c.c, sel);
-            a[2 * h] = __builtin_amdgcn_perm(hi, lo, 0x05010400u);
-            a[2 * h + 1] = __builtin_amdgcn_perm(hi, lo, 0x07030602u);
+        for (int k = 0; k < EACH; ++k) {
+            const uint32_t d = lane + k * LANES;
+            if (k * LANES >= 16 * words) break;
+            const uint32_t row = min(d * inverse >> 16, 15u), at = min(d - row * words, static_cast<uint32_t>(words - 1));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) raw[i][k] = m[i].scales[row * row_words + first + at];
         }
-        return a;
-    } else {
-        const uint32_t even = (g.w[j] & 0x0F0F0F0Fu) | l.which, odd = ((g.w[j] >> 4) & 0x0F0F0F0Fu) | l.which;
-        uint32_t v[8];
+    }
+    __device__ __forceinline__ void keep(PieceScales& to, int words, int lane) const {
+        const uint32_t inverse = 65536u / words + 1, odd = words | 1;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const uint32_t d = lane + k * LANES;
+            if (k * LANES >= 16 * words) break;
+            const uint32_t row = d * inverse >> 16;
+            if (row < 16) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) to[i][row * odd + d - row * words] = raw[i][k];
+            }
+        }
+    }
+};
+
+// The tables of two matrices' centroids: entries of 256 bytes, the first matrix's columns, then the second's; 1 bit: one after the other,
+// columns of eight bytes.
+template <int BITS> struct alignas(256) Tables {
+    static constexpr int ENTRIES = BITS == 1 ? 32 : 1 << (2 * BITS);
+    uint32_t word[ENTRIES][64];
+};
+// `centroids`: lane l < 16 holds the first matrix's l-th, lane 16 + l the second's.  Filled by all waves of a workgroup, 1 KB a write.
+template <int BITS>
+__device__ __forceinline__ void fill_tables(Tables<BITS>& tables, uint32_t centroids, int wave, int waves, int lane) {
+    const auto centroid = [&](int matrix, int index) { return static_cast<uint32_t>(__shfl(static_cast<int>(centroids), matrix * 16 + index)); };
+    for (int i = wave; i < Tables<BITS>::ENTRIES / 4; i += waves) {
+        const int e = 4 * i + (lane >> 4);
+        u32x4_t v;
+        if constexpr (BITS == 1) {
+            const uint32_t c0 = centroid(i >> 2, 0), c1 = centroid(i >> 2, 1);
+            v[0] = v[2] = (e & 1 ? c1 : c0) | (e & 2 ? c1 : c0) << 16;
+            v[1] = v[3] = (e & 4 ? c1 : c0) | (e & 8 ? c1 : c0) << 16;
+        } else {
+            const int matrix = (lane >> 3) & 1;
+            v[0] = v[1] = v[2] = v[3] = centroid(matrix, e & ((1 << BITS) - 1)) | centroid(matrix, e >> BITS) << 16;
+        }
+        *reinterpret_cast<u32x4_t*>(&tables.word[e][4 * (lane & 15)]) = v;
+    }
+}
+
+// Look-up addresses: byte 0 is the lane's column, byte 1 the entry.
+template <int BITS>
+struct LookUp {
+    static constexpr int EACH = BITS == 1 ? 2 : 4;
+    uint32_t at[2][EACH];
+    uint32_t table;
+    __device__ __forceinline__ LookUp(const Tables<BITS>& t, int lane) {
+        table = static_cast<uint32_t>(reinterpret_cast<size_t>((clds_cu32_t*)(&t.word[0][0])));
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) at[m][i] = BITS == 1 ? (lane & 31) * 8u : m * 128u + (lane & 31) * 4u;
+    }
+};
+typedef __attribute__((address_space(3))) const u32x2_t lds_u32x2_t;
+
+// Eight weights of step j of one granule.
+template <int BITS>
+__device__ __forceinline__ u32x4_t decode(const Granule<BITS>& g, LookUp<BITS>& l, int m, int j) {
+    u32x4_t v;
+    if constexpr (BITS == 1) {
+        const uint32_t even = g.w[j >> 2], odd = even >> 4, base = l.table + m * 4096u;
         const auto look = [&](auto bc) {
             constexpr int b = decltype(bc)::value;
-            canon_index_to_byte1<b>(l.at[2 * b], even, 0xFFu);
-            v[2 * b] = *reinterpret_cast<clds_cu32_t*>(static_cast<size_t>(l.at[2 * b] + table));
-            canon_index_to_byte1<b>(l.at[2 * b + 1], odd, 0xFFu);
-            v[2 * b + 1] = *reinterpret_cast<clds_cu32_t*>(static_cast<size_t>(l.at[2 * b + 1] + table));
+            canon_index_to_byte1<b>(l.at[m][0], even, 0x0Fu);
+            canon_index_to_byte1<b>(l.at[m][1], odd, 0x0Fu);
+        };
+        switch (j & 3) {
+            case 0: look(std::integral_constant<int, 0>{}); break;
+            case 1: look(std::integral_constant<int, 1>{}); break;
+            case 2: look(std::integral_constant<int, 2>{}); break;
+            default: look(std::integral_constant<int, 3>{}); break;
+        }
+        const u32x2_t lo = *reinterpret_cast<lds_u32x2_t*>(static_cast<size_t>(l.at[m][0] + base)), hi = *reinterpret_cast<lds_u32x2_t*>(static_cast<size_t>(l.at[m][1] + base));
+        v = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+    } else {
+        uint32_t x;
+        if constexpr (BITS == 4) x = g.w[j];
+        else if constexpr (BITS == 2) x = g.w[j >> 1] >> (4 * (j & 1));
+        else x = j < 3 ? g.w[j] : ((g.w[0] >> 6) & 0x03030303u) | ((g.w[1] >> 4) & 0x0C0C0C0Cu) | ((g.w[2] >> 2) & 0x30303030u);
+        const auto look = [&](auto bc) {
+            constexpr int b = decltype(bc)::value;
+            canon_index_to_byte1<b>(l.at[m][b], x, (1u << (2 * BITS)) - 1u);
+            v[b] = *reinterpret_cast<clds_cu32_t*>(static_cast<size_t>(l.at[m][b] + l.table));
         };
         look(std::integral_constant<int, 0>{});
         look(std::integral_constant<int, 1>{});
         look(std::integral_constant<int, 2>{});
         look(std::integral_constant<int, 3>{});
-        return u32x4_t{__builtin_amdgcn_perm(v[1], v[0], 0x07060100u), __builtin_amdgcn_perm(v[3], v[2], 0x07060100u),
-                       __builtin_amdgcn_perm(v[5], v[4], 0x07060100u), __builtin_amdgcn_perm(v[7], v[6], 0x07060100u)};
     }
+    return v;
 }
 
 __device__ __forceinline__ f32x4_t step(u32x4_t tokens, u32x4_t weights, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, tokens), __builtin_bit_cast(bf16x8_t, weights), c, 0, 0, 0);
 }
 
-// Which experts were chosen: a bit each, in shared memory; the pairs' ids as they are, their experts (-1: none, or an earlier pair of the
-// token has the same) and, where they are asked for, their weights: of all the token's pairs with that expert.
-template <int ROWS, bool WEIGHTS>
+// Which experts were chosen: a bit each, in shared memory, and the pairs' experts (-1: none, or an earlier pair of the token has the same).
+template <int ROWS>
 struct Choices {
     static constexpr int PAIRS = ROWS * KMQ_MOE_MAX_TOP_K;
     uint32_t has[KMQ_MOE_MAX_EXPERTS / 32];
-    int16_t id[PAIRS + KMQ_MOE_MAX_TOP_K], expert[PAIRS];
-    float gate[WEIGHTS ? PAIRS + KMQ_MOE_MAX_TOP_K : 1], weight[WEIGHTS ? PAIRS : 1];
+    int16_t expert[PAIRS + KMQ_MOE_MAX_TOP_K];
 };
 // What a lane knows of them: its 32 experts' bits, and how many experts were chosen up to them.
 struct Chosen {
@@ -190,32 +213,38 @@ struct Chosen {
         return __builtin_amdgcn_readfirstlane(word * 32 + __ffs(bits) - 1);
     }
 };
-template <int ROWS, bool WEIGHTS>
-__device__ __forceinline__ Chosen find_choices(const MoeArgs& a, Choices<ROWS, WEIGHTS>& p) {
+template <int ROWS, int THREADS>
+__device__ __forceinline__ Chosen find_choices(const MoeArgs& a, Choices<ROWS>& p) {
     static_assert(KMQ_MOE_MAX_EXPERTS / 32 <= kWave, "a word a lane");
+    constexpr int EACH = (Choices<ROWS>::PAIRS + THREADS - 1) / THREADS;
     const int pairs = a.rows * a.top_k, tid = threadIdx.x, lane = tid & 63;
-    for (int i = tid; i < pairs; i += blockDim.x) {
-        const int e = a.ids[i];
-        p.id[i] = static_cast<int16_t>(e >= 0 && e < a.experts ? e : -1);
-        if constexpr (WEIGHTS) p.gate[i] = a.gates[i];
+    int e[EACH];
+#pragma unroll
+    for (int t = 0; t < EACH; ++t) {
+        const int i = tid + t * THREADS;
+        e[t] = i < pairs ? a.ids[i] : -1;
+        if (e[t] < 0 || e[t] >= a.experts) e[t] = -1;
+        if (i < pairs) p.expert[i] = static_cast<int16_t>(e[t]);
     }
     if (tid < KMQ_MOE_MAX_EXPERTS / 32) p.has[tid] = 0;
     __syncthreads();
-    for (int i = tid; i < pairs; i += blockDim.x) {
-        const int e = p.id[i], slot = i % a.top_k, first = i - slot;
-        bool counts = e >= 0;
-        [[maybe_unused]] float w = 0.f;
 #pragma unroll
-        for (int j = 0; j < KMQ_MOE_MAX_TOP_K; ++j) {     // (behind the last pair there is room for reading on)
-            const bool same = j < a.top_k && p.id[first + j] == e;
-            counts = counts && !(same && j < slot);
-            if constexpr (WEIGHTS) w += same ? p.gate[first + j] : 0.f;
-        }
-        p.expert[i] = static_cast<int16_t>(counts ? e : -1);
-        if constexpr (WEIGHTS) p.weight[i] = w;
-        if (counts) atomicOr(&p.has[e >> 5], 1u << (e & 31));
+    for (int t = 0; t < EACH; ++t) {
+        const int i = tid + t * THREADS;
+        if (i >= pairs) continue;
+        const int slot = i % a.top_k;
+        bool again = false;
+#pragma unroll
+        for (int j = 0; j < KMQ_MOE_MAX_TOP_K - 1; ++j) again |= (j < slot) & (p.expert[i - slot + j] == e[t]);      // (there is room behind the last pair)
+        if (again) e[t] = -1;
+        if (e[t] >= 0) atomicOr(&p.has[e[t] >> 5], 1u << (e[t] & 31));
     }
     __syncthreads();
+#pragma unroll
+    for (int t = 0; t < EACH; ++t) {
+        const int i = tid + t * THREADS;
+        if (i < pairs) p.expert[i] = static_cast<int16_t>(e[t]);
+    }
     Chosen c;
     c.mine = lane < KMQ_MOE_MAX_EXPERTS / 32 ? p.has[lane] : 0u;
     c.upto = __popc(c.mine);
@@ -224,30 +253,27 @@ __device__ __forceinline__ Chosen find_choices(const MoeArgs& a, Choices<ROWS, W
         if (lane >= d) c.upto += o;
     }
     c.all = __builtin_amdgcn_readlane(c.upto, KMQ_MOE_MAX_EXPERTS / 32 - 1);
+    __syncthreads();
     return c;
 }
 
-// The pairs of an expert, into `list` (this wave's own): token << 16 | pair.  How many.
-template <int ROWS, bool WEIGHTS>
-__device__ __forceinline__ int pairs_of(const Choices<ROWS, WEIGHTS>& p, int pairs, int top_k, int expert, uint32_t* list) {
+// The pairs of an expert, in their order: lane l gets the (first + l)-th.  `count`: how many there are in all.
+template <int ROWS>
+__device__ __forceinline__ int pairs_of(const Choices<ROWS>& p, int pairs, int expert, int first, int& count) {
     const int lane = threadIdx.x & 63;
-    int count = 0;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    int mine = 0;
+    count = 0;
     for (int i = lane; i < (pairs + 63) / 64 * 64; i += 64) {
-        const bool mine = i < pairs && p.expert[i] == expert;
-        const uint64_t all = __ballot(mine);
-        if (mine) list[count + __popcll(all & ((uint64_t(1) << lane) - 1))] = static_cast<uint32_t>(i / top_k) << 16 | static_cast<uint32_t>(i);
+        const bool has = i < pairs && p.expert[i] == expert;
+        const uint64_t all = __ballot(has);
+        const int to = count + __popcll(all & ((uint64_t(1) << lane) - 1)) - first;
+        // what is sent to a lane is one more than the pair: 0 comes where nothing is sent (lane 63 takes what nobody asks for: 32 are looked at)
+        const int got = __builtin_amdgcn_ds_permute((has && to >= 0 && to < 32 ? to : 63) * 4, has ? i + 1 : 0);
+        if (lane < 32 && got) mine = got - 1;
         count += __popcll(all);
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    return __builtin_amdgcn_readfirstlane(count);
-}
-
-__device__ __forceinline__ void fill_masks(u32x2_t (&masks)[16]) {
-    if (threadIdx.x < 16) {
-        const uint32_t e = threadIdx.x;
-        masks[e] = u32x2_t{((e & 1u) ? 0xFFFFu : 0u) | ((e & 2u) ? 0xFFFF0000u : 0u), ((e & 4u) ? 0xFFFFu : 0u) | ((e & 8u) ? 0xFFFF0000u : 0u)};
-    }
+    count = __builtin_amdgcn_readfirstlane(count);
+    return mine;
 }
 
 // What a wave asks for at a time: a super-block of N matrices, and the elements under it of T tokens of the expert.  Fewer than 16 tokens
@@ -258,7 +284,7 @@ template <int BITS, int T, int N>
 struct Bundle {
     static constexpr int TILES = T > 16 ? T / 16 : 1, LOADS = T > 16 ? 4 : T / 4;      // column tiles; loads a tile and four steps
     static constexpr bool TOKENS = BITS > 1 || T < 16;
-    static constexpr int WORDS = N * (Granule<BITS>::WORDS + Granule<BITS>::BLOCKS / 2) + (TOKENS ? TILES * LOADS * Granule<BITS>::STEPS : 0);
+    static constexpr int WORDS = N * Granule<BITS>::WORDS + (TOKENS ? TILES * LOADS * Granule<BITS>::STEPS : 0);
     Granule<BITS> g[N];
     u32x4_t x[TILES][TOKENS ? Granule<BITS>::STEPS / 4 : 1][LOADS];
 };
@@ -274,17 +300,22 @@ __device__ __forceinline__ void load_tokens(const Tokens<T>& tokens, int tile, u
     for (int l = 0; l < (T > 16 ? 4 : T / 4); ++l) x[l] = load_row16(tokens.rows, tokens.at[tile] + l * (T < 16 ? 1024 / T : 64), column * 2);
 }
 template <int BITS, int T, int N>
-__device__ __forceinline__ void load_bundle(const Matrix (&m)[N], int units, int unit, const Tokens<T>& tokens, int first_column, int lane, Bundle<BITS, T, N>& b) {
+__device__ __forceinline__ void load_bundle(const Matrix (&m)[N], int unit, const Tokens<T>& tokens, int lane, Bundle<BITS, T, N>& b) {
     using G = Granule<BITS>;
     using B = Bundle<BITS, T, N>;
 #pragma unroll
-    for (int i = 0; i < N; ++i) load_granule<BITS>(m[i], units, unit, lane, b.g[i]);
+    for (int i = 0; i < N; ++i) load_granule<BITS>(m[i], unit, lane, b.g[i]);
     if constexpr (B::TOKENS) {
 #pragma unroll
         for (int t = 0; t < B::TILES; ++t)
 #pragma unroll
-            for (int k = 0; k < G::STEPS / 4; ++k) load_tokens<T>(tokens, t, first_column + unit * G::COLUMNS + 128 * k, b.x[t][k]);
+            for (int k = 0; k < G::STEPS / 4; ++k) load_tokens<T>(tokens, t, unit * G::COLUMNS + 128 * k, b.x[t][k]);
     }
+}
+// Elements 0 .. 7 as (0, 4), (1, 5), (2, 6), (3, 7).
+__device__ __forceinline__ u32x4_t pairs_apart(u32x4_t x) {
+    return u32x4_t{__builtin_amdgcn_perm(x[2], x[0], 0x05040100u), __builtin_amdgcn_perm(x[2], x[0], 0x07060302u),
+                   __builtin_amdgcn_perm(x[3], x[1], 0x05040100u), __builtin_amdgcn_perm(x[3], x[1], 0x07060302u)};
 }
 // The operand of step j of four.
 template <int T>
@@ -305,8 +336,8 @@ __device__ __forceinline__ u32x4_t operand(const u32x4_t (&x)[T > 16 ? 4 : T / 4
     }
 }
 template <int BITS, int T, int N>
-__device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T, N>& b, const Centroids<BITS> (&c)[N], LookUp& l, uint32_t tables, const u32x2_t* masks,
-                                                const Tokens<T>& tokens, int column, f32x4_t (&acc)[N][Tokens<T>::TILES]) {
+__device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T, N>& b, LookUp<BITS>& l, const uint32_t* scales, const Tokens<T>& tokens, int unit,
+                                                f32x4_t (&acc)[N][Tokens<T>::TILES]) {
     using G = Granule<BITS>;
     using B = Bundle<BITS, T, N>;
 #pragma unroll
@@ -318,9 +349,16 @@ __device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T, N>& b, con
 #pragma unroll
                 for (int i = 0; i < B::LOADS; ++i) x[t][i] = b.x[t][k][i];
             } else {
-                load_tokens<T>(tokens, t, column + 128 * k, x[t]);
+                load_tokens<T>(tokens, t, unit * G::COLUMNS + 128 * k, x[t]);
+            }
+            if constexpr (BITS == 2 || BITS == 3) {
+#pragma unroll
+                for (int i = 0; i < B::LOADS; ++i) x[t][i] = pairs_apart(x[t][i]);
             }
         }
+        uint32_t both[N];                                 // the scales of two blocks
+#pragma unroll
+        for (int i = 0; i < N; ++i) both[i] = scales[i * sizeof(PieceScales) / 8 + k];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int block = 2 * k + half;
@@ -332,8 +370,8 @@ __device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T, N>& b, con
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const u32x4_t w0 = decode<BITS>(b.g[i], c[i], l, tables + i * sizeof(Table), masks, 2 * block), w1 = decode<BITS>(b.g[i], c[i], l, tables + i * sizeof(Table), masks, 2 * block + 1);
-                const float s = kv_half(b.g[i].scale[block / 2], block % 2);
+                const u32x4_t w0 = decode<BITS>(b.g[i], l, i, 2 * block), w1 = decode<BITS>(b.g[i], l, i, 2 * block + 1);
+                const float s = kv_half(both[i], half);
 #pragma unroll
                 for (int t = 0; t < B::TILES; ++t) {
                     f32x4_t d = step(x0[t], w0, f32x4_t{0.f, 0.f, 0.f, 0.f});
@@ -343,285 +381,249 @@ __device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T, N>& b, con
                 }
             }
         }
-        if constexpr (!B::TOKENS) __builtin_amdgcn_sched_barrier(0);      // (else the elements of all steps are asked for at once, and spilled)
+        __builtin_amdgcn_sched_barrier(0);                // (else what later steps need is looked up and turned early, and spilled)
     }
 }
-// The sums over `count` super-blocks; the first D bundles have been asked for.  The loop's loads are unconditional, the last
-// super-blocks a copy of the code of their own: a branch around a load would make every wait assume the fewest of them.
+// The sums over super-blocks u .. end - 1; the first D bundles have been asked for.  `scales`: the lane's row from super-block 0 on.  The
+// loop's loads are unconditional, the last super-blocks a copy of the code of their own: a branch around a load would make every wait
+// assume the fewest of them.
 template <int BITS, int T, int N, int D>
-__device__ __forceinline__ void run_units(Bundle<BITS, T, N> (&b)[D], const Matrix (&m)[N], int units, int count, const Centroids<BITS> (&c)[N], LookUp& l, uint32_t tables,
-                                          const u32x2_t* masks, const Tokens<T>& tokens, int first_column, int lane, f32x4_t (&acc)[N][Tokens<T>::TILES]) {
-    constexpr int COLUMNS = Granule<BITS>::COLUMNS;
-    int u = 0;
-    const auto multiply_at = [&](int slot, int unit) { multiply_bundle<BITS, T, N>(b[slot], c, l, tables, masks, tokens, first_column + unit * COLUMNS, acc); };
-    for (; u + 2 * D <= count; u += D) {
+__device__ __forceinline__ void run_units(Bundle<BITS, T, N> (&b)[D], const Matrix (&m)[N], int u, int end, LookUp<BITS>& l, const uint32_t* scales,
+                                          const Tokens<T>& tokens, int lane, f32x4_t (&acc)[N][Tokens<T>::TILES]) {
+    const auto multiply_at = [&](int slot, int unit) { multiply_bundle<BITS, T, N>(b[slot], l, scales + unit * (Granule<BITS>::BLOCKS / 2), tokens, unit, acc); };
+    for (; u + 2 * D <= end; u += D) {
 #pragma unroll
         for (int p = 0; p < D; ++p) {
             multiply_at(p, u + p);
-            load_bundle<BITS, T, N>(m, units, u + p + D, tokens, first_column, lane, b[p]);
+            load_bundle<BITS, T, N>(m, u + p + D, tokens, lane, b[p]);
         }
     }
 #pragma unroll
     for (int p = 0; p < D; ++p) {
-        if (u + p >= count) return;
+        if (u + p >= end) return;
         multiply_at(p, u + p);
-        if (u + p + D < count) load_bundle<BITS, T, N>(m, units, u + p + D, tokens, first_column, lane, b[p]);
+        if (u + p + D < end) load_bundle<BITS, T, N>(m, u + p + D, tokens, lane, b[p]);
     }
 #pragma unroll
     for (int p = 0; p < D - 1; ++p) {
-        if (u + D + p >= count) return;
+        if (u + D + p >= end) return;
         multiply_at(p, u + D + p);
     }
 }
-template <int BITS, int T, int N, int D>
-__device__ __forceinline__ void first_bundles(Bundle<BITS, T, N> (&b)[D], const Matrix (&m)[N], int units, int count, const Tokens<T>& tokens, int first_column, int lane) {
-#pragma unroll
-    for (int p = 0; p < D; ++p)
-        if (p < count) load_bundle<BITS, T, N>(m, units, p, tokens, first_column, lane, b[p]);
-}
-// Where the lane's tokens begin, of those from `first` on in the list: rows of `stride` bytes; PAIR: a row a pair, else a row a token.
-template <int T, bool PAIR>
-__device__ __forceinline__ void find_tokens(Tokens<T>& tokens, const uint32_t* list, int first, int count, uint32_t stride, int lane) {
-    const int n = lane & 15, q = lane >> 4;
-#pragma unroll
-    for (int t = 0; t < Tokens<T>::TILES; ++t) {
-        const int i = first + 16 * t + (T < 16 ? n % T : n);
-        tokens.at[t] = kNoRow;
-        if (i < count) tokens.at[t] = (PAIR ? list[i] & 0xFFFFu : list[i] >> 16) * stride + 16u * q + (T < 16 ? n / T * 64u : 0u);
-    }
-}
-__device__ __forceinline__ uint32_t shared_offset(const void* p) { return static_cast<uint32_t>(reinterpret_cast<size_t>((clds_cu32_t*)(p))); }
-__device__ __forceinline__ LookUp look_up(uint32_t which, int lane) {
-    LookUp l;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) l.at[e] = static_cast<uint32_t>(lane) * 4u;
-    l.which = which * 0x10101010u;
-    return l;
+// A value that the compiler does not know to be the same in every round of a loop: what is worked out from it is worked out there again,
+// where kept for later it would take a register for as long.
+__device__ __forceinline__ int anew(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
 }
 
-template <int BITS, int T, int ROWS, int NW>
-__global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(gate_up_waves(BITS, T)))) void moe_gate_up_kernel(MoeArgs a) {
+// A workgroup of TEAMS teams of NW waves; T tokens at a time.  GATED: rows of gate and up, else pairs of row blocks of down.
+template <int BITS, int T, int ROWS, int NW, int TEAMS, bool GATED>
+__global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per_eu(waves_for(BITS, T)))) void moe_rows_kernel(MoeArgs a) {
     using G = Granule<BITS>;
-    constexpr int TILES = Tokens<T>::TILES, D = depth(Bundle<BITS, T, 2>::WORDS);
-    struct alignas(256) Smem {
-        Table tables[BITS == 4 ? 2 : 1];
-        Choices<ROWS, false> choices;
-        float part[2][NW][2][16][17];
-        uint32_t lists[NW][2][ROWS];
-        u32x2_t masks[16];
+    constexpr int TILES = Tokens<T>::TILES, D = depth(Bundle<BITS, T, 2>::WORDS), LANES = T < 16 ? 4 * T : 64;
+    struct Smem {
+        Tables<BITS> tables;
+        f32x4_t part[TEAMS][NW - 1][2][LANES];            // sums of a team's waves but the first
+        PieceScales scales[TEAMS];
+        Choices<ROWS> choices;
     };
     __shared__ Smem sm;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-    if constexpr (BITS == 1) fill_masks(sm.masks);
-    const Chosen chosen = find_choices(a, sm.choices);
-    const int blocks = static_cast<int>(a.width >> 4), units = static_cast<int>(a.hidden / G::COLUMNS), pairs = a.rows * a.top_k;
-    const int u0 = units * wave / NW, mine = units * (wave + 1) / NW - u0, column = u0 * G::COLUMNS;
-    const int64_t items = static_cast<int64_t>(chosen.all) * blocks;
-    const int from = static_cast<int>(items * blockIdx.x / gridDim.x), to = static_cast<int>(items * (blockIdx.x + 1) / gridDim.x);
+    const int team = wave / NW, member = wave % NW, place = member * kWave + lane;
+    const Chosen chosen = find_choices<ROWS, NW * TEAMS * kWave>(a, sm.choices);
+    const int columns = static_cast<int>(GATED ? a.hidden : a.width), units = columns / G::COLUMNS, pairs = a.rows * a.top_k;
+    const int per_expert = static_cast<int>(GATED ? a.width >> 4 : a.hidden >> 5) / TEAMS;
+    const unsigned items = static_cast<unsigned>(chosen.all) * per_expert, each = items / gridDim.x, over = items - each * gridDim.x;
+    const int from = static_cast<int>(each * blockIdx.x + min(blockIdx.x, over)), to = from + static_cast<int>(each + (blockIdx.x < over));
     if (from >= to) return;
     uint16_t* const h = static_cast<uint16_t*>(a.workspace);
+    float* const out = reinterpret_cast<float*>(h + static_cast<int64_t>(pairs) * a.width);
+    const uint32_t stride = static_cast<uint32_t>(GATED ? a.x_stride : a.width) * 2u;
     Tokens<T> tokens;
-    tokens.rows = rows_at(a.x);
+    tokens.rows = rows_at(GATED ? static_cast<const void*>(a.x) : h);
     Bundle<BITS, T, 2> b[D];
+    Scales<NW * kWave> scales;
     Matrix m[2];
-    Centroids<BITS> c[2] = {};
-    LookUp l = look_up(0, lane);
-    const uint32_t tables = shared_offset(&sm.tables[0]);
-    // where the wave is: rows `block` of the `which`-th expert, its pairs first ..
-    int which = from / blocks, block = from - which * blocks, e = chosen.expert(which), turn = 0;
-    uint32_t* list = sm.lists[wave][0];
-    int count = pairs_of(sm.choices, pairs, a.top_k, e, list), first = 0;
-    const auto ask = [&] {
-        m[0] = matrix_of<BITS>(a.gate, e, block, units, u0);
-        m[1] = matrix_of<BITS>(a.up, e, block, units, u0);
-        find_tokens<T, false>(tokens, list, first, count, static_cast<uint32_t>(a.x_stride * 2), lane);
-        first_bundles<BITS, T, 2, D>(b, m, units, mine, tokens, column, lane);
+    LookUp<BITS> l(sm.tables, lane);
+    // where the workgroup is: the `group`-th row blocks of the `which`-th expert e, its pairs from `first` on, a piece of the columns, of
+    // which super-blocks u .. end - 1 are this wave's; this lane's pair
+    int which = from / per_expert, group = from - which * per_expert, e = chosen.expert(which), first = 0, piece = 0, u, end, words, count, pair;
+    uint32_t centroids = 0;
+    const auto ask_piece = [&] {
+        constexpr int MOST = kPiece / G::COLUMNS;
+        const int start = piece * MOST, some = units - start < MOST ? units - start : MOST;
+        words = some * (G::BLOCKS / 2);
+        u = start + some * member / NW;
+        end = start + some * (member + 1) / NW;
+        scales.load(m, columns / 128, piece * kPieceWords, words, anew(place));
+#pragma unroll
+        for (int p = 0; p < D; ++p)
+            if (u + p < end) load_bundle<BITS, T, 2>(m, u + p, tokens, lane, b[p]);
     };
-    const auto look_at = [&] {                            // an expert's centroids
-        const uint16_t *bg = a.gate.books + (e << BITS), *bu = a.up.books + (e << BITS);
-        c[0] = centroids_of<BITS>(bg);
-        c[1] = centroids_of<BITS>(bu);
-        if constexpr (BITS == 4) {
-            fill_table(sm.tables[0], bg, wave, NW, lane);
-            fill_table(sm.tables[1], bu, wave, NW, lane);
-            __syncthreads();
+    const auto ask = [&](bool other, bool tokens_too) {
+        if (other) {                                      // (before the bundles: what is waited for first is asked for first)
+            const uint16_t* book = (!GATED ? a.down.books : lane & 16 ? a.up.books : a.gate.books) + (e << BITS);
+            centroids = book[anew(lane) & ((1 << BITS) - 1)];
         }
+        const int block = group * TEAMS + team;
+        m[0] = matrix_of<BITS>(GATED ? a.gate : a.down, e, GATED ? block : 2 * block, units);
+        m[1] = matrix_of<BITS>(GATED ? a.up : a.down, e, GATED ? block : 2 * block + 1, units);
+        if (tokens_too) {
+            const int lane = anew(static_cast<int>(threadIdx.x)) & 63, n = lane & 15, q = lane >> 4;
+            pair = pairs_of(sm.choices, pairs, e, first, count);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                const int i = 16 * t + (T < 16 ? n % T : n), p = __shfl(pair, i);
+                tokens.at[t] = kNoRow;
+                if (first + i < count) tokens.at[t] = static_cast<uint32_t>(GATED ? p / a.top_k : p) * stride + 16u * q + (T < 16 ? n / T * 64u : 0u);
+            }
+        }
+        piece = 0;
+        ask_piece();
     };
-    ask();
-    look_at();
+    ask(true, true);
+    scales.keep(sm.scales[team], words, anew(place));
+    fill_tables<BITS>(sm.tables, centroids, wave, NW * TEAMS, anew(lane));
+    __syncthreads();
     for (int item = from;;) {
         f32x4_t acc[2][TILES];
 #pragma unroll
         for (int t = 0; t < TILES; ++t) acc[0][t] = acc[1][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        run_units<BITS, T, 2, D>(b, m, units, mine, c, l, tables, sm.masks, tokens, column, lane, acc);
+        for (;;) {
+            run_units<BITS, T, 2, D>(b, m, u, end, l, &sm.scales[team][0][n * (words | 1) - piece * kPieceWords], tokens, lane, acc);
+            if ((piece + 1) * kPiece >= columns) break;
+            ++piece;
+            ask_piece();
+            __syncthreads();
+            scales.keep(sm.scales[team], words, anew(place));
+            __syncthreads();
+        }
         // what comes next is asked for before the sums are joined
-        const int left = count - first < T ? count - first : T, done = first, row = block * 16, last = e;
-        const uint32_t* const now = list;
-        bool more = true;
+        const int left = count - first < T ? count - first : T, block = group * TEAMS + team, now = pair;
+        bool more = true, other = false, whole = count <= T;
         if (first + T < count) {
             first += T;
         } else {
             first = 0;
             if (++item == to) more = false;
-            else if (++block == blocks) {
-                block = 0;
+            else if (++group == per_expert) {
+                group = 0;
                 e = chosen.expert(++which);
-                list = sm.lists[wave][which & 1];
-                if (list == now) list = sm.lists[wave][(which & 1) ^ 1];
-                count = pairs_of(sm.choices, pairs, a.top_k, e, list);
+                other = true;
             }
         }
-        if (more) ask();
+        if (more) ask(other, other || !whole);
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
             if (16 * t >= left) break;
-            float (&part)[NW][2][16][17] = sm.part[turn];
-            turn ^= 1;
-            if (16 * t + 4 * q < left) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    part[wave][0][4 * q + i][n] = acc[0][t][i];
-                    part[wave][1][4 * q + i][n] = acc[1][t][i];
-                }
+            if (t) __syncthreads();
+            const int lane = anew(static_cast<int>(threadIdx.x)) & 63, n = lane & 15, q = lane >> 4;
+            if (member > 0 && lane < LANES) {
+                sm.part[team][member - 1][0][lane] = acc[0][t];
+                sm.part[team][member - 1][1][lane] = acc[1][t];
             }
             __syncthreads();
-            const int column = threadIdx.x >> 4, r = threadIdx.x & 15;
-            if (column < 16 && 16 * t + column < left) {
-                float g = part[0][0][column][r], u = part[0][1][column][r];
+            if (member == 0) {
+                if (lane < LANES) {
 #pragma unroll
-                for (int w = 1; w < NW; ++w) {
-                    g += part[w][0][column][r];
-                    u += part[w][1][column][r];
+                    for (int w = 0; w < NW - 1; ++w) {
+                        acc[0][t] += sm.part[team][w][0][lane];
+                        acc[1][t] += sm.part[team][w][1][lane];
+                    }
                 }
-                h[(now[done + 16 * t + column] & 0xFFFFu) * a.width + row + r] = f32_to_bf16(g / (1.f + expf(-g)) * u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = 16 * t + 4 * q + i;
+                    const int64_t p = __shfl(now, at & 31);
+                    if (at >= left) continue;
+                    if constexpr (GATED) {
+                        const float g = acc[0][t][i], v = acc[1][t][i];
+                        h[p * a.width + block * 16 + n] = f32_to_bf16(g / (1.f + expf(-g)) * v);
+                    } else {
+                        out[p * a.hidden + block * 32 + n] = acc[0][t][i];
+                        out[p * a.hidden + block * 32 + 16 + n] = acc[1][t][i];
+                    }
+                }
             }
         }
         if (!more) break;
-        if (e != last) look_at();
+        scales.keep(sm.scales[team], words, anew(place));       // (every wave has been past a barrier since it read the last ones)
+        if (other) fill_tables<BITS>(sm.tables, centroids, wave, NW * TEAMS, anew(lane));
+        __syncthreads();
     }
 }
 
-template <int BITS, int T, int ROWS, int NW>
-__global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(down_waves(BITS, T)))) void moe_down_kernel(MoeArgs a) {
-    using G = Granule<BITS>;
-    constexpr int TILES = Tokens<T>::TILES, D = depth(Bundle<BITS, T, 1>::WORDS);
-    struct alignas(256) Smem {
-        Table tables[BITS == 4 ? NW : 1];
-        Choices<ROWS, true> choices;
-        uint32_t lists[NW][2][ROWS];
-        u32x2_t masks[16];
-    };
-    __shared__ Smem sm;
-    extern __shared__ float sums[];                       // [wave][token][16 rows]
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-    if constexpr (BITS == 1) fill_masks(sm.masks);
-    for (int i = threadIdx.x; i < NW * a.rows * 16; i += NW * kWave) sums[i] = 0.f;
-    const Chosen chosen = find_choices(a, sm.choices);
-    const int block = blockIdx.x, units = static_cast<int>(a.width / G::COLUMNS), pairs = a.rows * a.top_k;
-    const int64_t all = static_cast<int64_t>(chosen.all) * units;
-    const int from = static_cast<int>(all * wave / NW), to = static_cast<int>(all * (wave + 1) / NW);
-    float* const mine = sums + wave * a.rows * 16;
-    if (from < to) {
-        Tokens<T> tokens;
-        tokens.rows = rows_at(a.workspace);
-        Bundle<BITS, T, 1> b[D];
-        Matrix m[1];
-        Centroids<BITS> c[1];
-        LookUp l = look_up(wave, lane);
-        const uint32_t tables = shared_offset(&sm.tables[0]);
-        int which = from / units, u0 = from - which * units, some = units < u0 + to - from ? units - u0 : to - from, done = from + some;
-        int e = chosen.expert(which), first = 0;
-        uint32_t* list = sm.lists[wave][0];
-        int count = pairs_of(sm.choices, pairs, a.top_k, e, list);
-        const auto ask = [&] {
-            m[0] = matrix_of<BITS>(a.down, e, block, units, u0);
-            find_tokens<T, true>(tokens, list, first, count, static_cast<uint32_t>(a.width * 2), lane);
-            first_bundles<BITS, T, 1, D>(b, m, units, some, tokens, u0 * G::COLUMNS, lane);
-        };
-        const auto look_at = [&] {
-            const uint16_t* book = a.down.books + (e << BITS);
-            c[0] = centroids_of<BITS>(book);
-            if constexpr (BITS == 4) {
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                fill_table(sm.tables[wave], book, 0, 1, lane);
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            }
-        };
-        ask();
-        look_at();
-        for (;;) {
-            f32x4_t acc[1][TILES];
-#pragma unroll
-            for (int t = 0; t < TILES; ++t) acc[0][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            run_units<BITS, T, 1, D>(b, m, units, some, c, l, tables, sm.masks, tokens, u0 * G::COLUMNS, lane, acc);
-            const int start = first, had = count < first + T ? count : first + T, last = e;
-            const uint32_t* const now = list;
-            bool more = true;
-            if (first + T < count) {
-                first += T;
-            } else {
-                first = 0;
-                if (done == to) more = false;
-                else {
-                    ++which;
-                    u0 = 0;
-                    some = units < to - done ? units : to - done;
-                    done += some;
-                    e = chosen.expert(which);
-                    list = now == sm.lists[wave][0] ? sm.lists[wave][1] : sm.lists[wave][0];
-                    count = pairs_of(sm.choices, pairs, a.top_k, e, list);
-                }
-            }
-            if (more) ask();
-#pragma unroll
-            for (int t = 0; t < TILES; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int at = start + 16 * t + 4 * q + i;
-                    if (at < had) {
-                        const uint32_t p = now[at];
-                        float* s = mine + (p >> 16) * 16 + n;
-                        *s = fmaf(sm.choices.weight[p & 0xFFFFu], acc[0][t][i], *s);
-                    }
-                }
-            if (!more) break;
-            if (e != last) look_at();
-        }
+// y = residual + the sum of a token's pairs, in their order.  A thread four elements.
+__global__ __launch_bounds__(256) void moe_join_kernel(MoeArgs a) {
+    const int token = blockIdx.y, column = (static_cast<int>(blockIdx.x) * 256 + static_cast<int>(threadIdx.x)) * 4;
+    if (column >= a.hidden) return;
+    const float* out = reinterpret_cast<const float*>(static_cast<const uint16_t*>(a.workspace) + static_cast<int64_t>(a.rows) * a.top_k * a.width);
+    const int32_t* ids = a.ids + token * a.top_k;
+    const float* gates = a.gates + token * a.top_k;
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+    if (a.residual) {
+        const u32x2_t r = *reinterpret_cast<const u32x2_t*>(a.residual + token * a.residual_stride + column);
+        s = f32x4_t{kv_half(r[0], 0), kv_half(r[0], 1), kv_half(r[1], 0), kv_half(r[1], 1)};
     }
-    __syncthreads();
-    for (int o = threadIdx.x; o < a.rows * 16; o += NW * kWave) {
-        const int64_t token = o >> 4, row = static_cast<int64_t>(block) * 16 + (o & 15);
-        float s = a.residual ? bf16_to_f32(a.residual[token * a.residual_stride + row]) : 0.f;
-        for (int w = 0; w < NW; ++w) s += sums[w * a.rows * 16 + o];
-        a.y[token * a.y_stride + row] = f32_to_bf16(s);
+    int id[KMQ_MOE_MAX_TOP_K];
+#pragma unroll
+    for (int j = 0; j < KMQ_MOE_MAX_TOP_K; ++j) id[j] = j < a.top_k ? ids[j] : -1;
+    f32x4_t v[KMQ_MOE_MAX_TOP_K];
+    float w[KMQ_MOE_MAX_TOP_K];
+#pragma unroll
+    for (int j = 0; j < KMQ_MOE_MAX_TOP_K; ++j) {
+        int from = j;                                     // the first of the token's pairs with this expert
+#pragma unroll
+        for (int i = j - 1; i >= 0; --i) from = id[i] == id[j] ? i : from;
+        const bool counts = id[j] >= 0 && id[j] < a.experts;
+        w[j] = counts ? gates[j] : 0.f;
+        v[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (counts) v[j] = *reinterpret_cast<const f32x4_t*>(out + (static_cast<int64_t>(token) * a.top_k + from) * a.hidden + column);
     }
+#pragma unroll
+    for (int j = 0; j < KMQ_MOE_MAX_TOP_K; ++j) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = fmaf(w[j], v[j][i], s[i]);
+    }
+    *reinterpret_cast<u32x2_t*>(a.y + token * a.y_stride + column) = u32x2_t{kv_pack2(s[0], s[1]), kv_pack2(s[2], s[3])};
 }
 
 }  // namespace
 
-size_t moe_workspace_bytes(int64_t rows, int64_t top_k, int64_t width) { return static_cast<size_t>(rows * top_k * width * 2); }
+size_t moe_workspace_bytes(int64_t rows, int64_t top_k, int64_t width, int64_t hidden) { return static_cast<size_t>(rows * top_k * (width * 2 + hidden * 4)); }
 
-#ifndef KMQ_NWG
-#define KMQ_NWG 4
-#define KMQ_GRID 1024
+#ifndef KMQ_NW
+#define KMQ_NW 4
+#define KMQ_TEAMS 1
+#define KMQ_GRID 4096
 #endif
-template <int BITS, int T, int ROWS, int NWD>
+template <int BITS, int T, int ROWS, int NW, int TEAMS>
 static void launch_moe_one(const MoeArgs& a, hipStream_t s) {
-    const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, most = (pairs < a.experts ? pairs : a.experts) * (a.width / 16);
-    moe_gate_up_kernel<BITS, T, ROWS, KMQ_NWG><<<dim3(static_cast<unsigned>(most < KMQ_GRID ? most : KMQ_GRID)), KMQ_NWG * kWave, 0, s>>>(a);
-    moe_down_kernel<BITS, T, ROWS, NWD><<<dim3(static_cast<unsigned>(a.hidden / 16)), NWD * kWave, NWD * a.rows * 16 * sizeof(float), s>>>(a);
+    constexpr int MOST = KMQ_GRID / (NW * TEAMS);
+    const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = pairs < a.experts ? pairs : a.experts;
+    const auto grid = [&](int64_t each) { return dim3(static_cast<unsigned>(experts * each < MOST ? experts * each : MOST)); };
+    moe_rows_kernel<BITS, T, ROWS, NW, TEAMS, true><<<grid(a.width / 16 / TEAMS), NW * TEAMS * kWave, 0, s>>>(a);
+    moe_rows_kernel<BITS, T, ROWS, NW, TEAMS, false><<<grid(a.hidden / 32 / TEAMS), NW * TEAMS * kWave, 0, s>>>(a);
+    moe_join_kernel<<<dim3(static_cast<unsigned>((a.hidden + 1023) / 1024), static_cast<unsigned>(a.rows)), 256, 0, s>>>(a);
 }
+#ifndef KMQ_MNW
+#define KMQ_MNW 4
+#define KMQ_MT4 4
+#define KMQ_MT 1
+#endif
 #ifndef KMQ_TM
-#define KMQ_TM 32
+#define KMQ_TM 16
 #endif
 template <int BITS>
 static void launch_moe_bits(const MoeArgs& a, hipStream_t s) {
+    constexpr int TEAMS = BITS == 4 ? 2 : KMQ_TEAMS;
     const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k;
     const bool thin = pairs <= 2 * static_cast<int64_t>(a.experts);       // about two tokens an expert
-    if (a.rows <= 4) launch_moe_one<BITS, 4, 16, 16>(a, s);
-    else if (a.rows <= 8 || (a.rows <= 16 && thin)) launch_moe_one<BITS, 8, 16, 16>(a, s);
-    else if (a.rows <= 16) launch_moe_one<BITS, 16, 16, 16>(a, s);
-    else launch_moe_one<BITS, KMQ_TM, KMQ_MOE_MAX_ROWS, 8>(a, s);
+    if (a.rows <= 4) launch_moe_one<BITS, 4, 16, KMQ_NW, TEAMS>(a, s);
+    else if (a.rows <= 8 || (a.rows <= 16 && thin)) launch_moe_one<BITS, 8, 16, KMQ_NW, TEAMS>(a, s);
+    else if (a.rows <= 16) launch_moe_one<BITS, 16, 16, KMQ_NW, TEAMS>(a, s);
+    else launch_moe_one<BITS, KMQ_TM, KMQ_MOE_MAX_ROWS, KMQ_MNW, BITS == 4 ? KMQ_MT4 : KMQ_MT>(a, s);
 }
 
 hipError_t launch_moe(const MoeArgs& a, hipStream_t s) {
