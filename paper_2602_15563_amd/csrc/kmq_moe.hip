@@ -29,12 +29,16 @@ namespace kmq {
 namespace {
 
 // Bundles a wave has asked for, by their registers.
+#ifndef KMQ_T2
+#define KMQ_T2 32
+#define KMQ_W2 2
+#endif
 #ifndef KMQ_RING
 #define KMQ_RING 30
 #endif
 constexpr int depth(int words) { return words * 4 <= KMQ_RING ? 4 : words * 3 <= KMQ_RING ? 3 : 2; }
 // Waves a SIMD that the registers have to leave room for: as many as an instance needs no spilling for.
-constexpr int waves_for(int bits, int t) { return bits == 1 || t > 16 || (bits == 2 && t >= 8) || (bits == 3 && t == 16) ? 3 : 4; }
+constexpr int waves_for(int bits, int t) { return bits == 2 && t == 16 ? KMQ_W2 : bits == 1 || t > 16 || (bits == 2 && t >= 8) || (bits == 3 && t == 16) ? 3 : 4; }
 
 typedef __amdgpu_buffer_rsrc_t Rows;
 // Rows read by byte offset; kNoRow gives zeros.
@@ -194,30 +198,33 @@ __device__ __forceinline__ f32x4_t step(u32x4_t tokens, u32x4_t weights, f32x4_t
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, tokens), __builtin_bit_cast(bf16x8_t, weights), c, 0, 0, 0);
 }
 
-// Which experts were chosen: a bit each, in shared memory, and the pairs' experts (-1: none, or an earlier pair of the token has the same).
-template <int ROWS>
+// What a workgroup finds out about the choices: the pairs' experts (-1: none, or an earlier pair of the token has the same), and the list of
+// what there is to do: T tokens at most of an expert, as often as its tokens need, experts ascending.
+template <int ROWS, int T>
 struct Choices {
     static constexpr int PAIRS = ROWS * KMQ_MOE_MAX_TOP_K;
-    uint32_t has[KMQ_MOE_MAX_EXPERTS / 32];
+    static constexpr int MOST = (PAIRS < KMQ_MOE_MAX_EXPERTS ? PAIRS : KMQ_MOE_MAX_EXPERTS) + PAIRS / T;
+    static_assert(ROWS / T < 64, "six bits");
     int16_t expert[PAIRS + KMQ_MOE_MAX_TOP_K];
+    uint16_t list[MOST];                                  // expert << 6 | how many times T tokens of it came before
+    int all;                                              // entries of the list
 };
-// What a lane knows of them: its 32 experts' bits, and how many experts were chosen up to them.
-struct Chosen {
-    uint32_t mine;
-    int upto, all;
-    // The a-th chosen expert.
-    __device__ __forceinline__ int expert(int a) const {
-        const int word = __ffsll(__ballot(upto > a)) - 1;
-        uint32_t bits = __builtin_amdgcn_readlane(mine, word);
-        for (int skip = a - (__builtin_amdgcn_readlane(upto, word) - __popc(bits)); skip > 0; --skip) bits &= bits - 1;
-        return __builtin_amdgcn_readfirstlane(word * 32 + __ffs(bits) - 1);
-    }
-};
-template <int ROWS, int THREADS>
-__device__ __forceinline__ Chosen find_choices(const MoeArgs& a, Choices<ROWS>& p) {
-    static_assert(KMQ_MOE_MAX_EXPERTS / 32 <= kWave, "a word a lane");
-    constexpr int EACH = (Choices<ROWS>::PAIRS + THREADS - 1) / THREADS;
-    const int pairs = a.rows * a.top_k, tid = threadIdx.x, lane = tid & 63;
+// The sum over this lane and those below it.
+__device__ __forceinline__ int sum_upto(int v) {
+    const auto add = [&](auto ctrl, auto rows) { v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, true); };
+    add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xF>{});      // row_shr 1, 2, 4, 8
+    add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xF>{});
+    add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xF>{});
+    add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xF>{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});      // row_bcast15 into rows 1 and 3
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});      // row_bcast31 into rows 2 and 3
+    return v;
+}
+// (`counts`: a word an expert, of memory that is not used yet.)
+template <int ROWS, int T, int THREADS>
+__device__ __forceinline__ void find_choices(const MoeArgs& a, Choices<ROWS, T>& p, int* counts) {
+    constexpr int EACH = (Choices<ROWS, T>::PAIRS + THREADS - 1) / THREADS;
+    const int pairs = a.rows * a.top_k, tid = threadIdx.x;
     int e[EACH];
 #pragma unroll
     for (int t = 0; t < EACH; ++t) {
@@ -226,7 +233,7 @@ __device__ __forceinline__ Chosen find_choices(const MoeArgs& a, Choices<ROWS>& 
         if (e[t] < 0 || e[t] >= a.experts) e[t] = -1;
         if (i < pairs) p.expert[i] = static_cast<int16_t>(e[t]);
     }
-    if (tid < KMQ_MOE_MAX_EXPERTS / 32) p.has[tid] = 0;
+    for (int i = tid; i < a.experts; i += THREADS) counts[i] = 0;
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < EACH; ++t) {
@@ -237,7 +244,7 @@ __device__ __forceinline__ Chosen find_choices(const MoeArgs& a, Choices<ROWS>& 
 #pragma unroll
         for (int j = 0; j < KMQ_MOE_MAX_TOP_K - 1; ++j) again |= (j < slot) & (p.expert[i - slot + j] == e[t]);      // (there is room behind the last pair)
         if (again) e[t] = -1;
-        if (e[t] >= 0) atomicOr(&p.has[e[t] >> 5], 1u << (e[t] & 31));
+        if (e[t] >= 0) atomicAdd(&counts[e[t]], 1);
     }
     __syncthreads();
 #pragma unroll
@@ -245,24 +252,30 @@ __device__ __forceinline__ Chosen find_choices(const MoeArgs& a, Choices<ROWS>& 
         const int i = tid + t * THREADS;
         if (i < pairs) p.expert[i] = static_cast<int16_t>(e[t]);
     }
-    Chosen c;
-    c.mine = lane < KMQ_MOE_MAX_EXPERTS / 32 ? p.has[lane] : 0u;
-    c.upto = __popc(c.mine);
-    for (int d = 1; d < KMQ_MOE_MAX_EXPERTS / 32; d *= 2) {
-        const int o = __shfl_up(c.upto, d);
-        if (lane >= d) c.upto += o;
+    if (tid < kWave) {                                    // experts lane * some .. lane * some + some - 1
+        const int some = (a.experts + kWave - 1) / kWave, first = tid * some, end = min(first + some, a.experts);
+        int times = 0;
+        for (int i = first; i < end; ++i) times += (counts[i] + T - 1) / T;
+        int at = sum_upto(times);
+        if (tid == kWave - 1) p.all = at;
+        at -= times;
+        for (int i = first; i < end; ++i)
+            for (int k = 0; k * T < counts[i]; ++k) p.list[at++] = static_cast<uint16_t>(i << 6 | k);
     }
-    c.all = __builtin_amdgcn_readlane(c.upto, KMQ_MOE_MAX_EXPERTS / 32 - 1);
     __syncthreads();
-    return c;
 }
 
-// The pairs of an expert, in their order: lane l gets the (first + l)-th.  `count`: how many there are in all.
-template <int ROWS>
-__device__ __forceinline__ int pairs_of(const Choices<ROWS>& p, int pairs, int expert, int first, int& count) {
+template <int ROWS, int T>
+__device__ __forceinline__ int count_of(const Choices<ROWS, T>& p, int pairs, int expert) {
+    int count = 0;
+    for (int i = threadIdx.x & 63; i < (pairs + 63) / 64 * 64; i += 64) count += __popcll(__ballot(i < pairs && p.expert[i] == expert));
+    return __builtin_amdgcn_readfirstlane(count);
+}
+// The pairs of an expert, in their order: lane l < 32 gets the (first + l)-th.
+template <int ROWS, int T>
+__device__ __forceinline__ int pairs_of(const Choices<ROWS, T>& p, int pairs, int expert, int first) {
     const int lane = threadIdx.x & 63;
-    int mine = 0;
-    count = 0;
+    int mine = 0, count = 0;
     for (int i = lane; i < (pairs + 63) / 64 * 64; i += 64) {
         const bool has = i < pairs && p.expert[i] == expert;
         const uint64_t all = __ballot(has);
@@ -272,18 +285,17 @@ __device__ __forceinline__ int pairs_of(const Choices<ROWS>& p, int pairs, int e
         if (lane < 32 && got) mine = got - 1;
         count += __popcll(all);
     }
-    count = __builtin_amdgcn_readfirstlane(count);
     return mine;
 }
 
 // What a wave asks for at a time: a super-block of N matrices, and the elements under it of T tokens of the expert.  Fewer than 16 tokens
 // leave most lanes of the operand without one, so 16 / T steps' operands come with one load: lane n takes token n % T at step n / T, and a
 // rotation inside 16 lanes brings it to where the step wants it.  (What the other lanes hold then are columns that nobody reads.)
-// T = 16 at 1 bit would take 64 registers: there the elements are read when they are needed.
+// T = 8 and more at 1 bit would take 32 registers and more: there the elements are read when they are needed.
 template <int BITS, int T, int N>
 struct Bundle {
     static constexpr int TILES = T > 16 ? T / 16 : 1, LOADS = T > 16 ? 4 : T / 4;      // column tiles; loads a tile and four steps
-    static constexpr bool TOKENS = BITS > 1 || T < 16;
+    static constexpr bool TOKENS = BITS == 1 ? T < 8 : BITS == 2 ? T < KMQ_T2 : true;
     static constexpr int WORDS = N * Granule<BITS>::WORDS + (TOKENS ? TILES * LOADS * Granule<BITS>::STEPS : 0);
     Granule<BITS> g[N];
     u32x4_t x[TILES][TOKENS ? Granule<BITS>::STEPS / 4 : 1][LOADS];
@@ -424,17 +436,18 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
     constexpr int TILES = Tokens<T>::TILES, D = depth(Bundle<BITS, T, 2>::WORDS), LANES = T < 16 ? 4 * T : 64;
     struct Smem {
         Tables<BITS> tables;
-        f32x4_t part[TEAMS][NW - 1][2][LANES];            // sums of a team's waves but the first
+        f32x4_t part[TEAMS][NW > 1 ? NW - 1 : 1][2][LANES];      // sums of a team's waves but the first
         PieceScales scales[TEAMS];
-        Choices<ROWS> choices;
+        Choices<ROWS, T> choices;
     };
     __shared__ Smem sm;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
     const int team = wave / NW, member = wave % NW, place = member * kWave + lane;
-    const Chosen chosen = find_choices<ROWS, NW * TEAMS * kWave>(a, sm.choices);
+    static_assert(sizeof(sm.tables) >= sizeof(int) * KMQ_MOE_MAX_EXPERTS, "counts");
+    find_choices<ROWS, T, NW * TEAMS * kWave>(a, sm.choices, reinterpret_cast<int*>(&sm.tables));
     const int columns = static_cast<int>(GATED ? a.hidden : a.width), units = columns / G::COLUMNS, pairs = a.rows * a.top_k;
     const int per_expert = static_cast<int>(GATED ? a.width >> 4 : a.hidden >> 5) / TEAMS;
-    const unsigned items = static_cast<unsigned>(chosen.all) * per_expert, each = items / gridDim.x, over = items - each * gridDim.x;
+    const unsigned items = static_cast<unsigned>(sm.choices.all) * per_expert, each = items / gridDim.x, over = items - each * gridDim.x;
     const int from = static_cast<int>(each * blockIdx.x + min(blockIdx.x, over)), to = from + static_cast<int>(each + (blockIdx.x < over));
     if (from >= to) return;
     uint16_t* const h = static_cast<uint16_t*>(a.workspace);
@@ -446,9 +459,23 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
     Scales<NW * kWave> scales;
     Matrix m[2];
     LookUp<BITS> l(sm.tables, lane);
-    // where the workgroup is: the `group`-th row blocks of the `which`-th expert e, its pairs from `first` on, a piece of the columns, of
-    // which super-blocks u .. end - 1 are this wave's; this lane's pair
-    int which = from / per_expert, group = from - which * per_expert, e = chosen.expert(which), first = 0, piece = 0, u, end, words, count, pair;
+    // where the workgroup is: the `group`-th row blocks of expert e, of whose `count` pairs those from `time` * T on (`times` in all), a piece
+    // of the columns, of which super-blocks u .. end - 1 are this wave's; this lane's pair.  An expert's items lie by row blocks first, so that
+    // all its tokens meet these while they are in the L2; `entry` is the list's first of the next expert.
+    int entry = from / per_expert, group, e, time, times, count, piece = 0, u, end, words, pair;
+    const auto find_expert = [&](int at) {
+        const int found = __builtin_amdgcn_readfirstlane(sm.choices.list[at]);
+        e = found >> 6;
+        count = count_of(sm.choices, pairs, e);
+        times = (count + T - 1) / T;
+        entry = at - (found & 63) + times;
+    };
+    find_expert(entry);
+    {
+        const int within = from - (entry - times) * per_expert;
+        group = within / times;
+        time = within - group * times;
+    }
     uint32_t centroids = 0;
     const auto ask_piece = [&] {
         constexpr int MOST = kPiece / G::COLUMNS;
@@ -471,12 +498,12 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
         m[1] = matrix_of<BITS>(GATED ? a.up : a.down, e, GATED ? block : 2 * block + 1, units);
         if (tokens_too) {
             const int lane = anew(static_cast<int>(threadIdx.x)) & 63, n = lane & 15, q = lane >> 4;
-            pair = pairs_of(sm.choices, pairs, e, first, count);
+            pair = pairs_of(sm.choices, pairs, e, time * T);
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
                 const int i = 16 * t + (T < 16 ? n % T : n), p = __shfl(pair, i);
                 tokens.at[t] = kNoRow;
-                if (first + i < count) tokens.at[t] = static_cast<uint32_t>(GATED ? p / a.top_k : p) * stride + 16u * q + (T < 16 ? n / T * 64u : 0u);
+                if (time * T + i < count) tokens.at[t] = static_cast<uint32_t>(GATED ? p / a.top_k : p) * stride + 16u * q + (T < 16 ? n / T * 64u : 0u);
             }
         }
         piece = 0;
@@ -500,20 +527,18 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
             __syncthreads();
         }
         // what comes next is asked for before the sums are joined
-        const int left = count - first < T ? count - first : T, block = group * TEAMS + team, now = pair;
-        bool more = true, other = false, whole = count <= T;
-        if (first + T < count) {
-            first += T;
-        } else {
-            first = 0;
-            if (++item == to) more = false;
-            else if (++group == per_expert) {
+        const int left = count - time * T < T ? count - time * T : T, block = group * TEAMS + team, now = pair;
+        const bool more = ++item < to, several = times > 1;
+        bool other = false;
+        if (more && ++time == times) {
+            time = 0;
+            if (++group == per_expert) {
                 group = 0;
-                e = chosen.expert(++which);
+                find_expert(entry);
                 other = true;
             }
         }
-        if (more) ask(other, other || !whole);
+        if (more) ask(other, other || several);
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
             if (16 * t >= left) break;
@@ -608,9 +633,10 @@ static void launch_moe_one(const MoeArgs& a, hipStream_t s) {
     moe_join_kernel<<<dim3(static_cast<unsigned>((a.hidden + 1023) / 1024), static_cast<unsigned>(a.rows)), 256, 0, s>>>(a);
 }
 #ifndef KMQ_MNW
-#define KMQ_MNW 4
+#define KMQ_MNW 1
 #define KMQ_MT4 4
-#define KMQ_MT 1
+#define KMQ_MNW4 2
+#define KMQ_MT 4
 #endif
 #ifndef KMQ_TM
 #define KMQ_TM 16
@@ -621,9 +647,10 @@ static void launch_moe_bits(const MoeArgs& a, hipStream_t s) {
     const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k;
     const bool thin = pairs <= 2 * static_cast<int64_t>(a.experts);       // about two tokens an expert
     if (a.rows <= 4) launch_moe_one<BITS, 4, 16, KMQ_NW, TEAMS>(a, s);
-    else if (a.rows <= 8 || (a.rows <= 16 && thin)) launch_moe_one<BITS, 8, 16, KMQ_NW, TEAMS>(a, s);
+    else if (a.rows <= 16 && thin) launch_moe_one<BITS, BITS == 1 ? 4 : 8, 16, KMQ_NW, TEAMS>(a, s);
+    else if (a.rows <= 8 && BITS > 1) launch_moe_one<BITS, 8, 16, KMQ_NW, TEAMS>(a, s);
     else if (a.rows <= 16) launch_moe_one<BITS, 16, 16, KMQ_NW, TEAMS>(a, s);
-    else launch_moe_one<BITS, KMQ_TM, KMQ_MOE_MAX_ROWS, KMQ_MNW, BITS == 4 ? KMQ_MT4 : KMQ_MT>(a, s);
+    else launch_moe_one<BITS, KMQ_TM, KMQ_MOE_MAX_ROWS, BITS == 4 ? KMQ_MNW4 : KMQ_MNW, BITS == 4 ? KMQ_MT4 : KMQ_MT>(a, s);
 }
 
 hipError_t launch_moe(const MoeArgs& a, hipStream_t s) {

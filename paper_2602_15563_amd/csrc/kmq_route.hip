@@ -101,6 +101,7 @@ __device__ __forceinline__ int lane_of_largest(uint64_t v) {
 // A wave a token; lane l holds experts l * PER .. l * PER + PER - 1.
 template <int PER>
 __global__ __launch_bounds__(kWave) void route_choose_kernel(RouteArgs a, int slices) {
+    constexpr int kAtOnce = PER <= 2 ? 16 : PER <= 4 ? 8 : 2;
     __shared__ double choice[kWave * PER];
     const int lane = threadIdx.x;
     const int64_t row = blockIdx.x;
@@ -108,11 +109,20 @@ __global__ __launch_bounds__(kWave) void route_choose_kernel(RouteArgs a, int sl
     const int64_t slice = static_cast<int64_t>(a.rows) * a.experts;
     double s[PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = lane * PER + i;
-        s[i] = 0.0;
-        if (e < a.experts)
-            for (int k = 0; k < slices; ++k) s[i] += logits[k * slice + e];
+    for (int i = 0; i < PER; ++i) s[i] = 0.0;
+    for (int k0 = 0; k0 < slices; k0 += kAtOnce) {        // (several slices at once: a memory round trip each would be most of the call)
+        double v[kAtOnce][PER];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int e = lane * PER + i;
+                v[k][i] = k0 + k < slices && e < a.experts ? logits[(k0 + k) * slice + e] : 0.0;
+            }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) s[i] += v[k][i];
     }
     if (a.sigmoid) {
 #pragma unroll
