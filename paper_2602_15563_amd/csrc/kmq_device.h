@@ -69,6 +69,23 @@ __device__ __forceinline__ double dpp_move64(double v) {
     const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, 0xF, 0xF, true));
     return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
 }
+// Of a lane's own value and that of the lane 16 (HALF: 32) away, which both of them get: as (first, second) by lane number.
+template <bool HALF>
+__device__ __forceinline__ u32x2_t across_rows(uint32_t v) {
+    if constexpr (HALF) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return u32x2_t{r[0], r[1]};
+    } else {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return u32x2_t{r[0], r[1]};
+    }
+}
+template <bool HALF>
+__device__ __forceinline__ double sum_across_rows(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const u32x2_t lo = across_rows<HALF>(static_cast<uint32_t>(u)), hi = across_rows<HALF>(static_cast<uint32_t>(u >> 32));
+    return __builtin_bit_cast(double, static_cast<uint64_t>(hi[0]) << 32 | lo[0]) + __builtin_bit_cast(double, static_cast<uint64_t>(hi[1]) << 32 | lo[1]);
+}
 // The sum over groups of LANES lanes, in all of them.
 template <int LANES>
 __device__ __forceinline__ double sum_over(double v) {
@@ -76,8 +93,8 @@ __device__ __forceinline__ double sum_over(double v) {
     v += dpp_move64<0x4E>(v);                             // quad_perm [2,3,0,1]
     v += dpp_move64<0x141>(v);                            // row_half_mirror
     if (LANES >= 16) v += dpp_move64<0x140>(v);           // row_mirror
-    if (LANES >= 32) v += __shfl_xor(v, 16);
-    if (LANES >= 64) v += __shfl_xor(v, 32);
+    if (LANES >= 32) v = sum_across_rows<false>(v);
+    if (LANES >= 64) v = sum_across_rows<true>(v);
     return v;
 }
 // 1 / sqrt(v): the unit's estimate and two Newton steps, each of which doubles its good bits.  Of an infinity it is zero, which the steps

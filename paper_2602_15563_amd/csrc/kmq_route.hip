@@ -66,22 +66,19 @@ __global__ __launch_bounds__(kRouteWaves * kWave) void route_product_kernel(Rout
     }
 }
 
-__device__ __forceinline__ double max_over_wave(double v) {
-    v = fmax(v, dpp_move64<0xB1>(v));                     // quad_perm [1,0,3,2]
-    v = fmax(v, dpp_move64<0x4E>(v));                     // quad_perm [2,3,0,1]
-    v = fmax(v, dpp_move64<0x141>(v));                    // row_half_mirror
-    v = fmax(v, dpp_move64<0x140>(v));                    // row_mirror
-    v = fmax(v, __shfl_xor(v, 16));
-    return fmax(v, __shfl_xor(v, 32));
-}
 __device__ __forceinline__ uint32_t max_over_wave(uint32_t v) {
     const auto other = [](uint32_t x, auto ctrl) { return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, 0xF, 0xF, true)); };
-    v = max(v, other(v, std::integral_constant<int, 0xB1>{}));
-    v = max(v, other(v, std::integral_constant<int, 0x4E>{}));
-    v = max(v, other(v, std::integral_constant<int, 0x141>{}));
-    v = max(v, other(v, std::integral_constant<int, 0x140>{}));
-    v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 16)));
-    return max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 32)));
+    v = max(v, other(v, std::integral_constant<int, 0xB1>{}));          // quad_perm [1,0,3,2]
+    v = max(v, other(v, std::integral_constant<int, 0x4E>{}));          // quad_perm [2,3,0,1]
+    v = max(v, other(v, std::integral_constant<int, 0x141>{}));         // row_half_mirror
+    v = max(v, other(v, std::integral_constant<int, 0x140>{}));         // row_mirror
+    u32x2_t r = across_rows<false>(v);
+    r = across_rows<true>(max(r[0], r[1]));
+    return max(r[0], r[1]);
+}
+__device__ __forceinline__ uint64_t max_over_wave(uint64_t v) {
+    const uint32_t hi = max_over_wave(static_cast<uint32_t>(v >> 32));
+    return static_cast<uint64_t>(hi) << 32 | max_over_wave(static_cast<uint32_t>(v >> 32) == hi ? static_cast<uint32_t>(v) : 0u);
 }
 
 // A number that orders as the value does; a NaN comes behind all of them, and 0 is left for what may not be chosen.
@@ -90,13 +87,10 @@ __device__ __forceinline__ uint64_t order_of(double v) {
     const uint64_t u = __builtin_bit_cast(uint64_t, v + 0.0);
     return u >> 63 ? ~u : u | (uint64_t(1) << 63);
 }
+// The value that such a number stands for (not of a NaN or of 0).
+__device__ __forceinline__ double value_of(uint64_t order) { return __builtin_bit_cast(double, order >> 63 ? order & ~(uint64_t(1) << 63) : ~order); }
 // The lowest lane that holds the largest of the wave's numbers.
-__device__ __forceinline__ int lane_of_largest(uint64_t v) {
-    const uint32_t hi = max_over_wave(static_cast<uint32_t>(v >> 32));
-    const uint32_t mine = static_cast<uint32_t>(v >> 32) == hi ? static_cast<uint32_t>(v) : 0u;
-    const uint32_t lo = max_over_wave(mine);
-    return __ffsll(__ballot(v == (static_cast<uint64_t>(hi) << 32 | lo))) - 1;
-}
+__device__ __forceinline__ int lane_of_largest(uint64_t v) { return __ffsll(__ballot(v == max_over_wave(v))) - 1; }
 
 // A wave a token; lane l holds experts l * PER .. l * PER + PER - 1.
 template <int PER>
@@ -128,11 +122,13 @@ __global__ __launch_bounds__(kWave) void route_choose_kernel(RouteArgs a, int sl
 #pragma unroll
         for (int i = 0; i < PER; ++i) s[i] = 1.0 / (1.0 + exp(-s[i]));
     } else {
-        double most = -__builtin_inf(), sum = 0.0;
+        uint64_t largest = 0;                             // (a NaN is the least of them)
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (lane * PER + i < a.experts) most = fmax(most, s[i]);
-        most = max_over_wave(most);
+            if (lane * PER + i < a.experts) largest = max(largest, order_of(s[i]));
+        largest = max_over_wave(largest);
+        const double most = largest == 1 ? __builtin_nan("") : value_of(largest);
+        double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             s[i] = exp(s[i] - most);
@@ -156,6 +152,7 @@ __global__ __launch_bounds__(kWave) void route_choose_kernel(RouteArgs a, int sl
         uint64_t mine = 0;
         if (lane < a.groups) {
             double best = -__builtin_inf(), next = -__builtin_inf();
+#pragma unroll 8
             for (int i = 0; i < size; ++i) {
                 const double c = choice[lane * size + i];
                 next = fmax(next, fmin(best, c));
@@ -185,8 +182,10 @@ __global__ __launch_bounds__(kWave) void route_choose_kernel(RouteArgs a, int sl
         for (int i = 0; i < PER; ++i)
             if (order[i] > best) { best = order[i]; at = i; score = s[i]; }
         const int from = lane_of_largest(best);
-        const int e = from * PER + __shfl(at, from);
-        score = __shfl(score, from);
+        const int e = from * PER + __builtin_amdgcn_readlane(at, from);
+        const uint64_t bits = __builtin_bit_cast(uint64_t, score);
+        score = __builtin_bit_cast(double, static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(bits >> 32), from))) << 32 |
+                                               static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(bits), from)));
         if (lane == j) { id = e; weight = score; }
 #pragma unroll
         for (int i = 0; i < PER; ++i)
