@@ -429,18 +429,20 @@ __device__ __forceinline__ int anew(int v) {
     return v;
 }
 
+template <int BITS, int T, int ROWS, int NW, int TEAMS>
+struct Shared {
+    Tables<BITS> tables;
+    f32x4_t part[TEAMS][NW > 1 ? NW - 1 : 1][2][NW > 1 ? (T < 16 ? 4 * T : 64) : 1];      // sums of a team's waves but the first
+    PieceScales scales[TEAMS];
+    Choices<ROWS, T> choices;
+};
+
 // A workgroup of TEAMS teams of NW waves; T tokens at a time.  GATED: rows of gate and up, else pairs of row blocks of down.
 template <int BITS, int T, int ROWS, int NW, int TEAMS, bool GATED>
 __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per_eu(waves_for(BITS, T)))) void moe_rows_kernel(MoeArgs a) {
     using G = Granule<BITS>;
     constexpr int TILES = Tokens<T>::TILES, D = depth(Bundle<BITS, T, 2>::WORDS), LANES = T < 16 ? 4 * T : 64;
-    struct Smem {
-        Tables<BITS> tables;
-        f32x4_t part[TEAMS][NW > 1 ? NW - 1 : 1][2][LANES];      // sums of a team's waves but the first
-        PieceScales scales[TEAMS];
-        Choices<ROWS, T> choices;
-    };
-    __shared__ Smem sm;
+    __shared__ Shared<BITS, T, ROWS, NW, TEAMS> sm;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
     const int team = wave / NW, member = wave % NW, place = member * kWave + lane;
     static_assert(sizeof(sm.tables) >= sizeof(int) * KMQ_MOE_MAX_EXPERTS, "counts");
@@ -618,39 +620,49 @@ __global__ __launch_bounds__(256) void moe_join_kernel(MoeArgs a) {
 
 size_t moe_workspace_bytes(int64_t rows, int64_t top_k, int64_t width, int64_t hidden) { return static_cast<size_t>(rows * top_k * (width * 2 + hidden * 4)); }
 
-#ifndef KMQ_NW
-#define KMQ_NW 4
-#define KMQ_TEAMS 1
-#define KMQ_GRID 4096
-#endif
-template <int BITS, int T, int ROWS, int NW, int TEAMS>
-static void launch_moe_one(const MoeArgs& a, hipStream_t s) {
-    constexpr int MOST = KMQ_GRID / (NW * TEAMS);
+template <int BITS, int T, int ROWS, int NW, int WAVES, bool GATED>
+static void launch_rows(const MoeArgs& a, hipStream_t s) {
+    constexpr int TEAMS = WAVES / NW, BY_WAVES = 4 * waves_for(BITS, T) / WAVES, BY_MEMORY = 160 * 1024 / sizeof(Shared<BITS, T, ROWS, NW, TEAMS>);
+    static_assert(8 % TEAMS == 0, "row blocks come in eights");
+    constexpr int64_t MOST = 256 * (BY_WAVES < BY_MEMORY ? BY_WAVES : BY_MEMORY);          // as many as run at once
     const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = pairs < a.experts ? pairs : a.experts;
-    const auto grid = [&](int64_t each) { return dim3(static_cast<unsigned>(experts * each < MOST ? experts * each : MOST)); };
-    moe_rows_kernel<BITS, T, ROWS, NW, TEAMS, true><<<grid(a.width / 16 / TEAMS), NW * TEAMS * kWave, 0, s>>>(a);
-    moe_rows_kernel<BITS, T, ROWS, NW, TEAMS, false><<<grid(a.hidden / 32 / TEAMS), NW * TEAMS * kWave, 0, s>>>(a);
-    moe_join_kernel<<<dim3(static_cast<unsigned>((a.hidden + 1023) / 1024), static_cast<unsigned>(a.rows)), 256, 0, s>>>(a);
+    const int64_t items = (experts + pairs / T) * ((GATED ? a.width / 16 : a.hidden / 32) / TEAMS);
+    moe_rows_kernel<BITS, T, ROWS, NW, TEAMS, GATED><<<dim3(static_cast<unsigned>(items < MOST ? items : MOST)), WAVES * kWave, 0, s>>>(a);
 }
-#ifndef KMQ_MNW
-#define KMQ_MNW 1
-#define KMQ_MT4 4
-#define KMQ_MNW4 2
-#define KMQ_MT 4
-#endif
-#ifndef KMQ_TM
-#define KMQ_TM 16
-#endif
+template <int BITS, int T, bool GATED>
+static void launch_few(const MoeArgs& a, hipStream_t s) {
+    const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = pairs < a.experts ? pairs : a.experts;
+    const int64_t units = (GATED ? a.hidden : a.width) / Granule<BITS>::COLUMNS, items = experts * (GATED ? a.width / 16 : a.hidden / 32);
+    if constexpr (BITS == 4) launch_rows<BITS, T, 16, 4, 8, GATED>(a, s);
+    else if (units < 16 && items >= 2048) launch_rows<BITS, T, 16, 2, 4, GATED>(a, s);
+    else launch_rows<BITS, T, 16, 4, 4, GATED>(a, s);
+}
+template <int BITS, bool GATED>
+static void launch_product(const MoeArgs& a, hipStream_t s) {
+    const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = a.experts;
+    if (a.rows <= 4 || (a.rows <= 16 && 2 * pairs <= (BITS == 1 ? 6 : 3) * experts)) {
+        launch_few<BITS, 4, GATED>(a, s);
+        return;
+    }
+    if constexpr (BITS > 1) {
+        if (a.rows <= 8 || (a.rows <= 16 && pairs <= 3 * experts)) {
+            launch_few<BITS, 8, GATED>(a, s);
+            return;
+        }
+    }
+    if (a.rows <= 16) launch_rows<BITS, 16, 16, 2, 4, GATED>(a, s);
+    else if constexpr (BITS == 4) {
+        // (eight teams need row blocks in sixteens: the down projection's pairs of them come in fours)
+        if (GATED || a.hidden % 256 == 0) launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, 1, 8, GATED>(a, s);
+        else launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, 2, 8, GATED>(a, s);
+    }
+    else launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, 1, 4, GATED>(a, s);
+}
 template <int BITS>
 static void launch_moe_bits(const MoeArgs& a, hipStream_t s) {
-    constexpr int TEAMS = BITS == 4 ? 2 : KMQ_TEAMS;
-    const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k;
-    const bool thin = pairs <= 2 * static_cast<int64_t>(a.experts);       // about two tokens an expert
-    if (a.rows <= 4) launch_moe_one<BITS, 4, 16, KMQ_NW, TEAMS>(a, s);
-    else if (a.rows <= 16 && thin) launch_moe_one<BITS, BITS == 1 ? 4 : 8, 16, KMQ_NW, TEAMS>(a, s);
-    else if (a.rows <= 8 && BITS > 1) launch_moe_one<BITS, 8, 16, KMQ_NW, TEAMS>(a, s);
-    else if (a.rows <= 16) launch_moe_one<BITS, 16, 16, KMQ_NW, TEAMS>(a, s);
-    else launch_moe_one<BITS, KMQ_TM, KMQ_MOE_MAX_ROWS, BITS == 4 ? KMQ_MNW4 : KMQ_MNW, BITS == 4 ? KMQ_MT4 : KMQ_MT>(a, s);
+    launch_product<BITS, true>(a, s);
+    launch_product<BITS, false>(a, s);
+    moe_join_kernel<<<dim3(static_cast<unsigned>((a.hidden + 1023) / 1024), static_cast<unsigned>(a.rows)), 256, 0, s>>>(a);
 }
 
 hipError_t launch_moe(const MoeArgs& a, hipStream_t s) {
