@@ -620,7 +620,7 @@ kmq_status kmq_block_norm(const uint16_t* x, int64_t x_stride, int64_t rows, int
         (out && !kmq::row_of(out_stride, width, kmq::kMaxStride)) || (normed && !kmq::row_of(normed_stride, width, kmq::kMaxStride))) return KMQ_ERR_SHAPE;
     if (!kmq::aligned(x, 16) || !kmq::aligned(join->residual, 16) || !kmq::aligned(join->gate, 16) || !kmq::aligned(join->post_gain, 16) ||
         !kmq::aligned(join->pre_gain, 16) || !kmq::aligned(out, 16) || !kmq::aligned(normed, 16)) return KMQ_ERR_ALIGN;
-    const kmq::BlockNormArgs a{x, join->residual, join->gate, join->post_gain, join->pre_gain, x_stride, join->residual_stride, join->gate_stride,
+    const kmq::BlockNormArgs a{x, join->residual, join->gate, join->post_norm ? join->post_gain : nullptr, normed ? join->pre_gain : nullptr, x_stride, join->residual_stride, join->gate_stride,
                                rows, width, join->scale, join->residual_scale, join->eps, join->post_norm != 0, join->gate && join->gate_sigmoid,
                                out, normed, out_stride, normed_stride};
     return kmq::hip_status(kmq::launch_block_norm(a, static_cast<hipStream_t>(hip_stream)));
