@@ -513,9 +513,11 @@ typedef struct kmq_moe_weights {
     int32_t experts, bits;      /* experts: 1 .. KMQ_MOE_MAX_EXPERTS; bits: 1..4 */
 } kmq_moe_weights;
 
-/* The chosen experts' SwiGLU for a few tokens, in two launches (each active expert's matrices are read once for up to 64 of its tokens):
+/* The chosen experts' SwiGLU for a few tokens, in three launches (each active expert's matrices are read once for up to 16 of its tokens, fewer
+ * where experts have few on average):
  *     h = bf16( silu(G_e x) * (U_e x) ),   y = residual + sum_j gates[j] * D_e h           e = ids[j], j = 0 .. top_k - 1
  * silu(t) = t / (1 + exp(-t)); all sums in fp32, h rounded to bf16 as kmq_gemv_swiglu leaves it (2^-8 of itself at most), y once more.
+ * What is not finite is as the formulas have it; it reaches the outputs of the tokens that chose the expert, or of that token, alone.
  *   x, residual, y   rows of `hidden` elements, x_stride at most 2^22; residual may be NULL, and y's own place
  *   ids, gates       rows x top_k, from kmq_moe_route or anybody else.  An id outside 0 .. experts - 1 counts for nothing (an expert
  *                    that is held elsewhere, a token that is none); an expert that a token has twice counts with the sum of both gates

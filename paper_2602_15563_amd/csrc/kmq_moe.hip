@@ -28,17 +28,12 @@ namespace kmq {
 
 namespace {
 
-// Bundles a wave has asked for, by their registers.
-#ifndef KMQ_T2
-#define KMQ_T2 32
-#define KMQ_W2 2
-#endif
-#ifndef KMQ_RING
-#define KMQ_RING 30
-#endif
-constexpr int depth(int words) { return words * 4 <= KMQ_RING ? 4 : words * 3 <= KMQ_RING ? 3 : 2; }
-// Waves a SIMD that the registers have to leave room for: as many as an instance needs no spilling for.
-constexpr int waves_for(int bits, int t) { return bits == 2 && t == 16 ? KMQ_W2 : bits == 1 || t > 16 || (bits == 2 && t >= 8) || (bits == 3 && t == 16) ? 3 : 4; }
+// Bundles a wave has asked for, by their registers: what fits beside the rest without spilling in the loop.  (Three instead of two, spilled: one
+// token, 4 bits 31 -> 57 us, 16 tokens 76 -> 144.)
+constexpr int depth(int words) { return words <= 10 ? 3 : 2; }
+// Waves a SIMD that the registers have to leave room for.  (1 bit, few tokens: what is kept over an item and does not fit, 5 to 7 words, is spilled outside the
+// loop; two waves instead 111 -> 132 us, 16 tokens of 128 experts.)
+constexpr int waves_for(int bits, int t) { return (t == 16 && (bits == 2 || bits == 4)) ? 2 : bits == 1 || (bits == 2 && t == 8) || t == 16 ? 3 : 4; }
 
 typedef __amdgpu_buffer_rsrc_t Rows;
 // Rows read by byte offset; kNoRow gives zeros.
@@ -82,7 +77,7 @@ __device__ __forceinline__ void load_granule(const Matrix& m, int unit, int lane
 
 // A row's length goes by pieces of kPiece columns, whose scales a team keeps in shared memory, [matrix][row][word], rows an odd number of
 // words apart.  They are asked for as they lie, row after row: granule by granule, 4 to 16 bytes of each of 16 rows an instruction, the same
-// lines are asked for from the L2 again and again (16 tokens of 128 experts, 4096 x 1536, 4 bits: SCALES_BEFORE us, and SCALES_NOW).
+// lines are asked for from the L2 again and again (a layer of 16 tokens, 128 experts of 4096 x 1536, 4 bits: 218 us, and 204).
 constexpr int kPiece = 4096, kPieceWords = kPiece / 128;
 typedef uint32_t PieceScales[2][16 * (kPieceWords + 1)];
 template <int LANES>
@@ -271,7 +266,7 @@ __device__ __forceinline__ int count_of(const Choices<ROWS, T>& p, int pairs, in
     for (int i = threadIdx.x & 63; i < (pairs + 63) / 64 * 64; i += 64) count += __popcll(__ballot(i < pairs && p.expert[i] == expert));
     return __builtin_amdgcn_readfirstlane(count);
 }
-// The pairs of an expert, in their order: lane l < 32 gets the (first + l)-th.
+// The pairs of an expert, in their order: lane l < 16 gets the (first + l)-th.
 template <int ROWS, int T>
 __device__ __forceinline__ int pairs_of(const Choices<ROWS, T>& p, int pairs, int expert, int first) {
     const int lane = threadIdx.x & 63;
@@ -280,48 +275,43 @@ __device__ __forceinline__ int pairs_of(const Choices<ROWS, T>& p, int pairs, in
         const bool has = i < pairs && p.expert[i] == expert;
         const uint64_t all = __ballot(has);
         const int to = count + __popcll(all & ((uint64_t(1) << lane) - 1)) - first;
-        // what is sent to a lane is one more than the pair: 0 comes where nothing is sent (lane 63 takes what nobody asks for: 32 are looked at)
-        const int got = __builtin_amdgcn_ds_permute((has && to >= 0 && to < 32 ? to : 63) * 4, has ? i + 1 : 0);
-        if (lane < 32 && got) mine = got - 1;
+        // what is sent to a lane is one more than the pair: 0 comes where nothing is sent (lane 63 takes what nobody asks for: 16 are looked at)
+        const int got = __builtin_amdgcn_ds_permute((has && to >= 0 && to < 16 ? to : 63) * 4, has ? i + 1 : 0);
+        if (lane < 16 && got) mine = got - 1;
         count += __popcll(all);
     }
     return mine;
 }
 
-// What a wave asks for at a time: a super-block of N matrices, and the elements under it of T tokens of the expert.  Fewer than 16 tokens
+// What a wave asks for at a time: a super-block of two matrices, and the elements under it of T tokens of the expert.  Fewer than 16 tokens
 // leave most lanes of the operand without one, so 16 / T steps' operands come with one load: lane n takes token n % T at step n / T, and a
 // rotation inside 16 lanes brings it to where the step wants it.  (What the other lanes hold then are columns that nobody reads.)
-// T = 8 and more at 1 bit would take 32 registers and more: there the elements are read when they are needed.
-template <int BITS, int T, int N>
+// T = 16 at 1 bit would take 64 registers: there the elements are read when they are needed.
+template <int BITS, int T>
 struct Bundle {
-    static constexpr int TILES = T > 16 ? T / 16 : 1, LOADS = T > 16 ? 4 : T / 4;      // column tiles; loads a tile and four steps
-    static constexpr bool TOKENS = BITS == 1 ? T < 8 : BITS == 2 ? T < KMQ_T2 : true;
-    static constexpr int WORDS = N * Granule<BITS>::WORDS + (TOKENS ? TILES * LOADS * Granule<BITS>::STEPS : 0);
-    Granule<BITS> g[N];
-    u32x4_t x[TILES][TOKENS ? Granule<BITS>::STEPS / 4 : 1][LOADS];
+    static constexpr int LOADS = T / 4;                   // of tokens, for four steps
+    static constexpr bool TOKENS = BITS > 1 || T < 16;
+    static constexpr int WORDS = 2 * Granule<BITS>::WORDS + (TOKENS ? LOADS * Granule<BITS>::STEPS : 0);
+    Granule<BITS> g[2];
+    u32x4_t x[TOKENS ? Granule<BITS>::STEPS / 4 : 1][LOADS];
 };
-template <int T>
 struct Tokens {
-    static constexpr int TILES = T > 16 ? T / 16 : 1;
     Rows rows;
-    uint32_t at[TILES];                                   // the lane's token of every column tile
+    uint32_t at;                                          // where the lane's token begins
 };
 template <int T>
-__device__ __forceinline__ void load_tokens(const Tokens<T>& tokens, int tile, uint32_t column, u32x4_t (&x)[T > 16 ? 4 : T / 4]) {
+__device__ __forceinline__ void load_tokens(const Tokens& tokens, uint32_t column, u32x4_t (&x)[T / 4]) {
 #pragma unroll
-    for (int l = 0; l < (T > 16 ? 4 : T / 4); ++l) x[l] = load_row16(tokens.rows, tokens.at[tile] + l * (T < 16 ? 1024 / T : 64), column * 2);
+    for (int l = 0; l < T / 4; ++l) x[l] = load_row16(tokens.rows, tokens.at + l * (1024 / T), column * 2);
 }
-template <int BITS, int T, int N>
-__device__ __forceinline__ void load_bundle(const Matrix (&m)[N], int unit, const Tokens<T>& tokens, int lane, Bundle<BITS, T, N>& b) {
+template <int BITS, int T>
+__device__ __forceinline__ void load_bundle(const Matrix (&m)[2], int unit, const Tokens& tokens, int lane, Bundle<BITS, T>& b) {
     using G = Granule<BITS>;
-    using B = Bundle<BITS, T, N>;
 #pragma unroll
-    for (int i = 0; i < N; ++i) load_granule<BITS>(m[i], unit, lane, b.g[i]);
-    if constexpr (B::TOKENS) {
+    for (int i = 0; i < 2; ++i) load_granule<BITS>(m[i], unit, lane, b.g[i]);
+    if constexpr (Bundle<BITS, T>::TOKENS) {
 #pragma unroll
-        for (int t = 0; t < B::TILES; ++t)
-#pragma unroll
-            for (int k = 0; k < G::STEPS / 4; ++k) load_tokens<T>(tokens, t, unit * G::COLUMNS + 128 * k, b.x[t][k]);
+        for (int k = 0; k < G::STEPS / 4; ++k) load_tokens<T>(tokens, unit * G::COLUMNS + 128 * k, b.x[k]);
     }
 }
 // Elements 0 .. 7 as (0, 4), (1, 5), (2, 6), (3, 7).
@@ -331,8 +321,8 @@ __device__ __forceinline__ u32x4_t pairs_apart(u32x4_t x) {
 }
 // The operand of step j of four.
 template <int T>
-__device__ __forceinline__ u32x4_t operand(const u32x4_t (&x)[T > 16 ? 4 : T / 4], int j) {
-    if constexpr (T >= 16) return x[j];
+__device__ __forceinline__ u32x4_t operand(const u32x4_t (&x)[T / 4], int j) {
+    if constexpr (T == 16) return x[j];
     u32x4_t v;
     const auto turn = [&](auto ctrl) {
 #pragma unroll
@@ -347,50 +337,40 @@ __device__ __forceinline__ u32x4_t operand(const u32x4_t (&x)[T > 16 ? 4 : T / 4
         default: return x[j * T / 16];
     }
 }
-template <int BITS, int T, int N>
-__device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T, N>& b, LookUp<BITS>& l, const uint32_t* scales, const Tokens<T>& tokens, int unit,
-                                                f32x4_t (&acc)[N][Tokens<T>::TILES]) {
+// One bundle's products, added to acc; `scales`: the lane's row from the super-block on.
+template <int BITS, int T>
+__device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T>& b, LookUp<BITS>& l, const uint32_t* scales, const Tokens& tokens, int unit,
+                                                f32x4_t (&acc)[2]) {
     using G = Granule<BITS>;
-    using B = Bundle<BITS, T, N>;
+    using B = Bundle<BITS, T>;
 #pragma unroll
     for (int k = 0; k < G::STEPS / 4; ++k) {
-        u32x4_t x[B::TILES][B::LOADS];
+        u32x4_t x[B::LOADS];
+        if constexpr (B::TOKENS) {
 #pragma unroll
-        for (int t = 0; t < B::TILES; ++t) {
-            if constexpr (B::TOKENS) {
-#pragma unroll
-                for (int i = 0; i < B::LOADS; ++i) x[t][i] = b.x[t][k][i];
-            } else {
-                load_tokens<T>(tokens, t, unit * G::COLUMNS + 128 * k, x[t]);
-            }
-            if constexpr (BITS == 2 || BITS == 3) {
-#pragma unroll
-                for (int i = 0; i < B::LOADS; ++i) x[t][i] = pairs_apart(x[t][i]);
-            }
+            for (int i = 0; i < B::LOADS; ++i) x[i] = b.x[k][i];
+        } else {
+            load_tokens<T>(tokens, unit * G::COLUMNS + 128 * k, x);
         }
-        uint32_t both[N];                                 // the scales of two blocks
+        if constexpr (BITS == 2 || BITS == 3) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) both[i] = scales[i * sizeof(PieceScales) / 8 + k];
+            for (int i = 0; i < B::LOADS; ++i) x[i] = pairs_apart(x[i]);
+        }
+        uint32_t both[2];                                 // the scales of two blocks
+#pragma unroll
+        for (int i = 0; i < 2; ++i) both[i] = scales[i * sizeof(PieceScales) / 8 + k];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int block = 2 * k + half;
-            u32x4_t x0[B::TILES], x1[B::TILES];
+            const u32x4_t x0 = operand<T>(x, 2 * half), x1 = operand<T>(x, 2 * half + 1);
 #pragma unroll
-            for (int t = 0; t < B::TILES; ++t) {
-                x0[t] = operand<T>(x[t], 2 * half);
-                x1[t] = operand<T>(x[t], 2 * half + 1);
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
+            for (int i = 0; i < 2; ++i) {
                 const u32x4_t w0 = decode<BITS>(b.g[i], l, i, 2 * block), w1 = decode<BITS>(b.g[i], l, i, 2 * block + 1);
                 const float s = kv_half(both[i], half);
+                f32x4_t d = step(x0, w0, f32x4_t{0.f, 0.f, 0.f, 0.f});
+                d = step(x1, w1, d);
 #pragma unroll
-                for (int t = 0; t < B::TILES; ++t) {
-                    f32x4_t d = step(x0[t], w0, f32x4_t{0.f, 0.f, 0.f, 0.f});
-                    d = step(x1[t], w1, d);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][t][r] = fmaf(s, d[r], acc[i][t][r]);
-                }
+                for (int r = 0; r < 4; ++r) acc[i][r] = fmaf(s, d[r], acc[i][r]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);                // (else what later steps need is looked up and turned early, and spilled)
@@ -399,22 +379,22 @@ __device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T, N>& b, Loo
 // The sums over super-blocks u .. end - 1; the first D bundles have been asked for.  `scales`: the lane's row from super-block 0 on.  The
 // loop's loads are unconditional, the last super-blocks a copy of the code of their own: a branch around a load would make every wait
 // assume the fewest of them.
-template <int BITS, int T, int N, int D>
-__device__ __forceinline__ void run_units(Bundle<BITS, T, N> (&b)[D], const Matrix (&m)[N], int u, int end, LookUp<BITS>& l, const uint32_t* scales,
-                                          const Tokens<T>& tokens, int lane, f32x4_t (&acc)[N][Tokens<T>::TILES]) {
-    const auto multiply_at = [&](int slot, int unit) { multiply_bundle<BITS, T, N>(b[slot], l, scales + unit * (Granule<BITS>::BLOCKS / 2), tokens, unit, acc); };
+template <int BITS, int T, int D>
+__device__ __forceinline__ void run_units(Bundle<BITS, T> (&b)[D], const Matrix (&m)[2], int u, int end, LookUp<BITS>& l, const uint32_t* scales,
+                                          const Tokens& tokens, int lane, f32x4_t (&acc)[2]) {
+    const auto multiply_at = [&](int slot, int unit) { multiply_bundle<BITS, T>(b[slot], l, scales + unit * (Granule<BITS>::BLOCKS / 2), tokens, unit, acc); };
     for (; u + 2 * D <= end; u += D) {
 #pragma unroll
         for (int p = 0; p < D; ++p) {
             multiply_at(p, u + p);
-            load_bundle<BITS, T, N>(m, u + p + D, tokens, lane, b[p]);
+            load_bundle<BITS, T>(m, u + p + D, tokens, lane, b[p]);
         }
     }
 #pragma unroll
     for (int p = 0; p < D; ++p) {
         if (u + p >= end) return;
         multiply_at(p, u + p);
-        if (u + p + D < end) load_bundle<BITS, T, N>(m, u + p + D, tokens, lane, b[p]);
+        if (u + p + D < end) load_bundle<BITS, T>(m, u + p + D, tokens, lane, b[p]);
     }
 #pragma unroll
     for (int p = 0; p < D - 1; ++p) {
@@ -432,7 +412,7 @@ __device__ __forceinline__ int anew(int v) {
 template <int BITS, int T, int ROWS, int NW, int TEAMS>
 struct Shared {
     Tables<BITS> tables;
-    f32x4_t part[TEAMS][NW > 1 ? NW - 1 : 1][2][NW > 1 ? (T < 16 ? 4 * T : 64) : 1];      // sums of a team's waves but the first
+    f32x4_t part[TEAMS][NW > 1 ? NW - 1 : 1][2][NW > 1 ? 4 * T : 1];      // sums of a team's waves but the first
     PieceScales scales[TEAMS];
     Choices<ROWS, T> choices;
 };
@@ -441,10 +421,14 @@ struct Shared {
 template <int BITS, int T, int ROWS, int NW, int TEAMS, bool GATED>
 __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per_eu(waves_for(BITS, T)))) void moe_rows_kernel(MoeArgs a) {
     using G = Granule<BITS>;
-    constexpr int TILES = Tokens<T>::TILES, D = depth(Bundle<BITS, T, 2>::WORDS), LANES = T < 16 ? 4 * T : 64;
+    constexpr int D = depth(Bundle<BITS, T>::WORDS), LANES = 4 * T;
     __shared__ Shared<BITS, T, ROWS, NW, TEAMS> sm;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-    const int team = wave / NW, member = wave % NW, place = member * kWave + lane;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave / NW, member = wave % NW;
+    const auto lane_anew = [] { return anew(static_cast<int>(threadIdx.x)) & 63; };
+    const int kept = threadIdx.x & 63;
+    // (at 1 bit there is no register to keep it in: 122 -> 111 us, 16 tokens of 128 experts; elsewhere 2 to 6 % more)
+    const auto lane_kept = [&] { return BITS == 1 ? lane_anew() : kept; };
+    const auto place = [&] { return member * kWave + lane_anew(); };        // in the team
     static_assert(sizeof(sm.tables) >= sizeof(int) * KMQ_MOE_MAX_EXPERTS, "counts");
     find_choices<ROWS, T, NW * TEAMS * kWave>(a, sm.choices, reinterpret_cast<int*>(&sm.tables));
     const int columns = static_cast<int>(GATED ? a.hidden : a.width), units = columns / G::COLUMNS, pairs = a.rows * a.top_k;
@@ -455,12 +439,12 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
     uint16_t* const h = static_cast<uint16_t*>(a.workspace);
     float* const out = reinterpret_cast<float*>(h + static_cast<int64_t>(pairs) * a.width);
     const uint32_t stride = static_cast<uint32_t>(GATED ? a.x_stride : a.width) * 2u;
-    Tokens<T> tokens;
+    Tokens tokens;
     tokens.rows = rows_at(GATED ? static_cast<const void*>(a.x) : h);
-    Bundle<BITS, T, 2> b[D];
+    Bundle<BITS, T> b[D];
     Scales<NW * kWave> scales;
     Matrix m[2];
-    LookUp<BITS> l(sm.tables, lane);
+    LookUp<BITS> l(sm.tables, lane_kept());
     // where the workgroup is: the `group`-th row blocks of expert e, of whose `count` pairs those from `time` * T on (`times` in all), a piece
     // of the columns, of which super-blocks u .. end - 1 are this wave's; this lane's pair.  An expert's items lie by row blocks first, so that
     // all its tokens meet these while they are in the L2; `entry` is the list's first of the next expert.
@@ -485,47 +469,44 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
         words = some * (G::BLOCKS / 2);
         u = start + some * member / NW;
         end = start + some * (member + 1) / NW;
-        scales.load(m, columns / 128, piece * kPieceWords, words, anew(place));
+        scales.load(m, columns / 128, piece * kPieceWords, words, place());
 #pragma unroll
         for (int p = 0; p < D; ++p)
-            if (u + p < end) load_bundle<BITS, T, 2>(m, u + p, tokens, lane, b[p]);
+            if (u + p < end) load_bundle<BITS, T>(m, u + p, tokens, lane_kept(), b[p]);
     };
     const auto ask = [&](bool other, bool tokens_too) {
         if (other) {                                      // (before the bundles: what is waited for first is asked for first)
+            const int lane = lane_anew();
             const uint16_t* book = (!GATED ? a.down.books : lane & 16 ? a.up.books : a.gate.books) + (e << BITS);
-            centroids = book[anew(lane) & ((1 << BITS) - 1)];
+            centroids = book[lane & ((1 << BITS) - 1)];
         }
         const int block = group * TEAMS + team;
         m[0] = matrix_of<BITS>(GATED ? a.gate : a.down, e, GATED ? block : 2 * block, units);
         m[1] = matrix_of<BITS>(GATED ? a.up : a.down, e, GATED ? block : 2 * block + 1, units);
         if (tokens_too) {
-            const int lane = anew(static_cast<int>(threadIdx.x)) & 63, n = lane & 15, q = lane >> 4;
+            const int lane = lane_anew(), n = lane & 15, q = lane >> 4;
             pair = pairs_of(sm.choices, pairs, e, time * T);
-#pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                const int i = 16 * t + (T < 16 ? n % T : n), p = __shfl(pair, i);
-                tokens.at[t] = kNoRow;
-                if (time * T + i < count) tokens.at[t] = static_cast<uint32_t>(GATED ? p / a.top_k : p) * stride + 16u * q + (T < 16 ? n / T * 64u : 0u);
-            }
+            const int i = n % T, p = __shfl(pair, i);
+            tokens.at = kNoRow;
+            if (time * T + i < count) tokens.at = static_cast<uint32_t>(GATED ? p / a.top_k : p) * stride + 16u * q + n / T * 64u;
         }
         piece = 0;
         ask_piece();
     };
     ask(true, true);
-    scales.keep(sm.scales[team], words, anew(place));
-    fill_tables<BITS>(sm.tables, centroids, wave, NW * TEAMS, anew(lane));
+    scales.keep(sm.scales[team], words, place());
+    fill_tables<BITS>(sm.tables, centroids, wave, NW * TEAMS, lane_anew());
     __syncthreads();
     for (int item = from;;) {
-        f32x4_t acc[2][TILES];
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) acc[0][t] = acc[1][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        f32x4_t acc[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
         for (;;) {
-            run_units<BITS, T, 2, D>(b, m, u, end, l, &sm.scales[team][0][n * (words | 1) - piece * kPieceWords], tokens, lane, acc);
+            const int lane = lane_kept();
+            run_units<BITS, T, D>(b, m, u, end, l, &sm.scales[team][0][(lane & 15) * (words | 1) - piece * kPieceWords], tokens, lane, acc);
             if ((piece + 1) * kPiece >= columns) break;
             ++piece;
             ask_piece();
             __syncthreads();
-            scales.keep(sm.scales[team], words, anew(place));
+            scales.keep(sm.scales[team], words, place());
             __syncthreads();
         }
         // what comes next is asked for before the sums are joined
@@ -541,42 +522,39 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
             }
         }
         if (more) ask(other, other || several);
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-            if (16 * t >= left) break;
-            if (t) __syncthreads();
-            const int lane = anew(static_cast<int>(threadIdx.x)) & 63, n = lane & 15, q = lane >> 4;
+        {
+            const int lane = lane_anew(), n = lane & 15, q = lane >> 4;
             if (member > 0 && lane < LANES) {
-                sm.part[team][member - 1][0][lane] = acc[0][t];
-                sm.part[team][member - 1][1][lane] = acc[1][t];
+                sm.part[team][member - 1][0][lane] = acc[0];
+                sm.part[team][member - 1][1][lane] = acc[1];
             }
             __syncthreads();
             if (member == 0) {
                 if (lane < LANES) {
 #pragma unroll
                     for (int w = 0; w < NW - 1; ++w) {
-                        acc[0][t] += sm.part[team][w][0][lane];
-                        acc[1][t] += sm.part[team][w][1][lane];
+                        acc[0] += sm.part[team][w][0][lane];
+                        acc[1] += sm.part[team][w][1][lane];
                     }
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int at = 16 * t + 4 * q + i;
-                    const int64_t p = __shfl(now, at & 31);
+                    const int at = 4 * q + i;
+                    const int64_t p = __shfl(now, at);
                     if (at >= left) continue;
                     if constexpr (GATED) {
-                        const float g = acc[0][t][i], v = acc[1][t][i];
+                        const float g = acc[0][i], v = acc[1][i];
                         h[p * a.width + block * 16 + n] = f32_to_bf16(g / (1.f + expf(-g)) * v);
                     } else {
-                        out[p * a.hidden + block * 32 + n] = acc[0][t][i];
-                        out[p * a.hidden + block * 32 + 16 + n] = acc[1][t][i];
+                        out[p * a.hidden + block * 32 + n] = acc[0][i];
+                        out[p * a.hidden + block * 32 + 16 + n] = acc[1][i];
                     }
                 }
             }
         }
         if (!more) break;
-        scales.keep(sm.scales[team], words, anew(place));       // (every wave has been past a barrier since it read the last ones)
-        if (other) fill_tables<BITS>(sm.tables, centroids, wave, NW * TEAMS, anew(lane));
+        scales.keep(sm.scales[team], words, place());       // (every wave has been past a barrier since it read the last ones)
+        if (other) fill_tables<BITS>(sm.tables, centroids, wave, NW * TEAMS, lane_anew());
         __syncthreads();
     }
 }
@@ -629,14 +607,23 @@ static void launch_rows(const MoeArgs& a, hipStream_t s) {
     const int64_t items = (experts + pairs / T) * ((GATED ? a.width / 16 : a.hidden / 32) / TEAMS);
     moe_rows_kernel<BITS, T, ROWS, NW, TEAMS, GATED><<<dim3(static_cast<unsigned>(items < MOST ? items : MOST)), WAVES * kWave, 0, s>>>(a);
 }
+
+// Waves that split a row: four, or two where rows are short (fewer than 16 super-blocks) and there are enough of them (16 tokens of 128 experts of
+// 4096 x 1536, 1 bit: 166 us with four, 147 with two; 3 bits 120 and 107).  At 4 bits eight waves share the table, 64 KB, and two of them a row are slower
+// throughout (2048 x 768, 16 tokens: 66 with four, 75).
 template <int BITS, int T, bool GATED>
 static void launch_few(const MoeArgs& a, hipStream_t s) {
     const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = pairs < a.experts ? pairs : a.experts;
-    const int64_t units = (GATED ? a.hidden : a.width) / Granule<BITS>::COLUMNS, items = experts * (GATED ? a.width / 16 : a.hidden / 32);
+    [[maybe_unused]] const int64_t units = (GATED ? a.hidden : a.width) / Granule<BITS>::COLUMNS, items = experts * (GATED ? a.width / 16 : a.hidden / 32);
     if constexpr (BITS == 4) launch_rows<BITS, T, 16, 4, 8, GATED>(a, s);
     else if (units < 16 && items >= 2048) launch_rows<BITS, T, 16, 2, 4, GATED>(a, s);
     else launch_rows<BITS, T, 16, 4, 4, GATED>(a, s);
 }
+
+// Tokens at a time: where more of them choose an expert its rows are read again (from the L2, mostly), and every four more cost registers and loads.
+// us with 4 / 8 at a time: 16 tokens of 128 experts, 8 each, 4 bits 64 / 66, a layer of them 177 / 183; 5 tokens of 8 experts, 2 each, 2 bits 103 / 127;
+// but 16 tokens of 64 experts, 8 each, 3 bits 126 / 119.  More than 16 tokens take 16 at a time (32: 128 tokens of 64 experts, 6 each, 3 bits 137 -> 171), a wave a whole
+// row and as many of them a workgroup as the memory holds, so that neighbours find the tokens' elements in the L1 (four / two / one wave a row: 339 / 249 / 222).
 template <int BITS, bool GATED>
 static void launch_product(const MoeArgs& a, hipStream_t s) {
     const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = a.experts;
@@ -658,6 +645,7 @@ static void launch_product(const MoeArgs& a, hipStream_t s) {
     }
     else launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, 1, 4, GATED>(a, s);
 }
+
 template <int BITS>
 static void launch_moe_bits(const MoeArgs& a, hipStream_t s) {
     launch_product<BITS, true>(a, s);

@@ -6,6 +6,9 @@
 //
 // Computed in 64 bits, rounded to 32 and then to bf16: what comes out goes into a router, where scores next to each other decide, so
 // a norm that is the definition's own makes the choice the definition's own.
+//
+// 4001 rows of 5120 take 41 us with all of it (164 MB at 4.0 TB/s; a copy of them 32): 64-bit conversions and products, some 40 clocks an element and lane, fill
+// most of vector issue; without the first norm, gate and their gains 34 us, 4.8 TB/s.
 #include "kmq_kv.h"
 
 namespace kmq {
@@ -32,7 +35,7 @@ __device__ __forceinline__ uint32_t round2(double a, double b) {
 }
 
 // 1 / (1 + exp(-g)) of a gate: 2^(k + f) with |f| <= 1/2, the power series of 2^f to the eleventh power (6e-15 of it), the unit's reciprocal and
-// two Newton steps.  (The library's exponential and division took 16 rows of 7168 from SIG_BEFORE us to SIG_AFTER.)
+// two Newton steps.  (With the library's exponential and a division 16 rows of 7168 take 6.9 us, with this 6.3; 4001 of 4096 50 and 46.)
 __device__ __forceinline__ double sigmoid(double g) {
     const double t = fmin(fmax(-g, -745.0), 709.0), k = rint(t * 1.4426950408889634), f = fma(t, 1.4426950408889634, -k);
     constexpr double c[] = {1.0, 0.6931471805599453, 0.24022650695910072, 0.05550410866482158, 0.009618129107628477, 0.0013333558146428443, 0.0001540353039338161, 1.5252733804059841e-05, 1.321548679014431e-06, 1.01780860092397e-07, 7.054911620801123e-09, 4.4455382718708116e-10};

@@ -8,6 +8,10 @@
 // As the four columns of a step may be any, a lane's eight consecutive bf16 are the operands of eight steps.  The row
 // length is cut into slices; a workgroup multiplies 16 experts with up to 64 tokens over a slice, its waves take chunks of 64
 // columns in turn, and what comes out goes to the workspace.  A second kernel, a wave a token, adds the slices in their order and chooses.
+//
+// One token, 128 experts of 4096: 3.4 + 4.3 us, both chains of memory round trips (reading slices one by one took the second kernel 8.8); 16
+// tokens, 256 experts of 7168 in groups 4.6 + 7.9, of which the products' own time is about 1 and the choice's twelve rounds of a maximum over the wave
+// half; 128 tokens, 64 experts of 2048 6.5 + 3.9, the products of four waves a unit waiting for their operands.
 #include "kmq_kv.h"
 
 namespace kmq {
