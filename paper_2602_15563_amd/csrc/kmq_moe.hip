@@ -376,13 +376,13 @@ __device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T>& b, LookUp
         __builtin_amdgcn_sched_barrier(0);                // (else what later steps need is looked up and turned early, and spilled)
     }
 }
-// The sums over super-blocks u .. end - 1; the first D bundles have been asked for.  `scales`: the lane's row from super-block 0 on.  The
+// The sums over super-blocks u .. end - 1; the first D bundles have been asked for.  `scales`: the lane's row from super-block `start` on.  The
 // loop's loads are unconditional, the last super-blocks a copy of the code of their own: a branch around a load would make every wait
 // assume the fewest of them.
 template <int BITS, int T, int D>
-__device__ __forceinline__ void run_units(Bundle<BITS, T> (&b)[D], const Matrix (&m)[2], int u, int end, LookUp<BITS>& l, const uint32_t* scales,
+__device__ __forceinline__ void run_units(Bundle<BITS, T> (&b)[D], const Matrix (&m)[2], int u, int end, LookUp<BITS>& l, const uint32_t* scales, int start,
                                           const Tokens& tokens, int lane, f32x4_t (&acc)[2]) {
-    const auto multiply_at = [&](int slot, int unit) { multiply_bundle<BITS, T>(b[slot], l, scales + unit * (Granule<BITS>::BLOCKS / 2), tokens, unit, acc); };
+    const auto multiply_at = [&](int slot, int unit) { multiply_bundle<BITS, T>(b[slot], l, scales + (unit - start) * (Granule<BITS>::BLOCKS / 2), tokens, unit, acc); };
     for (; u + 2 * D <= end; u += D) {
 #pragma unroll
         for (int p = 0; p < D; ++p) {
@@ -501,7 +501,7 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
         f32x4_t acc[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
         for (;;) {
             const int lane = lane_kept();
-            run_units<BITS, T, D>(b, m, u, end, l, &sm.scales[team][0][(lane & 15) * (words | 1) - piece * kPieceWords], tokens, lane, acc);
+            run_units<BITS, T, D>(b, m, u, end, l, &sm.scales[team][0][(lane & 15) * (words | 1)], piece * (kPiece / G::COLUMNS), tokens, lane, acc);
             if ((piece + 1) * kPiece >= columns) break;
             ++piece;
             ask_piece();

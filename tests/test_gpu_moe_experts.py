@@ -46,9 +46,9 @@ def test_rows(layers, bits, rows):
 
 
 @pytest.mark.parametrize("bits", (1, 2, 3, 4))
-@pytest.mark.parametrize("hidden,width", ((1, 1), (1, 5), (3, 1), (9, 2), (2, 17), (5, 7)))
+@pytest.mark.parametrize("hidden,width", ((1, 1), (1, 5), (3, 1), (9, 2), (2, 17), (5, 7), (33, 1), (1, 33), (17, 2)))
 def test_sizes(layers, bits, hidden, width):
-    """In whole super-blocks: fewer of them than waves, and numbers that do not share evenly."""
+    """In whole super-blocks: fewer of them than waves, numbers that do not share evenly, rows of more than one piece of scales."""
     if bits == 1 and hidden * width > 30:
         pytest.skip("the others cover it")
     e, w = layers(3, hidden * UNIT[bits], width * UNIT[bits], bits)
@@ -68,6 +68,36 @@ def test_numbers_of_experts(layers, bits, experts, top_k, rows):
     x, res = tokens(g, rows, 256), tokens(g, rows, 256)
     mine = range(0, rows, max(1, rows // 12))
     check_experts(e, run_experts(w, x, ids, gates, res), x, ids, gates, res, f"{experts} experts, {rows} rows", mine)
+
+
+@pytest.mark.parametrize("bits", (1, 2, 3, 4))
+@pytest.mark.parametrize("rows,top_k", ((16, 8), (9, 16), (16, 16), (5, 13)))
+def test_many_short_rows(layers, bits, rows, top_k):
+    """More row blocks than run at once; experts with 4, 8 and 16 tokens and more at a time."""
+    e, w = layers(128, 512, 512, bits)
+    g = np.random.default_rng(rows * top_k)
+    ids, gates = choices(g, rows, 128, top_k)
+    ids[:, 0] = 77                                                               # one expert that all tokens have
+    ids[1:, 1:][ids[1:, 1:] == 77] = 5
+    x = tokens(g, rows, 512)
+    got = run_experts(w, x, ids, gates)
+    check_experts(e, got, x, ids, gates, None, f"{rows} rows", range(0, rows, 3))
+
+
+def test_most_of_everything():
+    """128 rows of 16 of 1024 experts: the longest list there is."""
+    e = Experts(91, 4, 256, 128, 4)
+    one = e.on_device()
+    of = np.random.default_rng(1).integers(0, 4, 1024)                           # 1024 experts that are four
+    pick = torch.from_numpy(of).cuda()
+    w = kmq.MoeWeights(*(t[pick].contiguous() for t in one.tensors), 1024, 256, 128, 4)
+    g = np.random.default_rng(2)
+    ids, gates = choices(g, 128, 1024, 16)
+    x, res = tokens(g, 128, 256), tokens(g, 128, 256)
+    got = run_experts(w, x, ids, gates, res)
+    check_experts(e, got, x, of[ids].astype(np.int32), gates, res, "", range(0, 128, 9))
+    all_same = np.tile(np.arange(0, 1024, 64, dtype=np.int32), (128, 1))
+    check_experts(e, run_experts(w, x, all_same, gates), x, of[all_same].astype(np.int32), gates, None, "", range(0, 128, 9))
 
 
 @pytest.mark.parametrize("bits", (1, 2, 3, 4))
