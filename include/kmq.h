@@ -464,7 +464,8 @@ typedef struct kmq_block_join {
     int32_t post_norm, gate_sigmoid;
 } kmq_block_join;
 
-/* The block's output x (rows of H = width elements, a multiple of 8 up to 32768) joined, in one launch.  out or normed may be NULL, not both.
+/* The block's output x (rows of H = width elements, a multiple of 8 up to 32768; at most 2^24 rows, rows * width <= 2^34) joined, in one launch.
+ * out or normed may be NULL, not both.
  * out may be x's or the residual's own place, normed x's (same strides). */
 kmq_status kmq_block_norm(const uint16_t* x, int64_t x_stride, int64_t rows, int64_t width, const kmq_block_join* join,
                           uint16_t* out, int64_t out_stride, uint16_t* normed, int64_t normed_stride, void* hip_stream);

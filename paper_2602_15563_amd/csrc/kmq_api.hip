@@ -263,6 +263,7 @@ static void set_turn(HeadsArgs& a, const kmq_head_turn* t) {
 // ---- norms around a block, mixture of experts ----
 static bool row_of(int64_t stride, int64_t width, int64_t most) { return stride % 8 == 0 && stride >= width && stride <= most; }
 constexpr int64_t kMaxStride = int64_t(1) << 31, kMaxMoeStride = int64_t(1) << 22, kMaxMoeDim = 65536, kMaxNormWidth = 32768;
+constexpr int64_t kMaxNormElements = int64_t(1) << 34;     // (a thread eight or more of them, in whole waves: fewer than 2^32 threads)
 
 static kmq_status check_router(const kmq_moe_router* r) {
     if (!r || !r->weights) return KMQ_ERR_NULL;
@@ -612,7 +613,7 @@ kmq_status kmq_kv_attention(const kmq_kv_cache* cache, const kmq_kv_batch* batch
 kmq_status kmq_block_norm(const uint16_t* x, int64_t x_stride, int64_t rows, int64_t width, const kmq_block_join* join,
                           uint16_t* out, int64_t out_stride, uint16_t* normed, int64_t normed_stride, void* hip_stream) {
     if (!x || !join || (!out && !normed)) return KMQ_ERR_NULL;
-    if (rows < 0 || rows > kmq::kMaxDim || width < 8 || width % 8 || width > kmq::kMaxNormWidth) return KMQ_ERR_SHAPE;
+    if (rows < 0 || rows > kmq::kMaxDim || width < 8 || width % 8 || width > kmq::kMaxNormWidth || rows * width > kmq::kMaxNormElements) return KMQ_ERR_SHAPE;
     if ((join->post_norm != 0 && join->post_norm != 1) || (join->gate_sigmoid != 0 && join->gate_sigmoid != 1) || !(join->eps >= 0.f) ||
         !(join->scale - join->scale == 0.f) || !(join->residual_scale - join->residual_scale == 0.f)) return KMQ_ERR_SHAPE;
     if (!kmq::row_of(x_stride, width, kmq::kMaxStride) || (join->residual && !kmq::row_of(join->residual_stride, width, kmq::kMaxStride)) ||
