@@ -19,6 +19,7 @@
 // whatever the indices are.  2 to 4 bits: a pair of indices (4, 6, 8 bits of a byte of the granule) is an entry of two centroids; at 2 and 3
 // bits it is elements k and k + 4 of a step, and the tokens' elements are brought into that order.  1 bit: four indices, eight bytes.  The
 // index goes into byte 1 of the address by one instruction.
+#include <cstddef>
 #include <type_traits>
 
 #include "kmq_kv.h"
@@ -29,11 +30,12 @@ namespace kmq {
 namespace {
 
 // Bundles a wave has asked for, by their registers: what fits beside the rest without spilling in the loop.  (Three instead of two, spilled: one
-// token, 4 bits 31 -> 57 us, 16 tokens 76 -> 144.)
+// token, 4 bits 31 -> 57 us, 16 tokens 76 -> 144.)  With tokens in shared memory two: sixteen waves a unit ask for enough (three, four: 105, 107 of 105 us at 3 bits, 101,
+// 108 of 98 at 4).
 constexpr int depth(int words) { return words <= 10 ? 3 : 2; }
 // Waves a SIMD that the registers have to leave room for.  (1 bit, few tokens: what is kept over an item and does not fit, 5 to 7 words, is spilled outside the
 // loop; two waves instead 111 -> 132 us, 16 tokens of 128 experts.)
-constexpr int waves_for(int bits, int t) { return (t == 16 && (bits == 2 || bits == 4)) ? 2 : bits == 1 || (bits == 2 && t == 8) || t == 16 ? 3 : 4; }
+constexpr int waves_for(int bits, int t, bool staged) { return staged ? (bits == 1 ? 2 : 4) : (t == 16 && (bits == 2 || bits == 4)) ? 2 : bits == 1 || (bits == 2 && t == 8) || t == 16 ? 3 : 4; }
 
 typedef __amdgpu_buffer_rsrc_t Rows;
 // Rows read by byte offset; kNoRow gives zeros.
@@ -78,11 +80,10 @@ __device__ __forceinline__ void load_granule(const Matrix& m, int unit, int lane
 // A row's length goes by pieces of kPiece columns, whose scales a team keeps in shared memory, [matrix][row][word], rows an odd number of
 // words apart.  They are asked for as they lie, row after row: granule by granule, 4 to 16 bytes of each of 16 rows an instruction, the same
 // lines are asked for from the L2 again and again (a layer of 16 tokens, 128 experts of 4096 x 1536, 4 bits: 218 us, and 204).
-constexpr int kPiece = 4096, kPieceWords = kPiece / 128;
-typedef uint32_t PieceScales[2][16 * (kPieceWords + 1)];
-template <int LANES>
+template <int PIECE> using PieceScales = uint32_t[2][16 * (PIECE / 128 + 1)];
+template <int PIECE, int LANES>
 struct Scales {
-    static constexpr int EACH = 16 * kPieceWords / LANES;
+    static constexpr int EACH = (16 * (PIECE / 128) + LANES - 1) / LANES;
     uint32_t raw[2][EACH];
     // Words first .. first + words - 1 of 16 rows of `row_words`; `lane` of the team's.
     __device__ __forceinline__ void load(const Matrix (&m)[2], int row_words, int first, int words, int lane) {
@@ -96,7 +97,7 @@ struct Scales {
             for (int i = 0; i < 2; ++i) raw[i][k] = m[i].scales[row * row_words + first + at];
         }
     }
-    __device__ __forceinline__ void keep(PieceScales& to, int words, int lane) const {
+    __device__ __forceinline__ void keep(PieceScales<PIECE>& to, int words, int lane) const {
         const uint32_t inverse = 65536u / words + 1, odd = words | 1;
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
@@ -193,15 +194,18 @@ __device__ __forceinline__ f32x4_t step(u32x4_t tokens, u32x4_t weights, f32x4_t
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, tokens), __builtin_bit_cast(bf16x8_t, weights), c, 0, 0, 0);
 }
 
-// What a workgroup finds out about the choices: the pairs' experts (-1: none, or an earlier pair of the token has the same), and the list of
-// what there is to do: T tokens at most of an expert, as often as its tokens need, experts ascending.
+// What a workgroup finds out about the choices: the pairs by their experts, those without one and those whose token has the same expert in an earlier
+// pair left out, and the list of what there is to do: T tokens at most of an expert, as often as its tokens need, experts ascending.
 template <int ROWS, int T>
 struct Choices {
     static constexpr int PAIRS = ROWS * KMQ_MOE_MAX_TOP_K;
     static constexpr int MOST = (PAIRS < KMQ_MOE_MAX_EXPERTS ? PAIRS : KMQ_MOE_MAX_EXPERTS) + PAIRS / T;
-    static_assert(ROWS / T < 64, "six bits");
-    int16_t expert[PAIRS + KMQ_MOE_MAX_TOP_K];
-    uint16_t list[MOST];                                  // expert << 6 | how many times T tokens of it came before
+    static_assert(PAIRS <= 2048 && ROWS <= 128 && ROWS / T <= 8 && KMQ_MOE_MAX_EXPERTS <= 1024, "bits of an entry");
+    union {
+        int16_t expert[PAIRS + KMQ_MOE_MAX_TOP_K];        // of a pair, -1: none
+        uint16_t pairs[PAIRS];                            // an expert's one after the other, ascending: all workgroups cut them alike
+    };
+    uint32_t list[MOST];                                  // expert << 21 | where its pairs begin << 10 | their number less one << 3 | how many times T came before
     int all;                                              // entries of the list
 };
 // The sum over this lane and those below it.
@@ -215,12 +219,40 @@ __device__ __forceinline__ int sum_upto(int v) {
     add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});      // row_bcast31 into rows 2 and 3
     return v;
 }
-// (`counts`: a word an expert, of memory that is not used yet.)
+// Which tokens an expert has, a bit each, gives their number and every pair's place.  (Counted and ranked by ballots over all pairs, expert by expert, when one was
+// needed: 6 us more of 128 tokens.)  The bits stand in memory that is not used yet, with them
+// where the expert's pairs begin.
+template <int ROWS>
+struct Bits {
+    static constexpr int WORDS = (ROWS + 31) / 32, STRIDE = ROWS <= 16 ? 1 : WORDS + 1;
+    static constexpr uint32_t MASK = ROWS <= 16 ? 0xFFFFu : ~0u;
+    uint32_t* word;
+    __device__ __forceinline__ void set(int expert, int token) { atomicOr(&word[expert * STRIDE + (token >> 5)], 1u << (token & 31)); }
+    __device__ __forceinline__ int count(int expert) const {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) n += __popc(word[expert * STRIDE + i]);
+        return n;
+    }
+    __device__ __forceinline__ void begin(int expert, int at) {
+        if constexpr (ROWS <= 16) word[expert] |= static_cast<uint32_t>(at) << 16;
+        else word[expert * STRIDE + WORDS] = at;
+    }
+    __device__ __forceinline__ int place(int expert, int token) const {
+        int n = ROWS <= 16 ? word[expert] >> 16 : word[expert * STRIDE + STRIDE - 1];
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            const int below = token - 32 * i;             // bits of this word that count
+            n += __popc(word[expert * STRIDE + i] & MASK & (below >= 32 ? ~0u : below > 0 ? (1u << below) - 1u : 0u));
+        }
+        return n;
+    }
+};
 template <int ROWS, int T, int THREADS>
-__device__ __forceinline__ void find_choices(const MoeArgs& a, Choices<ROWS, T>& p, int* counts) {
+__device__ __forceinline__ void find_choices(const MoeArgs& a, Choices<ROWS, T>& p, Bits<ROWS> bits) {
     constexpr int EACH = (Choices<ROWS, T>::PAIRS + THREADS - 1) / THREADS;
     const int pairs = a.rows * a.top_k, tid = threadIdx.x;
-    int e[EACH];
+    int e[EACH], token[EACH];
 #pragma unroll
     for (int t = 0; t < EACH; ++t) {
         const int i = tid + t * THREADS;
@@ -228,69 +260,50 @@ __device__ __forceinline__ void find_choices(const MoeArgs& a, Choices<ROWS, T>&
         if (e[t] < 0 || e[t] >= a.experts) e[t] = -1;
         if (i < pairs) p.expert[i] = static_cast<int16_t>(e[t]);
     }
-    for (int i = tid; i < a.experts; i += THREADS) counts[i] = 0;
+    for (int i = tid; i < a.experts * Bits<ROWS>::STRIDE; i += THREADS) bits.word[i] = 0;
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < EACH; ++t) {
         const int i = tid + t * THREADS;
         if (i >= pairs) continue;
-        const int slot = i % a.top_k;
+        token[t] = i / a.top_k;
+        const int slot = i - token[t] * a.top_k;
         bool again = false;
 #pragma unroll
         for (int j = 0; j < KMQ_MOE_MAX_TOP_K - 1; ++j) again |= (j < slot) & (p.expert[i - slot + j] == e[t]);      // (there is room behind the last pair)
         if (again) e[t] = -1;
-        if (e[t] >= 0) atomicAdd(&counts[e[t]], 1);
+        if (e[t] >= 0) bits.set(e[t], token[t]);
+    }
+    __syncthreads();
+    if (tid < kWave) {                                    // experts lane * some .. lane * some + some - 1
+        const int some = (a.experts + kWave - 1) / kWave, first = tid * some, end = min(first + some, a.experts);
+        int sum = 0;                                      // pairs << 16 | times
+        for (int i = first; i < end; ++i) sum += bits.count(i) << 16 | (bits.count(i) + T - 1) / T;
+        const int upto = sum_upto(sum);
+        if (tid == kWave - 1) p.all = upto & 0xFFFF;
+        int at = (upto - sum) & 0xFFFF, begin = (upto - sum) >> 16;
+        for (int i = first; i < end; ++i) {
+            const int count = bits.count(i);
+            for (int k = 0; k * T < count; ++k) p.list[at++] = static_cast<uint32_t>(i << 21 | begin << 10 | (count - 1) << 3 | k);
+            bits.begin(i, begin);
+            begin += count;
+        }
     }
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < EACH; ++t) {
-        const int i = tid + t * THREADS;
-        if (i < pairs) p.expert[i] = static_cast<int16_t>(e[t]);
-    }
-    if (tid < kWave) {                                    // experts lane * some .. lane * some + some - 1
-        const int some = (a.experts + kWave - 1) / kWave, first = tid * some, end = min(first + some, a.experts);
-        int times = 0;
-        for (int i = first; i < end; ++i) times += (counts[i] + T - 1) / T;
-        int at = sum_upto(times);
-        if (tid == kWave - 1) p.all = at;
-        at -= times;
-        for (int i = first; i < end; ++i)
-            for (int k = 0; k * T < counts[i]; ++k) p.list[at++] = static_cast<uint16_t>(i << 6 | k);
-    }
+    for (int t = 0; t < EACH; ++t)
+        if (e[t] >= 0) p.pairs[bits.place(e[t], token[t])] = static_cast<uint16_t>(tid + t * THREADS);
     __syncthreads();
-}
-
-template <int ROWS, int T>
-__device__ __forceinline__ int count_of(const Choices<ROWS, T>& p, int pairs, int expert) {
-    int count = 0;
-    for (int i = threadIdx.x & 63; i < (pairs + 63) / 64 * 64; i += 64) count += __popcll(__ballot(i < pairs && p.expert[i] == expert));
-    return __builtin_amdgcn_readfirstlane(count);
-}
-// The pairs of an expert, in their order: lane l < 16 gets the (first + l)-th.
-template <int ROWS, int T>
-__device__ __forceinline__ int pairs_of(const Choices<ROWS, T>& p, int pairs, int expert, int first) {
-    const int lane = threadIdx.x & 63;
-    int mine = 0, count = 0;
-    for (int i = lane; i < (pairs + 63) / 64 * 64; i += 64) {
-        const bool has = i < pairs && p.expert[i] == expert;
-        const uint64_t all = __ballot(has);
-        const int to = count + __popcll(all & ((uint64_t(1) << lane) - 1)) - first;
-        // what is sent to a lane is one more than the pair: 0 comes where nothing is sent (lane 63 takes what nobody asks for: 16 are looked at)
-        const int got = __builtin_amdgcn_ds_permute((has && to >= 0 && to < 16 ? to : 63) * 4, has ? i + 1 : 0);
-        if (lane < 16 && got) mine = got - 1;
-        count += __popcll(all);
-    }
-    return mine;
 }
 
 // What a wave asks for at a time: a super-block of two matrices, and the elements under it of T tokens of the expert.  Fewer than 16 tokens
 // leave most lanes of the operand without one, so 16 / T steps' operands come with one load: lane n takes token n % T at step n / T, and a
 // rotation inside 16 lanes brings it to where the step wants it.  (What the other lanes hold then are columns that nobody reads.)
 // T = 16 at 1 bit would take 64 registers: there the elements are read when they are needed.
-template <int BITS, int T>
+template <int BITS, int T, bool STAGED>
 struct Bundle {
     static constexpr int LOADS = T / 4;                   // of tokens, for four steps
-    static constexpr bool TOKENS = BITS > 1 || T < 16;
+    static constexpr bool TOKENS = !STAGED && (BITS > 1 || T < 16);
     static constexpr int WORDS = 2 * Granule<BITS>::WORDS + (TOKENS ? LOADS * Granule<BITS>::STEPS : 0);
     Granule<BITS> g[2];
     u32x4_t x[TOKENS ? Granule<BITS>::STEPS / 4 : 1][LOADS];
@@ -298,18 +311,19 @@ struct Bundle {
 struct Tokens {
     Rows rows;
     uint32_t at;                                          // where the lane's token begins
+    const u32x4_t* staged;                                // operands in shared memory, 64 lanes a step
 };
 template <int T>
 __device__ __forceinline__ void load_tokens(const Tokens& tokens, uint32_t column, u32x4_t (&x)[T / 4]) {
 #pragma unroll
     for (int l = 0; l < T / 4; ++l) x[l] = load_row16(tokens.rows, tokens.at + l * (1024 / T), column * 2);
 }
-template <int BITS, int T>
-__device__ __forceinline__ void load_bundle(const Matrix (&m)[2], int unit, const Tokens& tokens, int lane, Bundle<BITS, T>& b) {
+template <int BITS, int T, bool STAGED>
+__device__ __forceinline__ void load_bundle(const Matrix (&m)[2], int unit, const Tokens& tokens, int lane, Bundle<BITS, T, STAGED>& b) {
     using G = Granule<BITS>;
 #pragma unroll
     for (int i = 0; i < 2; ++i) load_granule<BITS>(m[i], unit, lane, b.g[i]);
-    if constexpr (Bundle<BITS, T>::TOKENS) {
+    if constexpr (Bundle<BITS, T, STAGED>::TOKENS) {
 #pragma unroll
         for (int k = 0; k < G::STEPS / 4; ++k) load_tokens<T>(tokens, unit * G::COLUMNS + 128 * k, b.x[k]);
     }
@@ -337,28 +351,31 @@ __device__ __forceinline__ u32x4_t operand(const u32x4_t (&x)[T / 4], int j) {
         default: return x[j * T / 16];
     }
 }
-// One bundle's products, added to acc; `scales`: the lane's row from the super-block on.
-template <int BITS, int T>
-__device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T>& b, LookUp<BITS>& l, const uint32_t* scales, const Tokens& tokens, int unit,
-                                                f32x4_t (&acc)[2]) {
+// One bundle's products, added to acc; `scales`: the lane's row from the super-block on, `staged`: the operands from it on.
+template <int BITS, int T, bool STAGED, int PIECE>
+__device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T, STAGED>& b, LookUp<BITS>& l, const uint32_t* scales, const u32x4_t* staged, const Tokens& tokens,
+                                                int unit, int lane, f32x4_t (&acc)[2]) {
     using G = Granule<BITS>;
-    using B = Bundle<BITS, T>;
+    using B = Bundle<BITS, T, STAGED>;
 #pragma unroll
     for (int k = 0; k < G::STEPS / 4; ++k) {
         u32x4_t x[B::LOADS];
-        if constexpr (B::TOKENS) {
+        if constexpr (STAGED) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = staged[(4 * k + i) * kWave + lane];
+        } else if constexpr (B::TOKENS) {
 #pragma unroll
             for (int i = 0; i < B::LOADS; ++i) x[i] = b.x[k][i];
         } else {
             load_tokens<T>(tokens, unit * G::COLUMNS + 128 * k, x);
         }
-        if constexpr (BITS == 2 || BITS == 3) {
+        if constexpr (!STAGED && (BITS == 2 || BITS == 3)) {
 #pragma unroll
             for (int i = 0; i < B::LOADS; ++i) x[i] = pairs_apart(x[i]);
         }
         uint32_t both[2];                                 // the scales of two blocks
 #pragma unroll
-        for (int i = 0; i < 2; ++i) both[i] = scales[i * sizeof(PieceScales) / 8 + k];
+        for (int i = 0; i < 2; ++i) both[i] = scales[i * sizeof(PieceScales<PIECE>) / 8 + k];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int block = 2 * k + half;
@@ -379,22 +396,25 @@ __device__ __forceinline__ void multiply_bundle(const Bundle<BITS, T>& b, LookUp
 // The sums over super-blocks u .. end - 1; the first D bundles have been asked for.  `scales`: the lane's row from super-block `start` on.  The
 // loop's loads are unconditional, the last super-blocks a copy of the code of their own: a branch around a load would make every wait
 // assume the fewest of them.
-template <int BITS, int T, int D>
-__device__ __forceinline__ void run_units(Bundle<BITS, T> (&b)[D], const Matrix (&m)[2], int u, int end, LookUp<BITS>& l, const uint32_t* scales, int start,
+template <int BITS, int T, bool STAGED, int PIECE, int D>
+__device__ __forceinline__ void run_units(Bundle<BITS, T, STAGED> (&b)[D], const Matrix (&m)[2], int u, int end, LookUp<BITS>& l, const uint32_t* scales, int start,
                                           const Tokens& tokens, int lane, f32x4_t (&acc)[2]) {
-    const auto multiply_at = [&](int slot, int unit) { multiply_bundle<BITS, T>(b[slot], l, scales + (unit - start) * (Granule<BITS>::BLOCKS / 2), tokens, unit, acc); };
+    using G = Granule<BITS>;
+    const auto multiply_at = [&](int slot, int unit) {
+        multiply_bundle<BITS, T, STAGED, PIECE>(b[slot], l, scales + (unit - start) * (G::BLOCKS / 2), tokens.staged + (unit - start) * (G::STEPS * kWave), tokens, unit, lane, acc);
+    };
     for (; u + 2 * D <= end; u += D) {
 #pragma unroll
         for (int p = 0; p < D; ++p) {
             multiply_at(p, u + p);
-            load_bundle<BITS, T>(m, u + p + D, tokens, lane, b[p]);
+            load_bundle<BITS, T, STAGED>(m, u + p + D, tokens, lane, b[p]);
         }
     }
 #pragma unroll
     for (int p = 0; p < D; ++p) {
         if (u + p >= end) return;
         multiply_at(p, u + p);
-        if (u + p + D < end) load_bundle<BITS, T>(m, u + p + D, tokens, lane, b[p]);
+        if (u + p + D < end) load_bundle<BITS, T, STAGED>(m, u + p + D, tokens, lane, b[p]);
     }
 #pragma unroll
     for (int p = 0; p < D - 1; ++p) {
@@ -409,28 +429,53 @@ __device__ __forceinline__ int anew(int v) {
     return v;
 }
 
+// More tokens than a wave's 16 at once stand as operands in shared memory, a piece of the columns at a time.
+constexpr bool staged(int rows) { return rows > 16; }
+constexpr int piece_columns(int bits, int rows) { return !staged(rows) ? 4096 : bits == 4 ? 1024 : 2048; }
+
 template <int BITS, int T, int ROWS, int NW, int TEAMS>
 struct Shared {
+    static constexpr bool STAGED = staged(ROWS);
+    static constexpr int PIECE = piece_columns(BITS, ROWS);
     Tables<BITS> tables;
+    u32x4_t tokens[STAGED ? PIECE / 32 * kWave : 1];
     f32x4_t part[TEAMS][NW > 1 ? NW - 1 : 1][2][NW > 1 ? 4 * T : 1];      // sums of a team's waves but the first
-    PieceScales scales[TEAMS];
+    PieceScales<PIECE> scales[TEAMS];
     Choices<ROWS, T> choices;
+};
+// The operands of a piece on their way into shared memory, step by step, the workgroup's waves in turn.
+template <int BITS, int PIECE, int WAVES>
+struct Stage {
+    static constexpr int EACH = PIECE ? PIECE / 32 / WAVES : 1;
+    u32x4_t raw[EACH];
+    __device__ __forceinline__ void load(const Tokens& tokens, int first, int steps, int wave) {
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+            if (wave + k * WAVES < steps) raw[k] = load_row16(tokens.rows, tokens.at, (first + wave + k * WAVES) * 64);
+    }
+    __device__ __forceinline__ void keep(u32x4_t* to, int steps, int wave, int lane) const {
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+            if (wave + k * WAVES < steps) to[(wave + k * WAVES) * kWave + lane] = BITS == 2 || BITS == 3 ? pairs_apart(raw[k]) : raw[k];
+    }
 };
 
 // A workgroup of TEAMS teams of NW waves; T tokens at a time.  GATED: rows of gate and up, else pairs of row blocks of down.
 template <int BITS, int T, int ROWS, int NW, int TEAMS, bool GATED>
-__global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per_eu(waves_for(BITS, T)))) void moe_rows_kernel(MoeArgs a) {
+__global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per_eu(waves_for(BITS, T, staged(ROWS))))) void moe_rows_kernel(MoeArgs a) {
     using G = Granule<BITS>;
-    constexpr int D = depth(Bundle<BITS, T>::WORDS), LANES = 4 * T;
-    __shared__ Shared<BITS, T, ROWS, NW, TEAMS> sm;
+    using Sm = Shared<BITS, T, ROWS, NW, TEAMS>;
+    constexpr bool STAGED = Sm::STAGED;
+    constexpr int PIECE = Sm::PIECE, D = STAGED ? 2 : depth(Bundle<BITS, T, STAGED>::WORDS), LANES = 4 * T;
+    __shared__ Sm sm;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave / NW, member = wave % NW;
     const auto lane_anew = [] { return anew(static_cast<int>(threadIdx.x)) & 63; };
     const int kept = threadIdx.x & 63;
     // (at 1 bit there is no register to keep it in: 122 -> 111 us, 16 tokens of 128 experts; elsewhere 2 to 6 % more)
     const auto lane_kept = [&] { return BITS == 1 ? lane_anew() : kept; };
     const auto place = [&] { return member * kWave + lane_anew(); };        // in the team
-    static_assert(sizeof(sm.tables) >= sizeof(int) * KMQ_MOE_MAX_EXPERTS, "counts");
-    find_choices<ROWS, T, NW * TEAMS * kWave>(a, sm.choices, reinterpret_cast<int*>(&sm.tables));
+    static_assert(offsetof(Sm, choices) >= sizeof(uint32_t) * Bits<ROWS>::STRIDE * KMQ_MOE_MAX_EXPERTS, "bits");      // (what lies before is filled later)
+    find_choices<ROWS, T, NW * TEAMS * kWave>(a, sm.choices, Bits<ROWS>{reinterpret_cast<uint32_t*>(&sm)});
     const int columns = static_cast<int>(GATED ? a.hidden : a.width), units = columns / G::COLUMNS, pairs = a.rows * a.top_k;
     const int per_expert = static_cast<int>(GATED ? a.width >> 4 : a.hidden >> 5) / TEAMS;
     const unsigned items = static_cast<unsigned>(sm.choices.all) * per_expert, each = items / gridDim.x, over = items - each * gridDim.x;
@@ -441,20 +486,23 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
     const uint32_t stride = static_cast<uint32_t>(GATED ? a.x_stride : a.width) * 2u;
     Tokens tokens;
     tokens.rows = rows_at(GATED ? static_cast<const void*>(a.x) : h);
-    Bundle<BITS, T> b[D];
-    Scales<NW * kWave> scales;
+    tokens.staged = sm.tokens;
+    Bundle<BITS, T, STAGED> b[D];
+    Scales<PIECE, NW * kWave> scales;
+    Stage<BITS, STAGED ? PIECE : 0, NW * TEAMS> stage;
     Matrix m[2];
     LookUp<BITS> l(sm.tables, lane_kept());
-    // where the workgroup is: the `group`-th row blocks of expert e, of whose `count` pairs those from `time` * T on (`times` in all), a piece
+    // where the workgroup is: the `group`-th row blocks of expert e, of whose `count` pairs (from `begin` on) those from `time` * T on (`times` in all), a piece
     // of the columns, of which super-blocks u .. end - 1 are this wave's; this lane's pair.  An expert's items lie by row blocks first, so that
     // all its tokens meet these while they are in the L2; `entry` is the list's first of the next expert.
-    int entry = from / per_expert, group, e, time, times, count, piece = 0, u, end, words, pair;
+    int entry = from / per_expert, group, e, time, times, count, begin, piece = 0, u, end, words, pair;
     const auto find_expert = [&](int at) {
-        const int found = __builtin_amdgcn_readfirstlane(sm.choices.list[at]);
-        e = found >> 6;
-        count = count_of(sm.choices, pairs, e);
+        const uint32_t found = __builtin_amdgcn_readfirstlane(sm.choices.list[at]);
+        e = found >> 21;
+        begin = found >> 10 & 0x7FF;
+        count = (found >> 3 & 0x7F) + 1;
         times = (count + T - 1) / T;
-        entry = at - (found & 63) + times;
+        entry = at - (found & 7) + times;
     };
     find_expert(entry);
     {
@@ -463,16 +511,21 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
         time = within - group * times;
     }
     uint32_t centroids = 0;
-    const auto ask_piece = [&] {
-        constexpr int MOST = kPiece / G::COLUMNS;
+    int steps = 0;                                        // to be staged
+    const auto ask_piece = [&](bool tokens_too) {
+        constexpr int MOST = PIECE / G::COLUMNS;
         const int start = piece * MOST, some = units - start < MOST ? units - start : MOST;
         words = some * (G::BLOCKS / 2);
         u = start + some * member / NW;
         end = start + some * (member + 1) / NW;
-        scales.load(m, columns / 128, piece * kPieceWords, words, place());
+        scales.load(m, columns / 128, piece * (PIECE / 128), words, place());
+        if constexpr (STAGED) {
+            steps = tokens_too ? some * G::STEPS : 0;
+            stage.load(tokens, start * G::STEPS, steps, wave);
+        }
 #pragma unroll
         for (int p = 0; p < D; ++p)
-            if (u + p < end) load_bundle<BITS, T>(m, u + p, tokens, lane_kept(), b[p]);
+            if (u + p < end) load_bundle<BITS, T, STAGED>(m, u + p, tokens, lane_kept(), b[p]);
     };
     const auto ask = [&](bool other, bool tokens_too) {
         if (other) {                                      // (before the bundles: what is waited for first is asked for first)
@@ -485,28 +538,33 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
         m[1] = matrix_of<BITS>(GATED ? a.up : a.down, e, GATED ? block : 2 * block + 1, units);
         if (tokens_too) {
             const int lane = lane_anew(), n = lane & 15, q = lane >> 4;
-            pair = pairs_of(sm.choices, pairs, e, time * T);
-            const int i = n % T, p = __shfl(pair, i);
+            const int i = n % T, from = begin + time * T;
+            pair = n < count - time * T ? sm.choices.pairs[from + n] : 0;
+            const int p = __shfl(pair, i);
             tokens.at = kNoRow;
             if (time * T + i < count) tokens.at = static_cast<uint32_t>(GATED ? p / a.top_k : p) * stride + 16u * q + n / T * 64u;
         }
         piece = 0;
-        ask_piece();
+        ask_piece(tokens_too || columns > PIECE);
+    };
+    const auto keep = [&] {
+        scales.keep(sm.scales[team], words, place());
+        if constexpr (STAGED) stage.keep(sm.tokens, steps, wave, lane_anew());
     };
     ask(true, true);
-    scales.keep(sm.scales[team], words, place());
+    keep();
     fill_tables<BITS>(sm.tables, centroids, wave, NW * TEAMS, lane_anew());
     __syncthreads();
     for (int item = from;;) {
         f32x4_t acc[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
         for (;;) {
             const int lane = lane_kept();
-            run_units<BITS, T, D>(b, m, u, end, l, &sm.scales[team][0][(lane & 15) * (words | 1)], piece * (kPiece / G::COLUMNS), tokens, lane, acc);
-            if ((piece + 1) * kPiece >= columns) break;
+            run_units<BITS, T, STAGED, PIECE, D>(b, m, u, end, l, &sm.scales[team][0][(lane & 15) * (words | 1)], piece * (PIECE / G::COLUMNS), tokens, lane, acc);
+            if ((piece + 1) * PIECE >= columns) break;
             ++piece;
-            ask_piece();
+            ask_piece(true);
             __syncthreads();
-            scales.keep(sm.scales[team], words, place());
+            keep();
             __syncthreads();
         }
         // what comes next is asked for before the sums are joined
@@ -553,7 +611,7 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
             }
         }
         if (!more) break;
-        scales.keep(sm.scales[team], words, place());       // (every wave has been past a barrier since it read the last ones)
+        keep();                                           // (every wave has been past a barrier since it read the last ones)
         if (other) fill_tables<BITS>(sm.tables, centroids, wave, NW * TEAMS, lane_anew());
         __syncthreads();
     }
@@ -600,7 +658,7 @@ size_t moe_workspace_bytes(int64_t rows, int64_t top_k, int64_t width, int64_t h
 
 template <int BITS, int T, int ROWS, int NW, int WAVES, bool GATED>
 static void launch_rows(const MoeArgs& a, hipStream_t s) {
-    constexpr int TEAMS = WAVES / NW, BY_WAVES = 4 * waves_for(BITS, T) / WAVES, BY_MEMORY = 160 * 1024 / sizeof(Shared<BITS, T, ROWS, NW, TEAMS>);
+    constexpr int TEAMS = WAVES / NW, BY_WAVES = 4 * waves_for(BITS, T, staged(ROWS)) / WAVES, BY_MEMORY = 160 * 1024 / sizeof(Shared<BITS, T, ROWS, NW, TEAMS>);
     static_assert(8 % TEAMS == 0, "row blocks come in eights");
     constexpr int64_t MOST = 256 * (BY_WAVES < BY_MEMORY ? BY_WAVES : BY_MEMORY);          // as many as run at once
     const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = pairs < a.experts ? pairs : a.experts;
@@ -622,8 +680,10 @@ static void launch_few(const MoeArgs& a, hipStream_t s) {
 
 // Tokens at a time: where more of them choose an expert its rows are read again (from the L2, mostly), and every four more cost registers and loads.
 // us with 4 / 8 at a time: 16 tokens of 128 experts, 8 each, 4 bits 64 / 66, a layer of them 177 / 183; 5 tokens of 8 experts, 2 each, 2 bits 103 / 127;
-// but 16 tokens of 64 experts, 8 each, 3 bits 126 / 119.  More than 16 tokens take 16 at a time (32: 128 tokens of 64 experts, 6 each, 3 bits 137 -> 171), a wave a whole
-// row and as many of them a workgroup as the memory holds, so that neighbours find the tokens' elements in the L1 (four / two / one wave a row: 339 / 249 / 222).
+// but 16 tokens of 64 experts, 8 each, 3 bits 126 / 119.  More than 16 tokens take 16 at a time (32: 128 tokens of 64 experts, 6 each, 3 bits 137 -> 171), which eight
+// teams of two waves share in shared memory (every wave for itself from the caches: 122 -> 105; 64 tokens, 4 bits 130 -> 98; 100 tokens, 2 bits 131 -> 86).  Four
+// teams of four take 120, eight of one 119; 1 bit needs the registers of eight waves (40 tokens of 128 experts 205 -> 180; as sixteen, spilled, 250).  For 16 rows
+// and fewer it does not pay (16 tokens of 8 experts of 4096 x 14336, 4 bits 170 -> 190).
 template <int BITS, bool GATED>
 static void launch_product(const MoeArgs& a, hipStream_t s) {
     const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = a.experts;
@@ -638,12 +698,12 @@ static void launch_product(const MoeArgs& a, hipStream_t s) {
         }
     }
     if (a.rows <= 16) launch_rows<BITS, 16, 16, 2, 4, GATED>(a, s);
-    else if constexpr (BITS == 4) {
-        // (eight teams need row blocks in sixteens: the down projection's pairs of them come in fours)
-        if (GATED || a.hidden % 256 == 0) launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, 1, 8, GATED>(a, s);
-        else launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, 2, 8, GATED>(a, s);
+    // (eight teams need row blocks in sixteens: the down projection's pairs of them come in fours)
+    else {
+        constexpr int WAVES = BITS == 1 ? 8 : 16;
+        if (GATED || a.hidden % 256 == 0) launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, WAVES / 8, WAVES, GATED>(a, s);
+        else launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, WAVES / 4, WAVES, GATED>(a, s);
     }
-    else launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, 1, 4, GATED>(a, s);
 }
 
 template <int BITS>

@@ -484,10 +484,16 @@ def moe_route_workspace_bytes(rows: int, experts: int, width: int) -> int:
     return int(_lib.kmq_moe_route_workspace_bytes(rows, experts, width))
 
 
-def _check_choices(ids, gates, rows: int, top_k: int):
-    if ids.element_size() != 4 or ids.is_floating_point() or gates.element_size() != 4 or not gates.is_floating_point():
-        raise KmqError(3)
-    if ids.numel() < rows * top_k or gates.numel() < rows * top_k or not (ids.is_contiguous() and gates.is_contiguous()):
+_choice_types = None
+
+
+def _check_choices(ids, gates):
+    """(64-bit ids, as they come from torch.topk, would be read as twice as many.)"""
+    global _choice_types
+    if _choice_types is None:
+        import torch
+        _choice_types = (torch.int32, torch.float32)
+    if ids.dtype is not _choice_types[0] or gates.dtype is not _choice_types[1]:
         raise KmqError(3)
 
 
@@ -495,7 +501,7 @@ def moe_route(x, x_stride: int, rows: int, router, experts: int, width: int, ids
               top_groups: int = 1, normalise: bool = True, scale: float = 1.0, workspace=None):
     """Experts of every row of x (ids int32, gates fp32; rows x top_k) by a router of experts x width bf16, on torch's current stream.
     workspace: moe_route_workspace_bytes() device bytes."""
-    _check_choices(ids, gates, rows, top_k)
+    _check_choices(ids, gates)
     r = _RouterStruct(_ptr(router), _ptr(bias), width, experts, top_k, groups, top_groups, 1 if sigmoid else 0, 1 if normalise else 0, scale)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(_lib.kmq_moe_route(_ptr(x), x_stride, rows, ctypes.addressof(r), _ptr(ids), _ptr(gates), _ptr(workspace), ws_bytes, _stream()))
@@ -532,7 +538,7 @@ def moe_experts(weights: MoeWeights, x, x_stride: int, rows: int, ids, gates, to
                 workspace=None):
     """y = residual + sum over a row's top_k experts of gate * down(silu(gate x) * up x), for up to MOE_MAX_ROWS rows, on torch's current
     stream.  workspace: moe_experts_workspace_bytes() device bytes."""
-    _check_choices(ids, gates, rows, top_k)
+    _check_choices(ids, gates)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(_lib.kmq_moe_experts(weights._at, _ptr(x), x_stride, rows, _ptr(ids), _ptr(gates), top_k, _ptr(residual), residual_stride, _ptr(y), y_stride,
                                 _ptr(workspace), ws_bytes, _stream()))

@@ -110,6 +110,20 @@ def test_all_tokens_choose_the_same(layers, bits, rows):
     check_experts(e, run_experts(w, x, ids, gates), x, ids, gates, None, f"{rows} rows", range(0, rows, 7))
 
 
+@pytest.mark.parametrize("bits,hidden,width", ((1, 9, 10), (2, 17, 9), (3, 17, 34), (4, 18, 9)))
+def test_more_tokens_than_sixteen_over_several_pieces(layers, bits, hidden, width):
+    """Experts with up to three times 16 tokens, rows of several pieces, calls that agree bit for bit."""
+    e, w = layers(3, hidden * UNIT[bits], width * UNIT[bits], bits)
+    g = np.random.default_rng(bits)
+    ids, gates = choices(g, 40, 3, 2)
+    ids[:, 0], ids[:, 1] = 1, np.where(np.arange(40) % 3 == 0, 2, 0)
+    x, res = tokens(g, 40, e.hidden), tokens(g, 40, e.hidden)
+    got = run_experts(w, x, ids, gates, res)
+    check_experts(e, got, x, ids, gates, res, f"{e.hidden} x {e.width}", range(0, 40, 5))
+    for _ in range(3):
+        assert np.array_equal(run_experts(w, x, ids, gates, res), got)
+
+
 @pytest.mark.parametrize("rows", (1, 9, 40))
 def test_ids_that_are_none_and_experts_chosen_twice(layers, rows):
     e, w = layers(12, 512, 512, 3)
