@@ -12,7 +12,11 @@
 // tokens, the gate's and the up projection's, or two blocks of the down projection.  NW waves (a team) split the rows' length, their
 // sums are added in shared memory; the teams of a workgroup share the table of the expert's centroids.  A workgroup takes neighbouring
 // rows of the list of all experts' rows, as many as any other; the first super-blocks of what comes next are asked for before the
-// sums are joined.
+// sums are joined.  Above 16 rows the 16 tokens of an item stand in shared memory as operands, for all of the workgroup's waves.
+//
+// What bounds it: 4 bits, 16 tokens of 128 experts of 4096 x 1536, the memory (90 + 57 us, 4.9 TB/s); 2 bits, five tokens of 8 experts of 4096 x 14336, the decode
+// (62 + 37 us, of which vector issue 32 + 15, look-ups as much); one token, 6 to 8 experts, latencies (15 + 10 us, 6 before the first products in each).
+//
 // Block scales: two matrix steps are a block of 64 columns; their sum from zero is multiplied by the block's scale.
 //
 // Decode: tables in shared memory whose entries are ready operand registers, a column a lane modulo 32, so that look-ups never collide
