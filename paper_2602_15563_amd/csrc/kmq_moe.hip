@@ -673,11 +673,18 @@ static void launch_rows(const MoeArgs& a, hipStream_t s) {
 
 // Waves that split a row: four, or two where rows are short (fewer than 16 super-blocks) and there are enough of them (16 tokens of 128 experts of
 // 4096 x 1536, 1 bit: 166 us with four, 147 with two; 3 bits 120 and 107).  At 4 bits eight waves share the table, 64 KB, and two of them a row are slower
-// throughout (2048 x 768, 16 tokens: 66 with four, 75).
+// throughout (2048 x 768, 16 tokens: 66 with four, 75).  Eight where few long rows would leave units without work (one token: an expert of 2176 x 15744, 3 bits
+// 43 -> 35.5; two of 4096 x 14336, 4 bits 60 -> 53; up to 1024 items instead: two of 7040 x 8576, 4 bits 59 -> 57, but four of 3840 x 8704, 3 bits 63 -> 66).
 template <int BITS, int T, bool GATED>
 static void launch_few(const MoeArgs& a, hipStream_t s) {
     const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = pairs < a.experts ? pairs : a.experts;
-    [[maybe_unused]] const int64_t units = (GATED ? a.hidden : a.width) / Granule<BITS>::COLUMNS, items = experts * (GATED ? a.width / 16 : a.hidden / 32);
+    const int64_t units = (GATED ? a.hidden : a.width) / Granule<BITS>::COLUMNS, items = experts * (GATED ? a.width / 16 : a.hidden / 32);
+    if constexpr (T == 4) {
+        if (items <= 512 && units >= 16) {
+            launch_rows<BITS, T, 16, 8, 8, GATED>(a, s);
+            return;
+        }
+    }
     if constexpr (BITS == 4) launch_rows<BITS, T, 16, 4, 8, GATED>(a, s);
     else if (units < 16 && items >= 2048) launch_rows<BITS, T, 16, 2, 4, GATED>(a, s);
     else launch_rows<BITS, T, 16, 4, 4, GATED>(a, s);

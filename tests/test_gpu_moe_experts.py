@@ -59,6 +59,18 @@ def test_sizes(layers, bits, hidden, width):
         check_experts(e, run_experts(w, x, ids, gates), x, ids, gates, None, f"{e.hidden} x {e.width}, {rows} rows")
 
 
+@pytest.mark.parametrize("bits", (1, 2, 3, 4))
+@pytest.mark.parametrize("hidden,width", ((16, 1), (1, 17), (31, 1)))
+def test_few_long_rows(layers, bits, hidden, width):
+    """Eight waves a row, one to four super-blocks each."""
+    e, w = layers(3, hidden * UNIT[bits], width * UNIT[bits], bits)
+    g = np.random.default_rng(hidden + 50 * width)
+    for rows in (1, 3, 5, 8):
+        ids, gates = choices(g, rows, 3, 2)
+        x, res = tokens(g, rows, e.hidden), tokens(g, rows, e.hidden)
+        check_experts(e, run_experts(w, x, ids, gates, res), x, ids, gates, res, f"{e.hidden} x {e.width}, {rows} rows")
+
+
 @pytest.mark.parametrize("bits", (2, 4))
 @pytest.mark.parametrize("experts,top_k,rows", ((1, 1, 1), (1, 1, 40), (2, 1, 128), (64, 16, 3), (64, 16, 128), (200, 10, 9)))
 def test_numbers_of_experts(layers, bits, experts, top_k, rows):
