@@ -694,11 +694,12 @@ static void launch_few(const MoeArgs& a, hipStream_t s) {
 // us with 4 / 8 at a time: 16 tokens of 128 experts, 8 each, 4 bits 64 / 66, a layer of them 177 / 183; 5 tokens of 8 experts, 2 each, 2 bits 103 / 127;
 // but 16 tokens of 64 experts, 8 each, 3 bits 126 / 119.  More than 16 tokens take 16 at a time (32: 128 tokens of 64 experts, 6 each, 3 bits 137 -> 171), which eight
 // teams of two waves share in shared memory (every wave for itself from the caches: 122 -> 105; 64 tokens, 4 bits 130 -> 98; 100 tokens, 2 bits 131 -> 86).  Four
-// teams of four take 120, eight of one 119; 1 bit needs the registers of eight waves (40 tokens of 128 experts 205 -> 180; as sixteen, spilled, 250).  For 16 rows
-// and fewer it does not pay (16 tokens of 8 experts of 4096 x 14336, 4 bits 170 -> 190).
+// teams of four take 120, eight of one 119; 1 bit needs the registers of eight waves (40 tokens of 128 experts 205 -> 180; as sixteen, spilled, 250).  Eight waves a row where
+// eight teams would leave half of the units without work (53 tokens of 3 of 4 experts of 2048 x 7168, 4 bits 80 -> 61, 60 tokens of 2048 x 8192, 1 bit 56 -> 36.5; at twice
+// that many items 20 tokens of 16 of 3328 x 5120, 4 bits 82 -> 78, but 40 of 8 of 4096 x 14336, 2 bits 185 -> 196).  For 16 rows and fewer sharing tokens does not pay (16 tokens of 8 experts of 4096 x 14336, 4 bits 170 -> 190).
 template <int BITS, bool GATED>
 static void launch_product(const MoeArgs& a, hipStream_t s) {
-    const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = a.experts;
+    const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = a.experts, items = ((pairs < experts ? pairs : experts) + pairs / 16) * (GATED ? a.width / 128 : a.hidden / 256);
     if (a.rows <= 4 || (a.rows <= 16 && 2 * pairs <= (BITS == 1 ? 6 : 3) * experts)) {
         launch_few<BITS, 4, GATED>(a, s);
         return;
@@ -713,7 +714,8 @@ static void launch_product(const MoeArgs& a, hipStream_t s) {
     // (eight teams need row blocks in sixteens: the down projection's pairs of them come in fours)
     else {
         constexpr int WAVES = BITS == 1 ? 8 : 16;
-        if (GATED || a.hidden % 256 == 0) launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, WAVES / 8, WAVES, GATED>(a, s);
+        if (items <= 128) launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, 8, WAVES, GATED>(a, s);
+        else if (GATED || a.hidden % 256 == 0) launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, WAVES / 8, WAVES, GATED>(a, s);
         else launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, WAVES / 4, WAVES, GATED>(a, s);
     }
 }

@@ -71,6 +71,22 @@ def test_few_long_rows(layers, bits, hidden, width):
         check_experts(e, run_experts(w, x, ids, gates, res), x, ids, gates, res, f"{e.hidden} x {e.width}, {rows} rows")
 
 
+@pytest.mark.parametrize("bits,hidden,width", [(b, *s) for b in (1, 2, 3, 4) for s in ((2560, 512), (512, 2560))] + [(3, 640, 384), (4, 640, 384)])
+def test_many_tokens_of_many_experts(bits, hidden, width):
+    """Work for every unit: up to 16 tokens at a time and more, rows of one piece and of several, numbers of them that teams do not share evenly."""
+    e = Experts(bits, 4, hidden, width, bits)
+    of = np.arange(40) % 4                                                       # 40 experts that are four
+    pick = torch.from_numpy(of).cuda()
+    w = kmq.MoeWeights(*(t[pick].contiguous() for t in e.on_device().tensors), 40, hidden, width, bits)
+    g = np.random.default_rng(hidden + bits)
+    ids, gates = choices(g, 70, 40, 8)
+    ids[:, 7][(ids[:, :7] != 33).all(1)] = 33                                    # one that all tokens have
+    x, res = tokens(g, 70, hidden), tokens(g, 70, hidden)
+    got = run_experts(w, x, ids, gates, res)
+    check_experts(e, got, x, of[ids].astype(np.int32), gates, res, "", range(0, 70, 6))
+    assert np.array_equal(run_experts(w, x, ids, gates, res), got)
+
+
 @pytest.mark.parametrize("bits", (2, 4))
 @pytest.mark.parametrize("experts,top_k,rows", ((1, 1, 1), (1, 1, 40), (2, 1, 128), (64, 16, 3), (64, 16, 128), (200, 10, 9)))
 def test_numbers_of_experts(layers, bits, experts, top_k, rows):
