@@ -487,21 +487,26 @@ def moe_route_workspace_bytes(rows: int, experts: int, width: int) -> int:
 _choice_types = None
 
 
-def _check_choices(ids, gates):
-    """(64-bit ids, as they come from torch.topk, would be read as twice as many.)"""
+def _check_choices(ids, gates, count: int):
+    """Of a type that is read as another (64-bit ids, as they come from torch.topk), too few, or not in one piece (a view of the first columns).
+    The ABI has no sizes and strides for them, and the router writes them: looked at in every call, 0.4 us of it."""
     global _choice_types
     if _choice_types is None:
         import torch
         _choice_types = (torch.int32, torch.float32)
-    if ids.dtype is not _choice_types[0] or gates.dtype is not _choice_types[1]:
+    if ids.dtype is not _choice_types[0] or gates.dtype is not _choice_types[1] or ids.numel() < count or gates.numel() < count:
+        raise KmqError(3)
+    if not (ids.is_contiguous() and gates.is_contiguous()):
         raise KmqError(3)
 
 
 def moe_route(x, x_stride: int, rows: int, router, experts: int, width: int, ids, gates, top_k: int, sigmoid: bool = False, bias=None, groups: int = 1,
               top_groups: int = 1, normalise: bool = True, scale: float = 1.0, workspace=None):
-    """Experts of every row of x (ids int32, gates fp32; rows x top_k) by a router of experts x width bf16, on torch's current stream.
-    workspace: moe_route_workspace_bytes() device bytes."""
-    _check_choices(ids, gates)
+    """Experts of every row of x (ids int32, gates fp32; rows x top_k, contiguous) by a router of experts x width bf16 and a bias of fp32, on
+    torch's current stream.  workspace: moe_route_workspace_bytes() device bytes."""
+    _check_choices(ids, gates, rows * top_k)
+    if bias is not None and (bias.dtype is not _choice_types[1] or bias.numel() < experts or not bias.is_contiguous()):
+        raise KmqError(3)
     r = _RouterStruct(_ptr(router), _ptr(bias), width, experts, top_k, groups, top_groups, 1 if sigmoid else 0, 1 if normalise else 0, scale)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(_lib.kmq_moe_route(_ptr(x), x_stride, rows, ctypes.addressof(r), _ptr(ids), _ptr(gates), _ptr(workspace), ws_bytes, _stream()))
@@ -537,8 +542,8 @@ def moe_experts_workspace_bytes(weights: MoeWeights, rows: int, top_k: int) -> i
 def moe_experts(weights: MoeWeights, x, x_stride: int, rows: int, ids, gates, top_k: int, y, y_stride: int, residual=None, residual_stride: int = 0,
                 workspace=None):
     """y = residual + sum over a row's top_k experts of gate * down(silu(gate x) * up x), for up to MOE_MAX_ROWS rows, on torch's current
-    stream.  workspace: moe_experts_workspace_bytes() device bytes."""
-    _check_choices(ids, gates)
+    stream.  ids and gates as in moe_route.  workspace: moe_experts_workspace_bytes() device bytes."""
+    _check_choices(ids, gates, rows * top_k)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(_lib.kmq_moe_experts(weights._at, _ptr(x), x_stride, rows, _ptr(ids), _ptr(gates), top_k, _ptr(residual), residual_stride, _ptr(y), y_stride,
                                 _ptr(workspace), ws_bytes, _stream()))
