@@ -710,14 +710,23 @@ static void launch_product(const MoeArgs& a, hipStream_t s) {
             return;
         }
     }
-    if (a.rows <= 16) launch_rows<BITS, 16, 16, 2, 4, GATED>(a, s);
-    // (eight teams need row blocks in sixteens: the down projection's pairs of them come in fours)
-    else {
-        constexpr int WAVES = BITS == 1 ? 8 : 16;
-        if (items <= 128) launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, 8, WAVES, GATED>(a, s);
-        else if (GATED || a.hidden % 256 == 0) launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, WAVES / 8, WAVES, GATED>(a, s);
-        else launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, WAVES / 4, WAVES, GATED>(a, s);
+    if (a.rows <= 16) {
+        launch_rows<BITS, 16, 16, 2, 4, GATED>(a, s);
+        return;
     }
+    constexpr int WAVES = BITS == 1 ? 8 : 16;
+    if (items <= 128) {
+        launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, 8, WAVES, GATED>(a, s);
+        return;
+    }
+    // (eight teams need row blocks in sixteens: the down projection's pairs of them come in fours at 3 and 4 bits)
+    if constexpr (!GATED && BITS >= 3) {
+        if (a.hidden % 256 != 0) {
+            launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, WAVES / 4, WAVES, GATED>(a, s);
+            return;
+        }
+    }
+    launch_rows<BITS, 16, KMQ_MOE_MAX_ROWS, WAVES / 8, WAVES, GATED>(a, s);
 }
 
 template <int BITS>
