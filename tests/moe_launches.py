@@ -83,3 +83,19 @@ def reachable():
                         for i, how in both(bits, rows, top_k, experts, hidden, width):
                             found.setdefault(i, set()).update(how)
     return found
+
+
+# (bits, rows, top_k, experts, hidden, width): between them every instance and every path, most of them short in the other direction
+CASES = (
+    (1, 1, 2, 4, 512, 4608), (1, 1, 2, 4, 4608, 512), (1, 1, 2, 4, 8704, 512), (1, 3, 1, 2, 512, 8704), (1, 16, 2, 4, 512, 4608),
+    (1, 16, 2, 4, 4608, 512), (1, 16, 8, 64, 7680, 512), (1, 16, 8, 128, 512, 7680), (1, 20, 2, 3, 512, 2560), (1, 20, 2, 3, 2560, 512),
+    (1, 24, 6, 24, 5120, 512), (1, 70, 8, 40, 512, 4608), (2, 3, 1, 2, 256, 4352), (2, 3, 1, 2, 4352, 256), (2, 5, 2, 4, 256, 8448),
+    (2, 12, 8, 64, 7424, 256), (2, 16, 2, 4, 256, 6400), (2, 16, 2, 8, 6400, 256), (2, 16, 4, 32, 2048, 2048), (2, 16, 4, 32, 7424, 256),
+    (2, 16, 8, 128, 256, 7424), (2, 16, 8, 128, 512, 2048), (2, 16, 8, 128, 2048, 256), (2, 20, 2, 3, 256, 2560), (2, 20, 2, 3, 2304, 256),
+    (2, 70, 8, 40, 512, 4352), (2, 70, 8, 40, 4352, 256), (3, 4, 4, 16, 128, 4224), (3, 4, 4, 16, 4352, 128), (3, 5, 2, 4, 128, 5760),
+    (3, 12, 8, 64, 384, 6784), (3, 12, 8, 64, 1408, 1408), (3, 16, 2, 4, 128, 5248), (3, 16, 2, 4, 5248, 128), (3, 16, 4, 32, 5760, 128),
+    (3, 16, 8, 64, 1024, 896), (3, 16, 8, 128, 6784, 128), (3, 20, 2, 3, 128, 2176), (3, 40, 4, 16, 2176, 128), (3, 70, 8, 40, 512, 3328),
+    (3, 70, 8, 40, 640, 4224), (3, 70, 8, 40, 3328, 256), (4, 3, 1, 2, 128, 7296), (4, 3, 1, 2, 7680, 128), (4, 5, 2, 4, 128, 5760),
+    (4, 5, 2, 4, 5760, 128), (4, 16, 2, 4, 128, 5248), (4, 16, 2, 4, 5248, 128), (4, 16, 4, 64, 384, 5760), (4, 16, 8, 128, 5760, 128),
+    (4, 20, 2, 3, 1152, 128), (4, 40, 2, 4, 128, 1152), (4, 70, 8, 40, 512, 2048), (4, 70, 8, 40, 640, 1152), (4, 70, 8, 40, 2048, 256),
+)

@@ -1,4 +1,5 @@
-"""The instances of the experts' row kernel in the built library are those that calls reach."""
+"""The instances of the experts' row kernel in the built library are those that calls reach, and the tests on the GPU go through all
+that each of them does with a row."""
 import os
 import re
 import subprocess
@@ -6,7 +7,7 @@ import subprocess
 import pytest
 
 from paper_2602_15563_amd import kmq
-from tests.moe_launches import Instance, reachable
+from tests.moe_launches import CASES, Instance, both, reachable
 from tests.test_lds_reads_in_flight import device_code
 from tests.test_matrix_core_scratch import READELF
 
@@ -22,3 +23,11 @@ def test_every_instance_is_reached(tmp_path):
     reached = set(reachable())
     assert not reached - built, "the rules written out in moe_launches.py are not the library's"
     assert not built - reached, "built for no call"
+
+
+def test_the_cases_go_through_every_path():
+    seen = {}
+    for case in CASES:
+        for i, how in both(*case):
+            seen.setdefault(i, set()).update(how)
+    assert seen == reachable()
