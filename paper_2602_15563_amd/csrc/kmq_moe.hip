@@ -2,17 +2,20 @@
 //
 //     h_p = silu(G_e x) * (U_e x),   y = residual + sum_j gate_j * D_e h_p            pair p = (token, j), e = its expert
 //
-// Every expert that some token chose is read once.  The kernels build the list of these experts from the choices themselves (so the
-// launches do not depend on them, and a captured call may be replayed with others) and gather the tokens of an expert as the
-// columns of matrix steps: v_mfma_f32_16x16x32_bf16 with the tokens first, so that what belongs to a row of the
-// matrix (its scales) is needed by the lane that holds it.  Columns do not mix: what one token holds reaches no other.
+// An expert that some token chose is read once for every T (4, 8 or 16) of its tokens, the repeats mostly from the L2; the others are not
+// read.  The kernels build the list of these experts from the choices themselves (so the launches do not depend on them, and a captured call
+// may be replayed with others) and gather the tokens of an expert as the columns of matrix steps: v_mfma_f32_16x16x32_bf16 with the tokens
+// first, so that what belongs to a row of the matrix (its scales) is needed by the lane that holds it.  Columns do not mix: what one token
+// holds reaches no other.
 //
-// Three launches: the rows of G and U (SwiGLU of both goes to the workspace, a row a pair, rounded to bf16), the rows of D (a row a pair
-// again, in fp32), and the sum of a token's pairs.  The first two are one kernel: a wave multiplies 16 rows of two matrices with the same
-// tokens, the gate's and the up projection's, or two blocks of the down projection.  NW waves (a team) split the rows' length, their
-// sums are added in shared memory; the teams of a workgroup share the table of the expert's centroids.  A workgroup takes neighbouring
-// rows of the list of all experts' rows, as many as any other; the first super-blocks of what comes next are asked for before the
-// sums are joined.  Above 16 rows the 16 tokens of an item stand in shared memory as operands, for all of the workgroup's waves.
+// Three launches: the rows of G and U (SwiGLU of both goes to the workspace, a row a pair, rounded to bf16: the matrix instruction takes no
+// more, and two parts of it would double the second product's steps; of an output without a residual the r.m.s. error is 0.0024 with it,
+// 0.0017, the output's own rounding, without), the rows of D (a row a pair again, in fp32), and the sum of a token's pairs.  The first two
+// are one kernel: a wave multiplies 16 rows of two matrices with the same tokens, the gate's and the up projection's, or two blocks of the
+// down projection.  NW waves (a team) split the rows' length, their sums are added in shared memory; the teams of a workgroup share the
+// table of the expert's centroids.  A workgroup takes neighbouring rows of the list of all experts' rows, as many as any other; the first
+// super-blocks of what comes next are asked for before the sums are joined.  Above 16 rows the 16 tokens of an item stand in shared memory
+// as operands, for all of the workgroup's waves.
 //
 // What bounds it: 4 bits, 16 tokens of 128 experts of 4096 x 1536, the memory (90 + 57 us, 4.9 TB/s); 2 bits, five tokens of 8 experts of 4096 x 14336, the decode
 // (62 + 37 us, of which vector issue 32 + 15, look-ups as much); one token, 6 to 8 experts, latencies (15 + 10 us, 6 before the first products in each).
@@ -22,8 +25,8 @@
 // Decode: tables in shared memory whose entries are ready operand registers, a column a lane modulo 32, so that look-ups never collide
 // whatever the indices are.  2 to 4 bits: a pair of indices (4, 6, 8 bits of a byte of the granule) is an entry of two centroids; at 2 and 3
 // bits it is elements k and k + 4 of a step, and the tokens' elements are brought into that order.  1 bit: four indices, eight bytes.  The
-// index goes into byte 1 of the address by one instruction.  (2 bits with four indices too, half the instructions for the same bytes: 109 us and 110, five tokens of 8
-// experts; what a token's sums cost behind the next item's barrier instead of ahead of it: no difference.)
+// index goes into byte 1 of the address by one instruction.  (2 bits with four indices too, half the instructions for the same bytes: 109 us and 110, five tokens, 2 of 8
+// experts of 4096 x 14336; what a token's sums cost behind the next item's barrier instead of ahead of it: no difference.)
 #include <cstddef>
 #include <type_traits>
 
@@ -34,12 +37,12 @@ namespace kmq {
 
 namespace {
 
-// Bundles a wave has asked for, by their registers: what fits beside the rest without spilling in the loop.  (Three instead of two, spilled: one
-// token, 4 bits 31 -> 57 us, 16 tokens 76 -> 144.)  With tokens in shared memory two: sixteen waves a unit ask for enough (three, four: 105, 107 of 105 us at 3 bits, 101,
-// 108 of 98 at 4).
+// Bundles a wave has asked for, by their registers: what fits beside the rest.  (Three instead of two, 16 tokens, 8 of 128 experts of 4096 x 1536: 2 bits 132 ->
+// 149 us, 4 bits 166 both; one token, 4 bits 30 -> 31.5.)  With tokens in shared memory two: sixteen waves a unit ask for enough (three, four: 128 tokens, 6 of 64
+// experts of 2048 x 1408, 3 bits 100 -> 105, 105; 64 tokens of them, 4 bits 97 -> 101, 107).
 constexpr int depth(int words) { return words <= 10 ? 3 : 2; }
 // Waves a SIMD that the registers have to leave room for.  (1 bit, few tokens: what is kept over an item and does not fit, 5 to 7 words, is spilled outside the
-// loop; two waves instead 111 -> 132 us, 16 tokens of 128 experts.)
+// loop; two waves instead 113 -> 129 us, 16 tokens, 8 of 128 experts of 4096 x 1536.)
 constexpr int waves_for(int bits, int t, bool staged) { return staged ? (bits == 1 ? 2 : 4) : (t == 16 && (bits == 2 || bits == 4)) ? 2 : bits == 1 || (bits == 2 && t == 8) || t == 16 ? 3 : 4; }
 
 typedef __amdgpu_buffer_rsrc_t Rows;
@@ -225,7 +228,7 @@ __device__ __forceinline__ int sum_upto(int v) {
     return v;
 }
 // Which tokens an expert has, a bit each, gives their number and every pair's place.  (Counted and ranked by ballots over all pairs, expert by expert, when one was
-// needed: 6 us more of 128 tokens.)  The bits stand in memory that is not used yet, with them
+// needed: 6 us more for 128 tokens, 6 of 64 experts.)  The bits stand in memory that is not used yet, with them
 // where the expert's pairs begin.
 template <int ROWS>
 struct Bits {
@@ -476,7 +479,7 @@ __global__ __launch_bounds__(NW * TEAMS * kWave) __attribute__((amdgpu_waves_per
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave / NW, member = wave % NW;
     const auto lane_anew = [] { return anew(static_cast<int>(threadIdx.x)) & 63; };
     const int kept = threadIdx.x & 63;
-    // (at 1 bit there is no register to keep it in: 122 -> 111 us, 16 tokens of 128 experts; elsewhere 2 to 6 % more)
+    // (at 1 bit there is no register to keep it in: 118 -> 113 us, 16 tokens, 8 of 128 experts of 4096 x 1536; at 2 to 4 bits it would cost 4 to 6 % there)
     const auto lane_kept = [&] { return BITS == 1 ? lane_anew() : kept; };
     const auto place = [&] { return member * kWave + lane_anew(); };        // in the team
     static_assert(offsetof(Sm, choices) >= sizeof(uint32_t) * Bits<ROWS>::STRIDE * KMQ_MOE_MAX_EXPERTS, "bits");      // (what lies before is filled later)
@@ -671,10 +674,12 @@ static void launch_rows(const MoeArgs& a, hipStream_t s) {
     moe_rows_kernel<BITS, T, ROWS, NW, TEAMS, GATED><<<dim3(static_cast<unsigned>(items < MOST ? items : MOST)), WAVES * kWave, 0, s>>>(a);
 }
 
-// Waves that split a row: four, or two where rows are short (fewer than 16 super-blocks) and there are enough of them (16 tokens of 128 experts of
-// 4096 x 1536, 1 bit: 166 us with four, 147 with two; 3 bits 120 and 107).  At 4 bits eight waves share the table, 64 KB, and two of them a row are slower
-// throughout (2048 x 768, 16 tokens: 66 with four, 75).  Eight where few long rows would leave units without work (one token: an expert of 2176 x 15744, 3 bits
-// 43 -> 35.5; two of 4096 x 14336, 4 bits 60 -> 53; up to 1024 items instead: two of 7040 x 8576, 4 bits 59 -> 57, but four of 3840 x 8704, 3 bits 63 -> 66).
+// Waves that split a row (us, `rows` tokens, top_k of experts, hidden x width): four, or two where rows are short (fewer than 16 super-blocks) and there are enough of
+// them (16, 8 of 128, 4096 x 1536: 1 bit 112 with two, 122 with four; 2 bits 125, 136; 3 bits 144, 149).  At 4 bits eight waves share the table, 64 KB, and two of
+// them a row are slower (the same 164 with four, 197 with two; 2048 x 768 62 and 74).  Eight where few long rows would leave units without work (one token, 1
+// expert of 2176 x 15744, 3 bits 35.8, with four 42.7; 2 of 4096 x 14336, 4 bits 52, 60.5; 2 of 7040 x 8576, 4 bits 56, 58.5; 4 of 3840 x 8704, 3 bits 49, 51).  Up to 1024
+// items instead of 512 it no longer pays (one token, 8 of 4096 x 1536: 2 bits 24.3 -> 24.9, 3 bits 26.4 -> 26.9, 4 bits 30.7 -> 30.1; 4 of 4096 x 3584, 4 bits 32.1 -> 32.7; two
+// tokens, 8 of 64, 2048 x 1024, 4 bits 24.4 -> 25.1).
 template <int BITS, int T, bool GATED>
 static void launch_few(const MoeArgs& a, hipStream_t s) {
     const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = pairs < a.experts ? pairs : a.experts;
@@ -690,13 +695,15 @@ static void launch_few(const MoeArgs& a, hipStream_t s) {
     else launch_rows<BITS, T, 16, 4, 4, GATED>(a, s);
 }
 
-// Tokens at a time: where more of them choose an expert its rows are read again (from the L2, mostly), and every four more cost registers and loads.
-// us with 4 / 8 at a time: 16 tokens of 128 experts, 8 each, 4 bits 64 / 66, a layer of them 177 / 183; 5 tokens of 8 experts, 2 each, 2 bits 103 / 127;
-// but 16 tokens of 64 experts, 8 each, 3 bits 126 / 119.  More than 16 tokens take 16 at a time (32: 128 tokens of 64 experts, 6 each, 3 bits 137 -> 171), which eight
-// teams of two waves share in shared memory (every wave for itself from the caches: 122 -> 105; 64 tokens, 4 bits 130 -> 98; 100 tokens, 2 bits 131 -> 86).  Four
-// teams of four take 120, eight of one 119; 1 bit needs the registers of eight waves (40 tokens of 128 experts 205 -> 180; as sixteen, spilled, 250).  Eight waves a row where
-// eight teams would leave half of the units without work (53 tokens of 3 of 4 experts of 2048 x 7168, 4 bits 80 -> 61, 60 tokens of 2048 x 8192, 1 bit 56 -> 36.5; at twice
-// that many items 20 tokens of 16 of 3328 x 5120, 4 bits 82 -> 78, but 40 of 8 of 4096 x 14336, 2 bits 185 -> 196).  For 16 rows and fewer sharing tokens does not pay (16 tokens of 8 experts of 4096 x 14336, 4 bits 170 -> 190).
+// Tokens at a time (us, as above): where more of them choose an expert its rows are read again (from the L2, mostly), and every four more cost registers and loads.  With
+// 4 / 8 / 16 at a time: 16 tokens, 8 of 128, 4096 x 1536, 2 bits 129 / 140 / 168, 3 bits 147 / 143, 4 bits 164 / 163 / 184; 5 tokens, 2 of 8, 4096 x 14336, 2 bits 102 / 113 /
+// 125; but 16 tokens, 8 of 64, 4096 x 1536, 3 bits 119 / 113 / 120, and 2 of 8, 4096 x 14336, 4 bits 197 with 4, 166 with 16, 1 bit 131 and 127.
+// More than 16 tokens take 16 at a time (32: 128 tokens, 6 of 64, 2048 x 1408, 3 bits 137 -> 171 before tokens were shared), which eight teams of two waves share in shared
+// memory (every wave for itself from the caches: these 122 -> 105; 64 of them, 4 bits 130 -> 98; 100, 2048 x 1536, 2 bits 131 -> 86).  Four teams of four: 98 -> 112, 97 -> 108, 86 ->
+// 103.  1 bit needs the registers of eight waves (40 tokens, 8 of 128, 4096 x 1536: 180; sixteen, spilled, 250; four teams of two 232).
+// Eight waves a row where eight teams would leave half of the units without work (53 tokens, 1 of 4, 2048 x 7168, 4 bits 59, without 78; 60 tokens, 1 of 4, 2048 x 8192, 1 bit 35,
+// 55); at twice that many items no longer (20 tokens, 1 of 16, 3328 x 5120, 4 bits 107 -> 122; 40, 2 of 8, 4096 x 14336, 2 bits 174 -> 189).  For 16 rows and fewer sharing tokens
+// does not pay (16 tokens, 2 of 8, 4096 x 14336, 4 bits 166 -> 191, 1 bit 127 -> 142; 8 of 64, 4096 x 1536, 3 bits 112 -> 111).
 template <int BITS, bool GATED>
 static void launch_product(const MoeArgs& a, hipStream_t s) {
     const int64_t pairs = static_cast<int64_t>(a.rows) * a.top_k, experts = a.experts, items = ((pairs < experts ? pairs : experts) + pairs / 16) * (GATED ? a.width / 128 : a.hidden / 256);
