@@ -450,8 +450,8 @@ const char* kmq_kernel_name_kv_attention(const kmq_kv_cache* cache, const kmq_kv
  *     n = x * post_gain / sqrt( (1/H) sum_j x_j^2 + eps )      (post_norm = 1; else n = x)
  *     s = residual_scale * residual + scale * g * n            g = gate, or 1 / (1 + exp(-gate)) where gate_sigmoid is 1, or 1
  *     out = s,   normed = s * pre_gain / sqrt( (1/H) sum_j s_j^2 + eps )
- * Computed in 64 bits (s goes into the second norm unrounded), rounded to 32 and then to bf16 (nearest even); infinities and NaN as the
- * formulas have them. */
+ * Computed in 64 bits (s goes into the second norm unrounded; the order of the sums depends on the number of rows), rounded to 32 and then to
+ * bf16 (nearest even); infinities and NaN as the formulas have them. */
 typedef struct kmq_block_join {
     const uint16_t* residual;   /* rows of H bf16, or NULL: none (zeros) */
     const uint16_t* gate;       /* rows of H bf16, or NULL */
@@ -479,8 +479,9 @@ kmq_status kmq_block_norm(const uint16_t* x, int64_t x_stride, int64_t rows, int
  *     groups > 1: the experts are that many groups of neighbours; the top_groups of them whose two largest c have the largest sum stay
  *     the top_k experts with the largest c, in descending order; weight = s_e, divided by the sum of the chosen (normalise = 1; a sum of
  *     zero: weights of zero), times scale
- * Equal values go to the lower index.  A NaN counts as minus infinity for its group, and is chosen behind everything else.
- * Computed in 64 bits, weights rounded to fp32. */
+ * Equal values go to the lower index.  A NaN counts as minus infinity for its group, and is chosen behind everything else.  A group whose two
+ * largest are infinities of both signs has no sum: it comes behind all others.
+ * Computed in 64 bits, weights rounded to fp32.  The order of the 64-bit sums depends on the number of rows. */
 typedef struct kmq_moe_router {
     const uint16_t* weights;    /* experts x width bf16, 16-byte aligned */
     const float* bias;          /* one an expert, or NULL */
@@ -517,7 +518,8 @@ typedef struct kmq_moe_weights {
 /* The chosen experts' SwiGLU for a few tokens, in three launches (each active expert's matrices are read once for up to 16 of its tokens, fewer
  * where experts have few on average):
  *     h = bf16( silu(G_e x) * (U_e x) ),   y = residual + sum_j gates[j] * D_e h           e = ids[j], j = 0 .. top_k - 1
- * silu(t) = t / (1 + exp(-t)); all sums in fp32, h rounded to bf16 as kmq_gemv_swiglu leaves it (2^-8 of itself at most), y once more.
+ * silu(t) = t / (1 + exp(-t)) in fp32 (zero below -88.7, where the exponential is an infinity: 3e-37 at most of U_e x is lost); all sums in fp32, h
+ * rounded to bf16 as kmq_gemv_swiglu leaves it (2^-8 of itself at most), y once more.
  * What is not finite is as the formulas have it; it reaches the outputs of the tokens that chose the expert, or of that token, alone.
  *   x, residual, y   rows of `hidden` elements, x_stride at most 2^22; residual may be NULL, and y's own place
  *   ids, gates       rows x top_k, from kmq_moe_route or anybody else.  An id outside 0 .. experts - 1 counts for nothing (an expert
@@ -525,7 +527,9 @@ typedef struct kmq_moe_weights {
  *   workspace        kmq_moe_experts_workspace_bytes() bytes, 16-byte aligned, not initialised (0 on bad arguments)
  * rows: 0 .. KMQ_MOE_MAX_ROWS (KMQ_ERR_SHAPE); more are cut into several calls, and prompts are better served by kmq_dequant_blockscaled
  * and dense products.  Launches and workspace do not depend on the choices, so a captured call may be replayed with others.  A token's
- * output depends on no other token's elements; experts that are not chosen are not read. */
+ * output depends on no other token's elements or choices, and calls of the same numbers agree bit for bit; the order of its sums depends on
+ * rows, top_k and the number of experts, so that the same token may differ by a rounding between batches of different sizes.  Experts that
+ * are not chosen are not read. */
 size_t kmq_moe_experts_workspace_bytes(const kmq_moe_weights* weights, int64_t rows, int top_k);
 kmq_status kmq_moe_experts(const kmq_moe_weights* weights, const uint16_t* x, int64_t x_stride, int64_t rows, const int32_t* ids,
                            const float* gates, int top_k, const uint16_t* residual, int64_t residual_stride, uint16_t* y, int64_t y_stride,

@@ -11,7 +11,9 @@
 //
 // One token, 128 experts of 4096: 3.4 + 4.3 us, both chains of memory round trips (reading slices one by one took the second kernel 8.8); 16
 // tokens, 256 experts of 7168 in groups 4.6 + 7.9, of which the products' own time is about 1 and the choice's twelve rounds of a maximum over the wave
-// half; 128 tokens, 64 experts of 2048 6.5 + 3.9, the products of four waves a unit waiting for their operands.
+// half; 128 tokens, 64 experts of 2048 6.5 + 4.1: at four tiles a workgroup these are 64 workgroups, a quarter of the units, and of a wave's 5.7 us its 64 matrix
+// instructions of 64 clocks are 1.7 and waiting for memory 46 %.  Prompts: the 64-bit matrix instructions; 4001 rows, 128 experts of 4096 89 + 9 us, a unit's
+// busy for 54 of the 89 (7 us for the bytes).
 #include "kmq_kv.h"
 
 namespace kmq {
