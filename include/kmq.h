@@ -528,7 +528,7 @@ typedef struct kmq_moe_weights {
  * rows: 0 .. KMQ_MOE_MAX_ROWS (KMQ_ERR_SHAPE); more are cut into several calls, and prompts are better served by kmq_dequant_blockscaled
  * and dense products.  Launches and workspace do not depend on the choices, so a captured call may be replayed with others.  A token's
  * output depends on no other token's elements or choices, and calls of the same numbers agree bit for bit; the order of its sums depends on
- * rows, top_k and the number of experts, so that the same token may differ by a rounding between batches of different sizes.  Experts that
+ * rows, top_k and the number of experts, so that the same token may differ in its last bits between batches of different sizes.  Experts that
  * are not chosen are not read. */
 size_t kmq_moe_experts_workspace_bytes(const kmq_moe_weights* weights, int64_t rows, int top_k);
 kmq_status kmq_moe_experts(const kmq_moe_weights* weights, const uint16_t* x, int64_t x_stride, int64_t rows, const int32_t* ids,
